@@ -313,6 +313,83 @@ int  pserve_resample_workspace(const pserve_resample_t* op, const pserve_plan_t*
 int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* plan_in, const pserve_plan_t* plan_out,
                              const void* x, void* workspace, size_t workspace_bytes, void* y, void* stream);
 
+/* ---- the prompt side: operators of the causal text transformer that turns the prompts of a batch into the text rows of
+ * the block, and of one that extends short prompts token by token (no operation of the paper, whose text encoder is a given).
+ * None of them allocates device memory after its create call; all can be captured into a graph.
+ *
+ * pserve_prompt_attention: attention over packed sequences of different lengths, causal, with grouped heads.
+ *   q, o  DEVICE [q_tokens][heads][head_dim], k, v DEVICE [k_tokens][kv_heads][head_dim], of desc.dtype (fp32 statistics and
+ *   accumulation; bf16: the probabilities are rounded to bf16 for the matrix cores).  Strides in elements between tokens and
+ *   between heads; a head's values are consecutive.  cu_q, cu_k DEVICE int32 [n + 1]: sequence s has the queries
+ *   cu_q[s] .. cu_q[s + 1] - 1 and the keys cu_k[s] .. cu_k[s + 1] - 1 (ascending; what points outside q_tokens / k_tokens is
+ *   cut off there).  Head h reads key/value head h / (heads / kv_heads).
+ *   The queries of a sequence of L_q queries and L_k keys stand at the END of its keys: with causal != 0 query i sees the keys
+ *   j <= i + L_k - L_q, else all keys of its sequence.  A query that sees no key gives zeros.  Rows of o in front of the first
+ *   and behind the last sequence are left as they are.  A key or value that a query does not see has no part in its result,
+ *   whatever it holds; one that is not finite makes the results of the queries that see it NaN or infinite.
+ *   max_q, max_k: the longest L_q and L_k as far as the caller knows (0: unknown).  Only the choice of kernel and of the
+ *   number of shares of the keys depends on them, never which keys count.
+ *   workspace DEVICE, at least pserve_prompt_attention_workspace bytes (0 where none is needed; it holds the partial results
+ *   of the shares and may be used for something else after the call in stream order).  o must not overlap an input.
+ * Errors: EINVAL (NULL, n <= 0, heads % kv_heads, head_dim not a multiple of 16 or above 128, unknown dtype, negative sizes,
+ * pointers or strides that are no multiples of 16 bytes, a scale that is not finite, workspace too small), EHIP.
+ *
+ * pserve_kv8: keys and values of `places` tokens in 8 bits.  A token's head is a group of head_dim values with one fp32 scale
+ * amax / 127, each value a whole number 127 x / amax rounded to nearest (halves to even; exact); a group with an infinity or a
+ * NaN reads back as NaN throughout.  head_dim + 4 bytes a group instead of 2 head_dim.  A new store holds zeros.
+ * pserve_kv8_write: k, v DEVICE rows of desc-like strides (elements between tokens, between heads); row i goes to places[i]
+ *   (DEVICE int64 [rows]).  A row whose place is negative or not below `places` is not written; of several rows of one call
+ *   with the same place the last one is.  Two writes that run at the same time must not share a place.
+ * pserve_kv8_read: the values of places[i] into row i of k and v, DEVICE [rows][kv_heads][head_dim] contiguous, each
+ *   rounded once to dtype; zeros where the place is out of range.
+ * pserve_kv8_attention: pserve_prompt_attention with keys and values in the store.  Key j of sequence s is token j % page of
+ *   page table[s][j / page], i.e. place table[s][j / page] * page + j % page; table DEVICE int32 [n][max_pages], key_len DEVICE
+ *   int32 [n] (cut to max_pages * page), page a power of two.  Keys on pages outside the store count as not there.  desc's
+ *   kv_heads and head_dim are the store's; its k / v fields (k_tokens, strides) are not read.
+ * Errors: EINVAL, also for a store of another device than the current one; ENOMEM; EHIP.
+ *
+ * pserve_linear8: y = x W + b (+ residual) with x and W in 8-bit integers.  W [K][N] is quantised once, a scale for each
+ * output channel; x [rows][K] in the call, a scale for each token (quantised as the store's groups are: a group is a column of W
+ * resp. a row of x).  The products are summed in 32-bit integers, exactly; y = sum * (scale_x * scale_w) + b + residual in
+ * fp32, rounded once.  A row of x (column of W) with an infinity or a NaN gives NaN.
+ * pserve_linear8_create: w DEVICE [K][N], b DEVICE [N] or NULL, of dtype; synchronises `stream`.  K + 4 bytes a column are
+ *   kept (rounded up to 128 values, columns to 256); the caller's buffers are not referenced afterwards.
+ * pserve_linear8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y),
+ *   y DEVICE [rows][N]; workspace DEVICE, 16-byte aligned, at least pserve_linear8_workspace bytes.  y must not overlap x.
+ * Errors: EINVAL (NULL, sizes <= 0, K above 131072, ldx < K, workspace too small, another device than the current one),
+ * ENOMEM, EHIP. */
+typedef struct {
+    int32_t n;                      /* sequences */
+    int32_t heads, kv_heads;        /* query heads, key/value heads */
+    int32_t head_dim;               /* multiple of 16, at most 128 */
+    int32_t dtype;                  /* PSERVE_F32 | PSERVE_BF16 */
+    int32_t causal;
+    float   scale;                  /* of the scores, usually 1 / sqrt(head_dim) */
+    int32_t max_q, max_k;           /* longest sequence, 0 = unknown */
+    int64_t q_tokens, k_tokens;     /* rows of q and o, of k and v */
+    int64_t q_stride[2], k_stride[2], v_stride[2], o_stride[2];     /* elements between tokens, between heads */
+} pserve_prompt_desc;
+int  pserve_prompt_attention_workspace(const pserve_prompt_desc* desc, size_t* bytes);
+int  pserve_prompt_attention(const pserve_prompt_desc* desc, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                             const int32_t* cu_k, void* workspace, size_t workspace_bytes, void* o, void* stream);
+
+typedef struct pserve_kv8_s pserve_kv8_t;
+int  pserve_kv8_create(int64_t places, int32_t kv_heads, int32_t head_dim, void* stream, pserve_kv8_t** out);
+void pserve_kv8_free(pserve_kv8_t* store);
+int  pserve_kv8_write(pserve_kv8_t* store, const void* k, const void* v, int dtype, const int64_t k_stride[2],
+                      const int64_t v_stride[2], const int64_t* places, int64_t rows, void* stream);
+int  pserve_kv8_read(const pserve_kv8_t* store, const int64_t* places, int64_t rows, int dtype, void* k, void* v, void* stream);
+int  pserve_kv8_attention(const pserve_kv8_t* store, const pserve_prompt_desc* desc, const void* q, const int32_t* cu_q,
+                          const int32_t* key_len, const int32_t* table, int32_t max_pages, int32_t page, void* workspace,
+                          size_t workspace_bytes, void* o, void* stream);
+
+typedef struct pserve_linear8_s pserve_linear8_t;
+int  pserve_linear8_create(int32_t K, int32_t N, int dtype, const void* w, const void* b, void* stream, pserve_linear8_t** out);
+void pserve_linear8_free(pserve_linear8_t* op);
+int  pserve_linear8_workspace(const pserve_linear8_t* op, int64_t rows, size_t* bytes);
+int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t ldx, int64_t rows, const void* residual,
+                            void* workspace, size_t workspace_bytes, void* y, void* stream);
+
 /* ---- host-side scheduler pieces (section "SLO-Aware Scheduler").  All pointers HOST; no GPU work; times in ms.
  *
  * pserve_task: a request as the scheduler sees it.  ddl = its SLO budget counted from arrival (DDL_i), standalone =

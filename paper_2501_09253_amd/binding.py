@@ -74,6 +74,13 @@ class _BlockParams(C.Structure):
     _fields_ = [("p", (C.c_void_p * MAX_PARAMS) * MAX_STAGES)]
 
 
+class _PromptDesc(C.Structure):
+    _fields_ = [("n", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("causal", C.c_int32), ("scale", C.c_float), ("max_q", C.c_int32), ("max_k", C.c_int32), ("q_tokens", C.c_int64),
+                ("k_tokens", C.c_int64), ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2), ("v_stride", C.c_int64 * 2),
+                ("o_stride", C.c_int64 * 2)]
+
+
 def library_path() -> str:
     return os.path.join(_HERE, "libpserve.so")
 
@@ -138,6 +145,20 @@ def lib() -> C.CDLL:
     L.pserve_resample_free.restype = None
     L.pserve_resample_workspace.argtypes = [vp, vp, C.POINTER(C.c_size_t)]
     L.pserve_resample_forward.argtypes = [vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    st2 = C.POINTER(i64)
+    L.pserve_prompt_attention_workspace.argtypes = [C.POINTER(_PromptDesc), C.POINTER(C.c_size_t)]
+    L.pserve_prompt_attention.argtypes = [C.POINTER(_PromptDesc), vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    L.pserve_kv8_create.argtypes = [i64, i32, i32, vp, C.POINTER(vp)]
+    L.pserve_kv8_free.argtypes = [vp]
+    L.pserve_kv8_free.restype = None
+    L.pserve_kv8_write.argtypes = [vp, vp, vp, C.c_int, st2, st2, vp, i64, vp]
+    L.pserve_kv8_read.argtypes = [vp, vp, i64, C.c_int, vp, vp, vp]
+    L.pserve_kv8_attention.argtypes = [vp, C.POINTER(_PromptDesc), vp, vp, vp, vp, i32, i32, vp, C.c_size_t, vp, vp]
+    L.pserve_linear8_create.argtypes = [i32, i32, C.c_int, vp, vp, vp, C.POINTER(vp)]
+    L.pserve_linear8_free.argtypes = [vp]
+    L.pserve_linear8_free.restype = None
+    L.pserve_linear8_workspace.argtypes = [vp, i64, C.POINTER(C.c_size_t)]
+    L.pserve_linear8_forward.argtypes = [vp, vp, i64, i64, vp, vp, C.c_size_t, vp, vp]
     _lib = L
     return L
 
@@ -481,6 +502,233 @@ class Resample:
     def close(self):
         if self._h:
             lib().pserve_resample_free(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---- the prompt side: causal attention over packed prompts, the 8-bit key/value store, 8-bit linear layers
+EINVAL = -1
+
+
+def _need(cond, msg: str):
+    """Argument checks of the calls below: PserveError as for those the library refuses itself."""
+    if not cond:
+        raise PserveError(EINVAL, msg)
+
+
+def _code(t, who: str) -> int:
+    import torch
+    _need(t.dtype in (torch.bfloat16, torch.float32), f"{who}: dtype {t.dtype} is neither bfloat16 nor float32")
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
+def _here(who: str, *tensors):
+    """Tensors (None: absent) on the current device: the library's kernels run there."""
+    import torch
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        _need(t is None or (t.is_cuda and t.device.index == dev), f"{who}: a tensor on {getattr(t, 'device', None)}, the current device is cuda:{dev}")
+
+
+def _ints(who: str, t, dtype, shape, name: str):
+    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(), f"{who}: {name} must be contiguous {dtype} {tuple(shape)}")
+
+
+def _workspace(need: int, workspace, device, who: str):
+    """The caller's workspace, or one from torch's allocator for this call: (pointer, bytes, what keeps it alive)."""
+    import torch
+    if workspace is None:
+        if need == 0:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    _need(workspace.is_contiguous(), f"{who}: the workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _apart(who: str, out, *inputs):
+    """`out` shares no byte with an input (dense or strided: the extents are compared)."""
+    def extent(t):
+        last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+        return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+    if out.numel() == 0:
+        return
+    o0, o1 = extent(out)
+    for t in inputs:
+        if t is not None and t.numel():
+            a0, a1 = extent(t)
+            _need(a1 <= o0 or o1 <= a0, f"{who}: the output overlaps an input")
+
+
+def _prompt_desc(who: str, q, o, n: int, kv_heads: int, causal: bool, scale, max_q: int, max_k: int) -> _PromptDesc:
+    _need(q.dim() == 3 and q.shape[1] > 0 and q.shape[2] > 0, f"{who}: q must be [tokens, heads, head_dim]")
+    _need(o.shape == q.shape and o.dtype == q.dtype, f"{who}: out must have q's shape and dtype")
+    _need(q.stride(2) == 1 and o.stride(2) == 1, f"{who}: the values of a head must be consecutive")
+    _need(o.numel() == 0 or (o.stride(0) >= o.shape[2] or o.shape[0] == 1) and (o.stride(1) >= o.shape[2] or o.shape[1] == 1),
+          f"{who}: rows of out overlap")
+    d = _PromptDesc()
+    d.n, d.heads, d.kv_heads, d.head_dim, d.dtype = n, q.shape[1], kv_heads, q.shape[2], _code(q, who)
+    d.causal, d.scale = int(bool(causal)), (q.shape[2] ** -0.5 if scale is None else float(scale))
+    d.max_q, d.max_k, d.q_tokens = int(max_q), int(max_k), q.shape[0]
+    d.q_stride[:], d.o_stride[:] = q.stride()[:2], o.stride()[:2]
+    return d
+
+
+def prompt_attention(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optional[float] = None, max_q: int = 0, max_k: int = 0,
+                     out=None, workspace=None):
+    """pserve_prompt_attention: q [Tq, heads, D], k and v [Tk, kv_heads, D] (any strides between tokens and heads that are
+    multiples of 16 bytes), cu_q and cu_k int32 [n + 1] on the device (cu_k = None: those of the queries); scale defaults to
+    1 / sqrt(D).  Rows of no sequence are not written.  `out` must lie apart from q, k and v, from its first to its last
+    byte.  Returns out [Tq, heads, D]."""
+    import torch
+    who = "prompt_attention"
+    cu_k = cu_q if cu_k is None else cu_k
+    _here(who, q, k, v, cu_q, cu_k, out, workspace)
+    _need(cu_q.dim() == 1 and cu_q.shape[0] >= 2, f"{who}: cu_q must be int32 [n + 1], n > 0")
+    _ints(who, cu_q, torch.int32, cu_q.shape, "cu_q")
+    _ints(who, cu_k, torch.int32, cu_q.shape, "cu_k")
+    _need(q.dim() == 3 and k.dim() == 3 and v.shape == k.shape and k.shape[2] == q.shape[2], f"{who}: q [Tq, heads, D], k and v [Tk, kv_heads, D]")
+    _need(k.dtype == q.dtype and v.dtype == q.dtype, f"{who}: q, k and v must have one dtype")
+    _need(k.stride(2) == 1 and v.stride(2) == 1, f"{who}: the values of a head must be consecutive")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    else:
+        _apart(who, out, q, k, v)
+    d = _prompt_desc(who, q, out, cu_q.shape[0] - 1, k.shape[1], causal, scale, max_q, max_k)
+    d.k_tokens = k.shape[0]
+    d.k_stride[:], d.v_stride[:] = k.stride()[:2], v.stride()[:2]
+    need = C.c_size_t()
+    _check(lib().pserve_prompt_attention_workspace(C.byref(d), C.byref(need)))
+    ws, nws, keep = _workspace(need.value, workspace, q.device, who)
+    _check(lib().pserve_prompt_attention(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
+                                         ws, nws, out.data_ptr(), _stream()))
+    return out
+
+
+class KV8:
+    """pserve_kv8: keys and values of `places` tokens in 8 bits, a scale for each token and head."""
+
+    def __init__(self, places: int, kv_heads: int, head_dim: int):
+        self._h = C.c_void_p()
+        _check(lib().pserve_kv8_create(int(places), int(kv_heads), int(head_dim), _stream(), C.byref(self._h)))
+        self.places, self.kv_heads, self.head_dim = int(places), int(kv_heads), int(head_dim)
+
+    def write(self, k, v, places):
+        """k and v [T, kv_heads, D] into places int64 [T] (on the device; negative or out of range: not written; the last row
+        of a place counts)."""
+        import torch
+        who = "KV8.write"
+        _here(who, k, v, places)
+        _need(k.dim() == 3 and tuple(k.shape[1:]) == (self.kv_heads, self.head_dim) and v.shape == k.shape and v.dtype == k.dtype,
+              f"{who}: k and v must be [T, {self.kv_heads}, {self.head_dim}] of one dtype")
+        _need(k.stride(2) == 1 and v.stride(2) == 1, f"{who}: the values of a head must be consecutive")
+        _ints(who, places, torch.int64, (k.shape[0],), "places")
+        ks, vs = (C.c_int64 * 2)(*k.stride()[:2]), (C.c_int64 * 2)(*v.stride()[:2])
+        _check(lib().pserve_kv8_write(self._h, k.data_ptr(), v.data_ptr(), _code(k, who), ks, vs, places.data_ptr(), k.shape[0], _stream()))
+
+    def read(self, places, dtype: int, k=None, v=None):
+        """The values held at places int64 [T], as (k, v) [T, kv_heads, D] of dtype F32 or BF16; zeros where out of range."""
+        import torch
+        who = "KV8.read"
+        _here(who, places, k, v)
+        _need(dtype in (F32, BF16), f"{who}: unknown dtype {dtype}")
+        _need(places.dim() == 1, f"{who}: places must be int64 [T]")
+        _ints(who, places, torch.int64, places.shape, "places")
+        shape = (places.shape[0], self.kv_heads, self.head_dim)
+        k = torch.empty(shape, dtype=_torch_dtype(dtype), device=places.device) if k is None else k
+        v = torch.empty(shape, dtype=_torch_dtype(dtype), device=places.device) if v is None else v
+        for t in (k, v):
+            _need(tuple(t.shape) == shape and t.is_contiguous() and t.dtype == _torch_dtype(dtype), f"{who}: k and v must be contiguous {shape}")
+        _apart(who, k, v)
+        _check(lib().pserve_kv8_read(self._h, places.data_ptr(), places.shape[0], dtype, k.data_ptr(), v.data_ptr(), _stream()))
+        return k, v
+
+    def attention(self, q, cu_q, key_len, table, page: int, causal: bool = True, scale: Optional[float] = None, max_q: int = 0,
+                  max_k: int = 0, out=None, workspace=None):
+        """pserve_kv8_attention: q [Tq, heads, D], cu_q int32 [n + 1], key_len int32 [n], table int32 [n, max_pages]: key j of
+        sequence s lies at place table[s, j // page] * page + j % page.  As prompt_attention otherwise."""
+        import torch
+        who = "KV8.attention"
+        _here(who, q, cu_q, key_len, table, out, workspace)
+        _need(cu_q.dim() == 1 and cu_q.shape[0] >= 2, f"{who}: cu_q must be int32 [n + 1], n > 0")
+        n = cu_q.shape[0] - 1
+        _ints(who, cu_q, torch.int32, cu_q.shape, "cu_q")
+        _ints(who, key_len, torch.int32, (n,), "key_len")
+        _need(table.dim() == 2, f"{who}: table must be int32 [n, max_pages]")
+        _ints(who, table, torch.int32, (n, table.shape[1]), "table")
+        _need(q.dim() == 3 and q.shape[2] == self.head_dim, f"{who}: q must be [Tq, heads, {self.head_dim}]")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            _apart(who, out, q)
+        d = _prompt_desc(who, q, out, n, self.kv_heads, causal, scale, max_q, max_k)
+        need = C.c_size_t()
+        _check(lib().pserve_prompt_attention_workspace(C.byref(d), C.byref(need)))
+        ws, nws, keep = _workspace(need.value, workspace, q.device, who)
+        _check(lib().pserve_kv8_attention(self._h, C.byref(d), q.data_ptr(), cu_q.data_ptr(), key_len.data_ptr(), table.data_ptr(),
+                                          table.shape[1], int(page), ws, nws, out.data_ptr(), _stream()))
+        return out
+
+    def close(self):
+        if self._h:
+            lib().pserve_kv8_free(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Linear8:
+    """pserve_linear8: y = x W + b (+ residual), x and W in 8-bit integers with a scale for each token and output channel.
+    w [K, N], b [N] or None; the weights are quantised here, once."""
+
+    def __init__(self, w, b, dtype: int):
+        who = "Linear8"
+        _here(who, w, b)
+        _need(dtype in (F32, BF16) and w.dim() == 2 and w.is_contiguous() and w.dtype == _torch_dtype(dtype), f"{who}: w must be contiguous [K, N] of the given dtype")
+        _need(b is None or (tuple(b.shape) == (w.shape[1],) and b.is_contiguous() and b.dtype == w.dtype), f"{who}: b must be [N] of the given dtype")
+        self.dtype, self.K, self.N = dtype, int(w.shape[0]), int(w.shape[1])
+        self._h = C.c_void_p()
+        _check(lib().pserve_linear8_create(self.K, self.N, dtype, w.data_ptr(), None if b is None else b.data_ptr(), _stream(), C.byref(self._h)))
+
+    def workspace_bytes(self, rows: int) -> int:
+        n = C.c_size_t()
+        _check(lib().pserve_linear8_workspace(self._h, rows, C.byref(n)))
+        return int(n.value)
+
+    def forward(self, x, res=None, y=None, workspace=None):
+        """x [rows, K] (rows may lie further apart), res [rows, N] or None (it may be y)."""
+        import torch
+        who = "Linear8.forward"
+        _here(who, x, res, y, workspace)
+        _need(x.dim() == 2 and x.shape[1] == self.K and x.dtype == _torch_dtype(self.dtype), f"{who}: x must be [rows, {self.K}] of the layer's dtype")
+        rows = x.shape[0]
+        _need(self.K == 1 or x.stride(1) == 1, f"{who}: the values of a row must be consecutive")
+        ldx = x.stride(0) if rows > 1 else self.K
+        _need(ldx >= self.K, f"{who}: rows of x overlap")
+        if y is None:
+            y = torch.empty((rows, self.N), dtype=x.dtype, device=x.device)
+        else:
+            _apart(who, y, x)
+        for t in (y, res):
+            _need(t is None or (tuple(t.shape) == (rows, self.N) and t.is_contiguous() and t.dtype == x.dtype),
+                  f"{who}: res and y must be contiguous [rows, {self.N}] of the layer's dtype")
+        if res is not None and res.data_ptr() != y.data_ptr():
+            _apart(who, y, res)
+        ws, nws, keep = _workspace(self.workspace_bytes(rows), workspace, x.device, who)
+        _check(lib().pserve_linear8_forward(self._h, x.data_ptr(), ldx, rows, None if res is None else res.data_ptr(), ws, nws, y.data_ptr(), _stream()))
+        return y
+
+    def close(self):
+        if self._h:
+            lib().pserve_linear8_free(self._h)
             self._h = C.c_void_p()
 
     def __del__(self):

@@ -1,0 +1,124 @@
+// Entry points of the prompt attention: argument checks and the choice of kernel.
+#include "prompt.h"
+#include <cmath>
+
+using namespace pserve;
+
+static int current_device(int* dev) {
+    PS_CHECK_HIP(hipGetDevice(dev));
+    return PSERVE_OK;
+}
+
+static int check_desc(const pserve_prompt_desc* d, const char* who) {
+    PS_REQUIRE(d, "%s: desc is NULL", who);
+    PS_REQUIRE(d->n > 0, "%s: need n > 0 sequences", who);
+    PS_REQUIRE(d->dtype == PSERVE_F32 || d->dtype == PSERVE_BF16, "%s: unknown dtype %d", who, d->dtype);
+    PS_REQUIRE(d->heads > 0 && d->kv_heads > 0 && d->heads % d->kv_heads == 0, "%s: %d heads over %d key/value heads", who, d->heads, d->kv_heads);
+    PS_REQUIRE(d->heads <= 4096, "%s: more than 4096 heads", who);
+    PS_REQUIRE(d->head_dim > 0 && d->head_dim % 16 == 0 && d->head_dim <= 128, "%s: head_dim %d is not a multiple of 16 up to 128", who, d->head_dim);
+    PS_REQUIRE(std::isfinite(d->scale), "%s: the scale is not finite", who);
+    PS_REQUIRE(d->q_tokens >= 0 && d->q_tokens <= INT32_MAX && d->max_q >= 0 && d->max_k >= 0, "%s: negative or too large sizes", who);
+    return PSERVE_OK;
+}
+
+// strides and pointers of a [tokens][heads][head_dim] tensor: 16-byte rows, and the end within 2^62 bytes
+static int check_tensor(const pserve_prompt_desc* d, const void* p, const int64_t* stride, const char* name, const char* who) {
+    const int64_t vn = 16 / (int64_t)dtype_size(d->dtype);
+    PS_REQUIRE(((uintptr_t)p & 15) == 0, "%s: %s is not 16-byte aligned", who, name);
+    for (int i = 0; i < 2; ++i)
+        PS_REQUIRE(stride[i] >= 0 && stride[i] < ((int64_t)1 << 28) && stride[i] % vn == 0, "%s: stride %lld of %s is not a multiple of 16 bytes", who,
+                   (long long)stride[i], name);
+    return PSERVE_OK;
+}
+
+static PromptArgs prompt_args(const pserve_prompt_desc* d) {
+    PromptArgs a{};
+    a.q_tokens = d->q_tokens;
+    a.q_row = d->q_stride[0]; a.q_head = d->q_stride[1];
+    a.o_row = d->o_stride[0]; a.o_head = d->o_stride[1];
+    a.n = d->n; a.H = d->heads; a.Hk = d->kv_heads; a.G = d->heads / d->kv_heads; a.D = d->head_dim;
+    a.causal = d->causal != 0;
+    a.scale2 = (float)((double)d->scale * 1.4426950408889634);
+    return a;
+}
+
+// Shares of the keys: enough blocks to fill the chip some times over (four blocks a CU), none below 256 keys.
+static int choose_splits(const pserve_prompt_desc* d, const PromptArgs& a) {
+    const int64_t tiles = prompt_slots(a, a.G, 16) * a.Hk, max_k = d->max_k ? d->max_k : 1024;
+    const int64_t s = std::min(cdiv(1024, tiles), max_k / 256);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(s, 128));
+}
+
+static size_t part_bytes(const PromptArgs& a) {
+    const int dp = a.D <= 64 ? 64 : 128;
+    return a.splits == 1 ? 0 : (size_t)prompt_slots(a, a.G, 16) * a.Hk * a.splits * 16 * (dp + 2) * sizeof(float);
+}
+
+static int run(const pserve_prompt_desc* d, PromptArgs& a, int src, void* workspace, size_t bytes, hipStream_t st, const char* who) {
+    if (d->q_tokens == 0) return PSERVE_OK;
+    a.splits = choose_splits(d, a);
+    PS_REQUIRE(prompt_slots(a, a.G, 16) * a.Hk * a.splits <= INT32_MAX, "%s: too many tiles of rows", who);
+    const size_t need = part_bytes(a);
+    PS_REQUIRE(bytes >= need && (need == 0 || (workspace && ((uintptr_t)workspace & 15) == 0)), "%s: workspace of %zu bytes, %zu needed (16-byte aligned)", who,
+               bytes, need);
+    a.part = (float*)workspace;
+    return launch_prompt_few(a, d->dtype, src, st);
+}
+
+extern "C" {
+
+int pserve_prompt_attention_workspace(const pserve_prompt_desc* desc, size_t* bytes) {
+    PS_REQUIRE(bytes, "pserve_prompt_attention_workspace: NULL argument");
+    PS_TRY(check_desc(desc, "pserve_prompt_attention_workspace"));
+    PromptArgs a = prompt_args(desc);
+    a.splits = choose_splits(desc, a);
+    *bytes = part_bytes(a);
+    return PSERVE_OK;
+}
+
+int pserve_prompt_attention(const pserve_prompt_desc* desc, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                            const int32_t* cu_k, void* workspace, size_t workspace_bytes, void* o, void* stream) {
+    static const char who[] = "pserve_prompt_attention";
+    PS_TRY(check_desc(desc, who));
+    PS_REQUIRE(desc->k_tokens >= 0 && desc->k_tokens <= INT32_MAX, "%s: negative or too large sizes", who);
+    if (desc->q_tokens == 0) return PSERVE_OK;
+    PS_REQUIRE(q && o && cu_q && cu_k && ((k && v) || desc->k_tokens == 0), "%s: NULL buffer", who);
+    PS_TRY(check_tensor(desc, q, desc->q_stride, "q", who));
+    PS_TRY(check_tensor(desc, k, desc->k_stride, "k", who));
+    PS_TRY(check_tensor(desc, v, desc->v_stride, "v", who));
+    PS_TRY(check_tensor(desc, o, desc->o_stride, "o", who));
+    PromptArgs a = prompt_args(desc);
+    a.Q = q; a.K = k; a.V = v; a.O = o;
+    a.cu_q = cu_q; a.cu_k = cu_k;
+    a.k_tokens = desc->k_tokens;
+    a.k_row = desc->k_stride[0]; a.k_head = desc->k_stride[1];
+    a.v_row = desc->v_stride[0]; a.v_head = desc->v_stride[1];
+    return run(desc, a, SRC_PACKED, workspace, workspace_bytes, (hipStream_t)stream, who);
+}
+
+int pserve_kv8_attention(const pserve_kv8_t* store, const pserve_prompt_desc* desc, const void* q, const int32_t* cu_q,
+                         const int32_t* key_len, const int32_t* table, int32_t max_pages, int32_t page, void* workspace,
+                         size_t workspace_bytes, void* o, void* stream) {
+    static const char who[] = "pserve_kv8_attention";
+    PS_REQUIRE(store, "%s: store is NULL", who);
+    PS_TRY(check_desc(desc, who));
+    PS_REQUIRE(desc->kv_heads == store->heads && desc->head_dim == store->dim, "%s: the store has %d heads of %d values", who, store->heads, store->dim);
+    PS_REQUIRE(page > 0 && (page & (page - 1)) == 0, "%s: page %d is no power of two", who, page);
+    PS_REQUIRE(max_pages >= 0 && (int64_t)max_pages * page <= INT32_MAX, "%s: %d pages of %d tokens", who, max_pages, page);
+    if (desc->q_tokens == 0) return PSERVE_OK;
+    PS_REQUIRE(q && o && cu_q && key_len && (table || max_pages == 0), "%s: NULL buffer", who);
+    int dev;
+    PS_TRY(current_device(&dev));
+    PS_REQUIRE(dev == store->device, "%s: the store is on device %d, the current one is %d", who, store->device, dev);
+    PS_TRY(check_tensor(desc, q, desc->q_stride, "q", who));
+    PS_TRY(check_tensor(desc, o, desc->o_stride, "o", who));
+    PromptArgs a = prompt_args(desc);
+    a.Q = q; a.O = o; a.cu_q = cu_q;
+    a.k8 = store->k; a.v8 = store->v; a.k_scale = store->k_scale; a.v_scale = store->v_scale;
+    a.key_len = key_len; a.table = table; a.max_pages = max_pages;
+    while ((1 << a.page_shift) < page) ++a.page_shift;
+    a.pages = (int32_t)(store->places >> a.page_shift);
+    return run(desc, a, SRC_STORE, workspace, workspace_bytes, (hipStream_t)stream, who);
+}
+
+}  // extern "C"

@@ -1,0 +1,477 @@
+// Causal attention with grouped heads, gfx950: tiles of 16 rows, keys shared out between wavefronts and blocks.
+//
+// A row is a query token's head; the G heads that share a key/value head are neighbouring rows of that head's tile, so one pass
+// over keys and values serves them all.  One block has one tile of 16 rows and a share of its keys; its four wavefronts take 32 keys
+// (fp32: 16) at a time in turn, each with a softmax of its own (running maximum and sum in fp32), and meet in LDS at the end.
+// Where the call has few tiles the keys are shared out between `splits` blocks, whose results a second kernel joins.
+//
+// Scores are formed transposed, S^T = K Q^T on 16 x 16 matrix instructions, so a lane owns one row and NV consecutive keys; the keys
+// of a step are assigned to the instruction's rows so that the lane's probabilities are the B operand of O^T = V^T P^T as they lie.
+// bf16: V passes LDS row by row and is read back transposed (ds_read_b64_tr); fp32: V comes from memory in the operand's layout.
+// Keys and values in 8 bits are exact as bf16 numbers; the scale of a key multiplies its score, that of a value its probability.
+#include "prompt.h"
+
+namespace pserve {
+
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+typedef __attribute__((address_space(3))) q8_u32x2 lds_u32x2;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+constexpr float NEG_INF = -INFINITY;
+
+// bytes of one wavefront's value tile in LDS: 32 rows
+template <typename T, int DP, int SRC> constexpr int few_v_bytes() { return sizeof(T) == 4 ? 0 : 32 * DP * (SRC == SRC_STORE ? 1 : 2); }
+
+template <typename T, int DP, int SRC>
+__global__ void __launch_bounds__(256, 2)
+prompt_few_kernel(PromptArgs a) {
+    constexpr bool F32 = sizeof(T) == 4, ST = SRC == SRC_STORE;
+    constexpr int KT = F32 ? 16 : 32, NV = KT / 4, DT = DP / 16;
+    constexpr int KS = F32 ? DP / 4 : DP / 32;              // contraction steps of a score
+    constexpr int NQ = F32 ? DP / 4 : DP / 32;
+    constexpr int BUF_ROW = DP + 4;                         // floats of a row in the meeting place (16 bytes of padding: banks)
+    constexpr int VB = few_v_bytes<T, DP, SRC>();
+    constexpr int MEET = 4 * 16 * BUF_ROW * 4, SMEM = MEET > 4 * VB ? MEET : 4 * VB;
+    __shared__ __attribute__((aligned(16))) uint8_t smem[SMEM];
+    __shared__ float s_ml[4][16][2];
+    __shared__ __attribute__((aligned(16))) float s_scale[ST ? 4 : 1][64];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, g4 = lane >> 4;
+    const int per = a.Hk * a.splits;
+    const int64_t slot = blockIdx.x / per;
+    const int rest = blockIdx.x % per, split = rest / a.Hk, hk = rest % a.Hk;
+    int s, tile;
+    if (!prompt_slot(a, a.G, 16, slot, s, tile)) return;
+    const PromptSeq q = prompt_seq<SRC>(a, s);
+    const int64_t rows = (int64_t)q.Lq * a.G, r0 = (int64_t)tile * 16;
+    if (tile < 0 || r0 >= rows) return;
+    const int nrow = (int)min((int64_t)16, rows - r0);
+
+    // the lane's row, and the end of the keys it sees
+    const int64_t row = r0 + min(col, nrow - 1);
+    const int tok = (int)(row / a.G), head = hk * a.G + (int)(row - (int64_t)tok * a.G);
+    const int ahead = q.Lk - q.Lq;                          // queries stand at the end of the keys
+    const int row_end = a.causal ? max(0, min(q.Lk, tok + ahead + 1)) : q.Lk;
+    const int tok_last = (int)((r0 + nrow - 1) / a.G);
+    const int all = a.causal ? max(0, min(q.Lk, tok_last + ahead + 1)) : q.Lk;      // keys of the tile
+    const int share = ((all + a.splits - 1) / a.splits + KT - 1) / KT * KT;
+    const int kbeg = (int)min((int64_t)all, (int64_t)split * share), kend = (int)min((int64_t)all, (int64_t)kbeg + share);
+    const int lim = min(row_end, kend);                     // the row's keys are those below
+
+    // ---- query fragments, in the order of the contraction that the key loads below give
+    bf16x8 qb[F32 ? 1 : NQ];
+    float qf[F32 ? NQ : 1];
+    {
+        const T* qp = (const T*)a.Q + (q.q0 + tok) * a.q_row + (int64_t)head * a.q_head;
+#pragma unroll
+        for (int i = 0; i < (F32 ? NQ / 4 : NQ); ++i) {
+            // first value of the lane's i-th chunk of 8 (fp32: 4) values
+            const int d = F32 ? (ST ? 64 * (i / 4) + 16 * g4 + 4 * (i % 4) : 16 * i + 4 * g4)
+                              : (ST ? 64 * (i / 2) + 16 * g4 + 8 * (i % 2) : 32 * i + 8 * g4);
+            const bool in = d < a.D;                        // D is a multiple of 16: a chunk is inside or outside
+            const u32x4 w = *reinterpret_cast<const u32x4*>(qp + (in ? d : 0));
+            if constexpr (F32) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qf[4 * i + e] = in ? __uint_as_float(w[e]) : 0.f;
+            } else {
+                qb[i] = __builtin_bit_cast(bf16x8, in ? w : u32x4{0, 0, 0, 0});
+            }
+        }
+    }
+
+    // ---- what a wavefront holds of a step: keys in fragment order, values by rows (bf16) or in operand order (fp32)
+    constexpr int NK = F32 ? (ST ? DP / 64 : DP / 16) : 2 * (ST ? DP / 64 : DP / 32);
+    constexpr int NVL = F32 ? 4 * (ST ? 1 : DP / 64) : (ST ? DP / 32 : DP / 16);
+    struct Step {
+        u32x4 k[NK], v[NVL];
+        float scale;
+        uint32_t bad;                                       // keys whose page is no page of the store
+    };
+    const T* kb_ = ST ? nullptr : (const T*)a.K + q.k0 * a.k_row + (int64_t)hk * a.k_head;
+    const T* vb_ = ST ? nullptr : (const T*)a.V + q.k0 * a.v_row + (int64_t)hk * a.v_head;
+    // store: the place of key (kb + lane % KT), -1: none
+    auto place_of = [&](int kb) -> int {
+        const int key = min(kb + (lane & (KT - 1)), kend - 1);
+        const int page = a.table[(int64_t)s * a.max_pages + (key >> a.page_shift)];
+        return (uint32_t)page < (uint32_t)a.pages ? (int)(((uint32_t)page << a.page_shift) | ((uint32_t)key & ((1u << a.page_shift) - 1))) : -1;
+    };
+    auto load = [&](Step& f, int kb, int place) {
+        auto key_at = [&](int j) { return min(kb + j, kend - 1); };
+        const int pl = ST ? max(place, 0) : 0;
+        if constexpr (ST) {
+            f.bad = (uint32_t)__ballot(place < 0) & (KT == 32 ? 0xffffffffu : 0xffffu);
+            const bool vs = F32 ? (lane & 16) != 0 : lane >= 32;
+            f.scale = (vs ? a.v_scale : a.k_scale)[(int64_t)pl * a.Hk + hk];
+        }
+        // keys
+        if constexpr (ST) {
+#pragma unroll
+            for (int t = 0; t < (F32 ? 1 : 2); ++t) {
+                const int j = F32 ? col : 8 * (col >> 2) + 4 * t + (col & 3);
+                const int8_t* p = a.k8 + ((int64_t)__shfl(pl, j) * a.Hk + hk) * a.D;
+#pragma unroll
+                for (int i = 0; i < DP / 64; ++i) {
+                    const int d = 64 * i + 16 * g4;
+                    f.k[t * (DP / 64) + i] = *reinterpret_cast<const u32x4*>(p + (d < a.D ? d : 0));
+                }
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < (F32 ? 1 : 2); ++t) {
+                const int j = F32 ? col : 8 * (col >> 2) + 4 * t + (col & 3);
+                const T* p = kb_ + (int64_t)key_at(j) * a.k_row;
+                constexpr int CH = F32 ? 4 : 8, NC = DP / (4 * CH);
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    const int d = 4 * CH * i + CH * g4;
+                    f.k[t * NC + i] = *reinterpret_cast<const u32x4*>(p + (d < a.D ? d : 0));
+                }
+            }
+        }
+        // values
+        if constexpr (F32 && ST) {
+            // the lane's DP / 16 values of each of its four keys
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = min(col * (DP / 16), a.D - DP / 16);
+                const int8_t* p = a.v8 + ((int64_t)__shfl(pl, 4 * g4 + i) * a.Hk + hk) * a.D + d;
+                if constexpr (DP == 128) {
+                    const q8_u32x2 w = *reinterpret_cast<const q8_u32x2*>(p);
+                    f.v[i][0] = w[0]; f.v[i][1] = w[1];
+                } else {
+                    f.v[i][0] = *reinterpret_cast<const uint32_t*>(p);
+                }
+            }
+        } else if constexpr (F32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const T* p = vb_ + (int64_t)key_at(4 * g4 + i) * a.v_row;
+                const int d = min(col * (DP / 16), a.D - DP / 16);
+#pragma unroll
+                for (int c = 0; c < DP / 64; ++c) f.v[i * (DP / 64) + c] = *reinterpret_cast<const u32x4*>(p + d + 4 * c);
+            }
+        } else {
+            constexpr int CH = ST ? 16 : 8, CP = DP / CH;   // values of a 16-byte chunk, chunks of a row
+#pragma unroll
+            for (int i = 0; i < NVL; ++i) {
+                const int idx = 64 * i + lane, j = idx / CP, c = idx % CP, d = c * CH < a.D ? c * CH : 0;
+                if constexpr (ST) f.v[i] = *reinterpret_cast<const u32x4*>(a.v8 + ((int64_t)__shfl(pl, j) * a.Hk + hk) * a.D + d);
+                else f.v[i] = *reinterpret_cast<const u32x4*>(vb_ + (int64_t)key_at(j) * a.v_row + d);
+            }
+        }
+    };
+
+    f32x4 acc[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = NEG_INF, l = 0.f;
+    uint8_t* sv = smem + wave * VB;
+
+    // row positions of the value tile in LDS: 16-byte chunk c of row j lies at chunk c ^ swz(j), so that the 16 rows that a
+    // transposed read touches at a time lie in different banks
+    auto swz = [](int j) -> int {
+        if constexpr (ST) return DP == 128 ? (j >> 1) & 7 : (j >> 2) & 3;
+        else return DP == 128 ? ((j & 3) << 1) | (((j >> 3) & 1) << 3) : (((j >> 1) & 1) << 1) | (((j >> 3) & 1) << 2);
+    };
+
+    auto step = [&](const Step& f, int kb) {
+        // ---- scores of the lane's row and its NV keys kb + NV g4 ..
+        float x[NV];
+        if constexpr (F32) {
+            f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                float kv;
+                if constexpr (ST) kv = (float)(int8_t)(f.k[i / 16][(i / 4) % 4] >> (8 * (i % 4)));
+                else kv = __uint_as_float(f.k[i / 4][i % 4]);
+                sc = __builtin_amdgcn_mfma_f32_16x16x4f32(kv, qf[i], sc, 0, 0, 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = sc[e];
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    bf16x8 fk;
+                    if constexpr (ST) {
+                        const u32x4 w = f.k[t * (DP / 64) + i / 2];
+                        const uint32_t w0 = w[2 * (i % 2)], w1 = w[2 * (i % 2) + 1];
+                        fk = __builtin_bit_cast(bf16x8, u32x4{bf16_of_i8(w0, 0), bf16_of_i8(w0, 1), bf16_of_i8(w1, 0), bf16_of_i8(w1, 1)});
+                    } else {
+                        fk = __builtin_bit_cast(bf16x8, f.k[t * (DP / 32) + i]);
+                    }
+                    sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fk, qb[i], sc, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[4 * t + e] = sc[e];
+            }
+        }
+        float vs[NV];
+        if constexpr (ST) {
+            s_scale[wave][lane] = f.scale;
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int j = 0; j < NV; j += 4) {
+                const f32x4 ks = *reinterpret_cast<const f32x4*>(&s_scale[wave][NV * g4 + j]);
+                const f32x4 w = *reinterpret_cast<const f32x4*>(&s_scale[wave][KT + NV * g4 + j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { x[j + e] *= ks[e] * a.scale2; vs[j + e] = w[e]; }
+            }
+            __builtin_amdgcn_wave_barrier();
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) x[j] *= a.scale2;
+        }
+        const bool masks = __any(kb + KT > lim) || (ST && f.bad);
+        bool ok[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) ok[j] = true;
+        if (masks) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                ok[j] = kb + NV * g4 + j < lim && !(ST && (f.bad >> (NV * g4 + j) & 1));
+                x[j] = ok[j] ? x[j] : NEG_INF;
+            }
+        }
+        // ---- softmax: reference = running maximum of the row (log2 domain)
+        float mx = x[0];
+#pragma unroll
+        for (int j = 1; j < NV; ++j) mx = fmaxf(mx, x[j]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (__any(mx > m)) {
+            const float m2 = fmaxf(m, mx), f_ = m2 == m ? 1.f : __builtin_amdgcn_exp2f(m - m2);
+            m = m2;
+            l *= f_;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t][e] *= f_;
+        }
+        const float ref = m == NEG_INF ? 0.f : m;
+        float p[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(x[j] - ref);
+            l += p[j];
+            if constexpr (ST) p[j] = masks && !ok[j] ? 0.f : p[j] * vs[j];
+        }
+        // ---- O^T += V^T P^T.  A masked key adds nothing, whatever its value is: 0 times a value that is not finite would be NaN
+        if constexpr (F32) {
+            float vv[4][DT];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    if constexpr (ST) vv[i][t] = (float)(int8_t)(f.v[i][t / 4] >> (8 * (t % 4)));
+                    else vv[i][t] = __uint_as_float(f.v[i * (DP / 64) + t / 4][t % 4]);
+                }
+            if (!ST && masks) {
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) odd |= abs_bits(vv[i][t]) >= 0x7f800000u;
+                if (__any(odd)) {
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        f32x4 hit = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const bool o = abs_bits(vv[i][t]) >= 0x7f800000u;
+                            hit = __builtin_amdgcn_mfma_f32_16x16x4f32(o ? 1.f : 0.f, ok[i] ? 1.f : 0.f, hit, 0, 0, 0);
+                            vv[i][t] = o ? 0.f : vv[i][t];
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[t][e] = hit[e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[t][e];
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(vv[i][t], p[i], acc[t], 0, 0, 0);
+        } else {
+            const bf16x8 fp = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4 % NV], p[5 % NV]),
+                                                               pack_bf16x2(p[6 % NV], p[7 % NV])});
+            constexpr int CP = DP / (ST ? 16 : 8), RB = DP * (ST ? 1 : 2);      // chunks, bytes of a row
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < NVL; ++i) {
+                const int idx = 64 * i + lane, j = idx / CP, c = idx % CP;
+                *reinterpret_cast<u32x4*>(sv + j * RB + ((c ^ swz(j)) << 4)) = f.v[i];
+                if (!ST && masks) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) odd |= (f.v[i][e] & 0x7f80u) == 0x7f80u || (f.v[i][e] & 0x7f800000u) == 0x7f800000u;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            odd = !ST && masks && __any(odd);
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                bf16x8 fv;
+                if constexpr (ST) {
+                    const int j = 8 * g4 + (col >> 1);
+                    const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(lds_u8*)(sv + j * RB + ((t ^ swz(j)) << 4) + 8 * (col & 1)));
+                    const uint32_t w0 = (uint32_t)w[0], w1 = (uint32_t)w[1];
+                    fv = __builtin_bit_cast(bf16x8, u32x4{bf16_of_i8(w0, 0), bf16_of_i8(w0, 1), bf16_of_i8(w1, 0), bf16_of_i8(w1, 1)});
+                } else {
+                    bf16x4 h[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int j = 8 * g4 + 4 * u + (col >> 2), c = 2 * t + ((col & 3) >> 1);
+                        h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(lds_u8*)(sv + j * RB + ((c ^ swz(j)) << 4) + 8 * (col & 1)));
+                    }
+                    fv = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                    if (odd) {
+                        u32x4 w = __builtin_bit_cast(u32x4, fv), bad;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t lo = (w[e] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w[e] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                            bad[e] = 0x3f803f80u & (lo | hi);
+                            w[e] &= ~(lo | hi);
+                        }
+                        u32x4 see;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) see[e] = (ok[(2 * e) % NV] ? 0x3f80u : 0u) | (ok[(2 * e + 1) % NV] ? 0x3f800000u : 0u);
+                        f32x4 hit = {0.f, 0.f, 0.f, 0.f};
+                        hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bad), __builtin_bit_cast(bf16x8, see), hit, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[t][e] = hit[e] > 0.f ? __uint_as_float(0x7fc00000u) : acc[t][e];
+                        fv = __builtin_bit_cast(bf16x8, w);
+                    }
+                }
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv, fp, acc[t], 0, 0, 0);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();                // the next step's rows come after these reads
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+    };
+
+    // ---- the wavefront's steps, one ahead in registers
+    int kb = kbeg + wave * KT;
+    if (kb < kend) {
+        Step cur, nxt;
+        int place = 0;
+        if constexpr (ST) place = place_of(kb);
+        load(cur, kb, place);
+        if constexpr (ST) place = place_of(kb + 4 * KT);
+        for (;; kb += 4 * KT) {
+            const bool more = kb + 4 * KT < kend;
+            if (more) {
+                load(nxt, kb + 4 * KT, place);
+                if constexpr (ST) place = place_of(kb + 8 * KT);
+            }
+            step(cur, kb);
+            if (!more) break;
+            cur = nxt;
+        }
+    }
+
+    // ---- the four wavefronts meet
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    __syncthreads();                                        // value tiles are done with
+    float* buf = reinterpret_cast<float*>(smem);
+    if (g4 == 0) { s_ml[wave][col][0] = m; s_ml[wave][col][1] = l; }
+    {
+        float* b = buf + (wave * 16 + col) * BUF_ROW;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            if constexpr (F32) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b[(4 * g4 + e) * (DP / 16) + t] = acc[t][e];
+            } else {
+                *reinterpret_cast<f32x4*>(b + 16 * t + 4 * g4) = acc[t];
+            }
+        }
+    }
+    __syncthreads();
+    const int r = tid >> 4, d0 = (tid & 15) * (DP / 16);
+    if (r >= nrow) return;
+    float mm = NEG_INF, ll = 0.f, o[DP / 16];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][r][0]);
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float mw = s_ml[w][r][0], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+        ll += s_ml[w][r][1] * f;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) o[i] += buf[(w * 16 + r) * BUF_ROW + d0 + i] * f;
+    }
+    if (a.splits > 1) {
+        float* part = a.part + (int64_t)blockIdx.x * (16 * (DP + 2));
+        if ((tid & 15) == 0) { part[16 * DP + r] = mm; part[16 * DP + 16 + r] = ll; }
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) part[r * DP + d0 + i] = o[i];
+        return;
+    }
+    if (d0 >= a.D) return;
+    const int64_t rr = r0 + r;
+    const int tk = (int)(rr / a.G), hd = hk * a.G + (int)(rr - (int64_t)tk * a.G);
+    T* op = (T*)a.O + (q.q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;           // a row without keys: 0
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) st_f(op + i, o[i] * inv);
+}
+
+// joins the shares of a tile: one block a tile, 16 threads a row
+template <typename T, int DP>
+__global__ void __launch_bounds__(256)
+prompt_join_kernel(PromptArgs a, int src) {
+    const int64_t slot = blockIdx.x / a.Hk;
+    const int hk = blockIdx.x % a.Hk;
+    int s, tile;
+    if (!prompt_slot(a, a.G, 16, slot, s, tile)) return;
+    const int64_t q0 = prompt_start(a.cu_q, s, a.q_tokens), rows = (prompt_start(a.cu_q, s + 1, a.q_tokens) - q0) * a.G, r0 = (int64_t)tile * 16;
+    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (DP / 16);
+    if (tile < 0 || r0 + r >= rows || d0 >= a.D) return;
+    const float* part = a.part + (slot * a.Hk * a.splits + hk) * (16 * (DP + 2));
+    const int64_t next = (int64_t)a.Hk * (16 * (DP + 2));
+    float mm = NEG_INF, ll = 0.f, o[DP / 16];
+    for (int i = 0; i < a.splits; ++i) mm = fmaxf(mm, part[i * next + 16 * DP + r]);
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) o[i] = 0.f;
+    for (int i = 0; i < a.splits; ++i) {
+        const float* p = part + i * next;
+        const float mw = p[16 * DP + r], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+        ll += p[16 * DP + 16 + r] * f;
+#pragma unroll
+        for (int e = 0; e < DP / 16; ++e) o[e] += p[r * DP + d0 + e] * f;
+    }
+    const int64_t rr = r0 + r;
+    const int tk = (int)(rr / a.G), hd = hk * a.G + (int)(rr - (int64_t)tk * a.G);
+    T* op = (T*)a.O + (q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
+    const float inv = ll == 0.f ? 0.f : 1.f / ll;
+#pragma unroll
+    for (int e = 0; e < DP / 16; ++e) st_f(op + e, o[e] * inv);
+}
+
+template <typename T, int DP>
+static int launch_few(const PromptArgs& a, int src, hipStream_t st) {
+    const unsigned tiles = (unsigned)(prompt_slots(a, a.G, 16) * a.Hk);
+    if (src == SRC_STORE) prompt_few_kernel<T, DP, SRC_STORE><<<tiles * a.splits, 256, 0, st>>>(a);
+    else prompt_few_kernel<T, DP, SRC_PACKED><<<tiles * a.splits, 256, 0, st>>>(a);
+    PS_TRY(check_launch("prompt_few_kernel"));
+    if (a.splits > 1) {
+        prompt_join_kernel<T, DP><<<tiles, 256, 0, st>>>(a, src);
+        PS_TRY(check_launch("prompt_join_kernel"));
+    }
+    return PSERVE_OK;
+}
+
+int launch_prompt_few(const PromptArgs& a, int dtype, int src, hipStream_t st) {
+    if (dtype == PSERVE_BF16) return a.D <= 64 ? launch_few<uint16_t, 64>(a, src, st) : launch_few<uint16_t, 128>(a, src, st);
+    return a.D <= 64 ? launch_few<float, 64>(a, src, st) : launch_few<float, 128>(a, src, st);
+}
+
+}  // namespace pserve

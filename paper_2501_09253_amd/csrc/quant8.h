@@ -1,0 +1,82 @@
+// Rounding to 8-bit integers, shared by the key/value store and the 8-bit linear layers.
+//
+// A group of values x_i (a token's head in the store, a token's row or a weight column in a layer) is held as whole numbers
+// q_i = 127 x_i / amax, amax = max |x_i|, and one fp32 scale amax / 127.  q_i is the exact quotient rounded to the nearest
+// number, halves to the even one: the fp32 product below decides it unless it lies next to a border of two numbers, which is
+// then decided in exact arithmetic.  So every implementation of the definition holds the same numbers, whatever it rounds
+// on the way.  A group with an infinity or a NaN gets a NaN scale (it reads back as NaN throughout), a group of zeros scale 0.
+#pragma once
+
+#include "mfma_util.h"
+
+namespace pserve {
+
+typedef __attribute__((ext_vector_type(2))) uint32_t q8_u32x2;
+typedef __attribute__((ext_vector_type(16))) int i32x16;
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+
+struct Quant8 {
+    float mul, amax, inv, scale;                    // x * mul: groups of tiny values are read 2^64 times as large (exact)
+    // amax_bits: the largest |x| as its bit pattern (so infinities and NaN come out on top)
+    __device__ __forceinline__ explicit Quant8(uint32_t amax_bits) {
+        const float a = __uint_as_float(amax_bits);
+        mul = a < 0x1p-60f ? 0x1p64f : 1.f;
+        amax = a * mul;
+        scale = fminf(a / 127.f, 0x1.0204060000000p+121f);         // 127 times the scale of the largest number rounds to infinity, one step below it does not
+        inv = a > 0.f ? 127.f / amax : 0.f;
+        if (amax_bits >= 0x7f800000u) { scale = __uint_as_float(0x7fc00000u); mul = 0.f; inv = 0.f; amax = 1.f; }
+    }
+    __device__ __forceinline__ int operator()(float x) const {
+        const float y = x * mul, t = y * inv;       // |error of t| < 127 * 2^-22.9 < 2^-15
+        float r = rintf(t);
+        if (fabsf(fabsf(t - r) - 0.5f) < 0x1p-14f) {
+            const double k = floorf(fabsf(t)), twice = 254.0 * fabs((double)y), border = (2.0 * k + 1.0) * (double)amax;  // exact: 32 bits each
+            const double up = twice > border ? 1.0 : twice < border ? 0.0 : fmod(k, 2.0);
+            r = copysignf((float)(k + up), t);
+        }
+        return scale == scale ? (int)r : 0;         // (inf * 0 is NaN)
+    }
+};
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// eight consecutive values as fp32
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) {
+    const u32x4 r = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(r[i] << 16); v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+}
+__device__ __forceinline__ float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ __forceinline__ float load1(const float* p) { return *p; }
+__device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+__device__ __forceinline__ void store1(uint16_t* p, float v) { *p = to_bf16(v); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = (uint32_t)to_bf16(v[2 * i]) | ((uint32_t)to_bf16(v[2 * i + 1]) << 16);
+    *reinterpret_cast<u32x4*>(p) = o;
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+// eight whole numbers as bytes
+__device__ __forceinline__ q8_u32x2 pack8(const Quant8& z, const float (&v)[8]) {
+    q8_u32x2 o;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w |= ((uint32_t)z(v[4 * h + i]) & 255u) << (8 * i);
+        o[h] = w;
+    }
+    return o;
+}
+
+}  // namespace pserve
