@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from array import array
+from functools import lru_cache
 from itertools import chain
 from typing import Dict, List, Optional, Sequence
 
@@ -521,22 +522,18 @@ def _need(cond, msg: str):
         raise PserveError(EINVAL, msg)
 
 
-def _code(t, who: str) -> int:
-    import torch
-    _need(t.dtype in (torch.bfloat16, torch.float32), f"{who}: dtype {t.dtype} is neither bfloat16 nor float32")
-    return BF16 if t.dtype == torch.bfloat16 else F32
-
-
 def _here(who: str, *tensors):
     """Tensors (None: absent) on the current device: the library's kernels run there."""
     import torch
     dev = torch.cuda.current_device()
     for t in tensors:
-        _need(t is None or (t.is_cuda and t.device.index == dev), f"{who}: a tensor on {getattr(t, 'device', None)}, the current device is cuda:{dev}")
+        if t is not None and t.get_device() != dev:         # -1: not on a GPU
+            raise PserveError(EINVAL, f"{who}: a tensor on {t.device}, the current device is cuda:{dev}")
 
 
 def _ints(who: str, t, dtype, shape, name: str):
-    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous(), f"{who}: {name} must be contiguous {dtype} {tuple(shape)}")
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise PserveError(EINVAL, f"{who}: {name} must be contiguous {dtype} {tuple(shape)}")
 
 
 def _workspace(need: int, workspace, device, who: str):
@@ -546,6 +543,7 @@ def _workspace(need: int, workspace, device, who: str):
         if need == 0:
             return None, 0, None
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace.data_ptr(), need, workspace
     _need(workspace.is_contiguous(), f"{who}: the workspace must be contiguous")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
@@ -564,18 +562,35 @@ def _apart(who: str, out, *inputs):
             _need(a1 <= o0 or o1 <= a0, f"{who}: the output overlaps an input")
 
 
-def _prompt_desc(who: str, q, o, n: int, kv_heads: int, causal: bool, scale, max_q: int, max_k: int) -> _PromptDesc:
-    _need(q.dim() == 3 and q.shape[1] > 0 and q.shape[2] > 0, f"{who}: q must be [tokens, heads, head_dim]")
-    _need(o.shape == q.shape and o.dtype == q.dtype, f"{who}: out must have q's shape and dtype")
-    _need(q.stride(2) == 1 and o.stride(2) == 1, f"{who}: the values of a head must be consecutive")
-    _need(o.numel() == 0 or (o.stride(0) >= o.shape[2] or o.shape[0] == 1) and (o.stride(1) >= o.shape[2] or o.shape[1] == 1),
-          f"{who}: rows of out overlap")
+@lru_cache(maxsize=1024)
+def _prompt_desc(n: int, heads: int, kv_heads: int, dim: int, dtype: int, causal: bool, scale: Optional[float], max_q: int, max_k: int,
+                 q_tokens: int, k_tokens: int, q_stride, k_stride, v_stride, o_stride):
+    """(pserve_prompt_desc, bytes of workspace) of these sizes: decoding steps ask for the same one again and again (7 us each)."""
     d = _PromptDesc()
-    d.n, d.heads, d.kv_heads, d.head_dim, d.dtype = n, q.shape[1], kv_heads, q.shape[2], _code(q, who)
-    d.causal, d.scale = int(bool(causal)), (q.shape[2] ** -0.5 if scale is None else float(scale))
-    d.max_q, d.max_k, d.q_tokens = int(max_q), int(max_k), q.shape[0]
-    d.q_stride[:], d.o_stride[:] = q.stride()[:2], o.stride()[:2]
-    return d
+    d.n, d.heads, d.kv_heads, d.head_dim, d.dtype = n, heads, kv_heads, dim, dtype
+    d.causal, d.scale = int(causal), (dim ** -0.5 if scale is None else scale)
+    d.max_q, d.max_k, d.q_tokens, d.k_tokens = max_q, max_k, q_tokens, k_tokens
+    d.q_stride[:], d.k_stride[:], d.v_stride[:], d.o_stride[:] = q_stride[:2], k_stride[:2], v_stride[:2], o_stride[:2]
+    need = C.c_size_t()
+    _check(lib().pserve_prompt_attention_workspace(C.byref(d), C.byref(need)))
+    return C.byref(d), need.value
+
+
+def _prompt_out(who: str, q, out, *inputs):
+    """The output tensor: the caller's, checked, or a new one."""
+    import torch
+    if q.dtype != torch.bfloat16 and q.dtype != torch.float32:
+        raise PserveError(EINVAL, f"{who}: dtype {q.dtype} is neither bfloat16 nor float32")
+    if q.stride(2) != 1:
+        raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
+    if out is None:
+        return torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape and out.dtype == q.dtype, f"{who}: out must have q's shape and dtype")
+    _need(out.stride(2) == 1, f"{who}: the values of a head must be consecutive")
+    _need(out.numel() == 0 or (out.stride(0) >= out.shape[2] or out.shape[0] == 1) and (out.stride(1) >= out.shape[2] or out.shape[1] == 1),
+          f"{who}: rows of out overlap")
+    _apart(who, out, q, *inputs)
+    return out
 
 
 def prompt_attention(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optional[float] = None, max_q: int = 0, max_k: int = 0,
@@ -591,22 +606,25 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optio
     _need(cu_q.dim() == 1 and cu_q.shape[0] >= 2, f"{who}: cu_q must be int32 [n + 1], n > 0")
     _ints(who, cu_q, torch.int32, cu_q.shape, "cu_q")
     _ints(who, cu_k, torch.int32, cu_q.shape, "cu_k")
-    _need(q.dim() == 3 and k.dim() == 3 and v.shape == k.shape and k.shape[2] == q.shape[2], f"{who}: q [Tq, heads, D], k and v [Tk, kv_heads, D]")
-    _need(k.dtype == q.dtype and v.dtype == q.dtype, f"{who}: q, k and v must have one dtype")
-    _need(k.stride(2) == 1 and v.stride(2) == 1, f"{who}: the values of a head must be consecutive")
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    else:
-        _apart(who, out, q, k, v)
-    d = _prompt_desc(who, q, out, cu_q.shape[0] - 1, k.shape[1], causal, scale, max_q, max_k)
-    d.k_tokens = k.shape[0]
-    d.k_stride[:], d.v_stride[:] = k.stride()[:2], v.stride()[:2]
-    need = C.c_size_t()
-    _check(lib().pserve_prompt_attention_workspace(C.byref(d), C.byref(need)))
-    ws, nws, keep = _workspace(need.value, workspace, q.device, who)
-    _check(lib().pserve_prompt_attention(C.byref(d), q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
+    if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape or k.shape[2] != q.shape[2] or 0 in q.shape[1:] or 0 in k.shape[1:]:
+        raise PserveError(EINVAL, f"{who}: q [Tq, heads, D], k and v [Tk, kv_heads, D]")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise PserveError(EINVAL, f"{who}: q, k and v must have one dtype")
+    sk, sv = k.stride(), v.stride()
+    if sk[2] != 1 or sv[2] != 1:
+        raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
+    out = _prompt_out(who, q, out, k, v)
+    d, need = _prompt_desc(cu_q.shape[0] - 1, q.shape[1], k.shape[1], q.shape[2], BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), scale,
+                           max_q, max_k, q.shape[0], k.shape[0], q.stride(), sk, sv, out.stride())
+    ws, nws, keep = _workspace(need, workspace, q.device, who)
+    _check(lib().pserve_prompt_attention(d, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
                                          ws, nws, out.data_ptr(), _stream()))
     return out
+
+
+@lru_cache(maxsize=1024)
+def _strides(token: int, head: int):
+    return (C.c_int64 * 2)(token, head)
 
 
 class KV8:
@@ -623,12 +641,15 @@ class KV8:
         import torch
         who = "KV8.write"
         _here(who, k, v, places)
-        _need(k.dim() == 3 and tuple(k.shape[1:]) == (self.kv_heads, self.head_dim) and v.shape == k.shape and v.dtype == k.dtype,
-              f"{who}: k and v must be [T, {self.kv_heads}, {self.head_dim}] of one dtype")
-        _need(k.stride(2) == 1 and v.stride(2) == 1, f"{who}: the values of a head must be consecutive")
-        _ints(who, places, torch.int64, (k.shape[0],), "places")
-        ks, vs = (C.c_int64 * 2)(*k.stride()[:2]), (C.c_int64 * 2)(*v.stride()[:2])
-        _check(lib().pserve_kv8_write(self._h, k.data_ptr(), v.data_ptr(), _code(k, who), ks, vs, places.data_ptr(), k.shape[0], _stream()))
+        if k.dim() != 3 or k.shape[1] != self.kv_heads or k.shape[2] != self.head_dim or v.shape != k.shape or v.dtype != k.dtype or \
+                (k.dtype != torch.bfloat16 and k.dtype != torch.float32):
+            raise PserveError(EINVAL, f"{who}: k and v must be [T, {self.kv_heads}, {self.head_dim}], both bfloat16 or both float32")
+        sk, sv = k.stride(), v.stride()
+        if sk[2] != 1 or sv[2] != 1:
+            raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
+        _ints(who, places, torch.int64, k.shape[:1], "places")
+        _check(lib().pserve_kv8_write(self._h, k.data_ptr(), v.data_ptr(), BF16 if k.dtype == torch.bfloat16 else F32, _strides(sk[0], sk[1]),
+                                      _strides(sv[0], sv[1]), places.data_ptr(), k.shape[0], _stream()))
 
     def read(self, places, dtype: int, k=None, v=None):
         """The values held at places int64 [T], as (k, v) [T, kv_heads, D] of dtype F32 or BF16; zeros where out of range."""
@@ -639,11 +660,14 @@ class KV8:
         _need(places.dim() == 1, f"{who}: places must be int64 [T]")
         _ints(who, places, torch.int64, places.shape, "places")
         shape = (places.shape[0], self.kv_heads, self.head_dim)
+        given = [t for t in (k, v) if t is not None]
+        for t in given:
+            _need(t.shape == shape and t.is_contiguous() and t.dtype == _torch_dtype(dtype), f"{who}: k and v must be contiguous {shape} of dtype")
         k = torch.empty(shape, dtype=_torch_dtype(dtype), device=places.device) if k is None else k
         v = torch.empty(shape, dtype=_torch_dtype(dtype), device=places.device) if v is None else v
-        for t in (k, v):
-            _need(tuple(t.shape) == shape and t.is_contiguous() and t.dtype == _torch_dtype(dtype), f"{who}: k and v must be contiguous {shape}")
-        _apart(who, k, v)
+        if given:
+            _apart(who, k, v, places)
+            _apart(who, v, places)
         _check(lib().pserve_kv8_read(self._h, places.data_ptr(), places.shape[0], dtype, k.data_ptr(), v.data_ptr(), _stream()))
         return k, v
 
@@ -660,17 +684,13 @@ class KV8:
         _ints(who, key_len, torch.int32, (n,), "key_len")
         _need(table.dim() == 2, f"{who}: table must be int32 [n, max_pages]")
         _ints(who, table, torch.int32, (n, table.shape[1]), "table")
-        _need(q.dim() == 3 and q.shape[2] == self.head_dim, f"{who}: q must be [Tq, heads, {self.head_dim}]")
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        else:
-            _apart(who, out, q)
-        d = _prompt_desc(who, q, out, n, self.kv_heads, causal, scale, max_q, max_k)
-        need = C.c_size_t()
-        _check(lib().pserve_prompt_attention_workspace(C.byref(d), C.byref(need)))
-        ws, nws, keep = _workspace(need.value, workspace, q.device, who)
-        _check(lib().pserve_kv8_attention(self._h, C.byref(d), q.data_ptr(), cu_q.data_ptr(), key_len.data_ptr(), table.data_ptr(),
-                                          table.shape[1], int(page), ws, nws, out.data_ptr(), _stream()))
+        _need(q.dim() == 3 and q.shape[1] > 0 and q.shape[2] == self.head_dim, f"{who}: q must be [Tq, heads, {self.head_dim}]")
+        out = _prompt_out(who, q, out)
+        d, need = _prompt_desc(n, q.shape[1], self.kv_heads, self.head_dim, BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), scale,
+                               max_q, max_k, q.shape[0], 0, q.stride(), (0, 0), (0, 0), out.stride())
+        ws, nws, keep = _workspace(need, workspace, q.device, who)
+        _check(lib().pserve_kv8_attention(self._h, d, q.data_ptr(), cu_q.data_ptr(), key_len.data_ptr(), table.data_ptr(),
+                                          table.shape[1], page, ws, nws, out.data_ptr(), _stream()))
         return out
 
     def close(self):
@@ -697,6 +717,7 @@ class Linear8:
         self.dtype, self.K, self.N = dtype, int(w.shape[0]), int(w.shape[1])
         self._h = C.c_void_p()
         _check(lib().pserve_linear8_create(self.K, self.N, dtype, w.data_ptr(), None if b is None else b.data_ptr(), _stream(), C.byref(self._h)))
+        self._dtype, self._row_bytes = w.dtype, self.workspace_bytes(1)         # (workspace_bytes is linear in the rows)
 
     def workspace_bytes(self, rows: int) -> int:
         n = C.c_size_t()
@@ -708,21 +729,22 @@ class Linear8:
         import torch
         who = "Linear8.forward"
         _here(who, x, res, y, workspace)
-        _need(x.dim() == 2 and x.shape[1] == self.K and x.dtype == _torch_dtype(self.dtype), f"{who}: x must be [rows, {self.K}] of the layer's dtype")
+        if x.dim() != 2 or x.shape[1] != self.K or x.dtype != self._dtype:
+            raise PserveError(EINVAL, f"{who}: x must be [rows, {self.K}] of the layer's dtype")
         rows = x.shape[0]
-        _need(self.K == 1 or x.stride(1) == 1, f"{who}: the values of a row must be consecutive")
-        ldx = x.stride(0) if rows > 1 else self.K
-        _need(ldx >= self.K, f"{who}: rows of x overlap")
+        ldx, one = x.stride()
+        if rows <= 1:
+            ldx = self.K
+        if (one != 1 and self.K > 1) or ldx < self.K:
+            raise PserveError(EINVAL, f"{who}: the values of a row must be consecutive, rows must not overlap")
+        for t in (y, res):
+            if t is not None and (t.shape != (rows, self.N) or not t.is_contiguous() or t.dtype != x.dtype):
+                raise PserveError(EINVAL, f"{who}: res and y must be contiguous [rows, {self.N}] of the layer's dtype")
         if y is None:
             y = torch.empty((rows, self.N), dtype=x.dtype, device=x.device)
         else:
-            _apart(who, y, x)
-        for t in (y, res):
-            _need(t is None or (tuple(t.shape) == (rows, self.N) and t.is_contiguous() and t.dtype == x.dtype),
-                  f"{who}: res and y must be contiguous [rows, {self.N}] of the layer's dtype")
-        if res is not None and res.data_ptr() != y.data_ptr():
-            _apart(who, y, res)
-        ws, nws, keep = _workspace(self.workspace_bytes(rows), workspace, x.device, who)
+            _apart(who, y, x, *([res] if res is not None and res.data_ptr() != y.data_ptr() else []))
+        ws, nws, keep = _workspace(rows * self._row_bytes, workspace, x.device, who)
         _check(lib().pserve_linear8_forward(self._h, x.data_ptr(), ldx, rows, None if res is None else res.data_ptr(), ws, nws, y.data_ptr(), _stream()))
         return y
 

@@ -16,7 +16,7 @@ struct PromptArgs {
     float* part;                        // partial results of the key shares
     int64_t q_tokens, k_tokens;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;     // strides in elements
-    int32_t n, H, Hk, G, D, causal, splits;
+    int32_t n, H, Hk, G, D, causal, rows, splits;      // rows of a tile, shares of its keys
     int32_t max_pages, page_shift, pages;
     float scale2;                       // scale * log2(e)
 };
@@ -75,6 +75,8 @@ __device__ __forceinline__ uint32_t bf16_of_i8(uint32_t w, int h) {
     return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
 }
 
+int launch_prompt_tile(const PromptArgs& a, int rows, int src, hipStream_t st);
+int launch_prompt_join(const PromptArgs& a, int dtype, hipStream_t st);
 int launch_prompt_few(const PromptArgs& a, int dtype, int src, hipStream_t st);
 
 }  // namespace pserve

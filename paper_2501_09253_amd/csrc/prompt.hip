@@ -21,13 +21,13 @@ static int check_desc(const pserve_prompt_desc* d, const char* who) {
     return PSERVE_OK;
 }
 
-// strides and pointers of a [tokens][heads][head_dim] tensor: 16-byte rows, and the end within 2^62 bytes
+// strides and pointers of a [tokens][heads][head_dim] tensor: 16-byte rows; the rows of a tile are addressed in 32 bits
 static int check_tensor(const pserve_prompt_desc* d, const void* p, const int64_t* stride, const char* name, const char* who) {
     const int64_t vn = 16 / (int64_t)dtype_size(d->dtype);
     PS_REQUIRE(((uintptr_t)p & 15) == 0, "%s: %s is not 16-byte aligned", who, name);
     for (int i = 0; i < 2; ++i)
-        PS_REQUIRE(stride[i] >= 0 && stride[i] < ((int64_t)1 << 28) && stride[i] % vn == 0, "%s: stride %lld of %s is not a multiple of 16 bytes", who,
-                   (long long)stride[i], name);
+        PS_REQUIRE(stride[i] >= 0 && stride[i] < (int64_t)1 << (i ? 40 : 24) && stride[i] % vn == 0,
+                   "%s: stride %lld of %s is not a multiple of 16 bytes or too large", who, (long long)stride[i], name);
     return PSERVE_OK;
 }
 
@@ -42,27 +42,35 @@ static PromptArgs prompt_args(const pserve_prompt_desc* d) {
     return a;
 }
 
-// Shares of the keys: enough blocks to fill the chip some times over (four blocks a CU), none below 256 keys.
-static int choose_splits(const pserve_prompt_desc* d, const PromptArgs& a) {
-    const int64_t tiles = prompt_slots(a, a.G, 16) * a.Hk, max_k = d->max_k ? d->max_k : 1024;
-    const int64_t s = std::min(cdiv(1024, tiles), max_k / 256);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(s, 128));
+// Rows of a tile and shares of its keys.
+static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
+    const int64_t max_q = d->max_q ? d->max_q : cdiv(d->q_tokens, d->n), 
+                  keys = d->max_k ? d->max_k : src == SRC_PACKED ? cdiv(std::max<int64_t>(d->k_tokens, 0), d->n) : 1024;
+    if (d->dtype == PSERVE_BF16 && max_q * a.G > 16) {
+        a.rows = src == SRC_PACKED && prompt_slots(a, a.G, 256) * a.Hk >= 512 ? 256 : 128;
+        a.splits = (int)std::max<int64_t>(1, std::min(512 / (prompt_slots(a, a.G, a.rows) * a.Hk), keys / 512));
+        return;
+    }
+    a.rows = 16;
+    const int64_t tiles = prompt_slots(a, a.G, 16) * a.Hk, s = std::min(cdiv(1024, tiles), keys / 256);
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(s, 128));
 }
 
 static size_t part_bytes(const PromptArgs& a) {
     const int dp = a.D <= 64 ? 64 : 128;
-    return a.splits == 1 ? 0 : (size_t)prompt_slots(a, a.G, 16) * a.Hk * a.splits * 16 * (dp + 2) * sizeof(float);
+    return a.splits == 1 ? 0 : (size_t)prompt_slots(a, a.G, a.rows) * a.Hk * a.splits * a.rows * (dp + 2) * sizeof(float);
 }
 
 static int run(const pserve_prompt_desc* d, PromptArgs& a, int src, void* workspace, size_t bytes, hipStream_t st, const char* who) {
     if (d->q_tokens == 0) return PSERVE_OK;
-    a.splits = choose_splits(d, a);
-    PS_REQUIRE(prompt_slots(a, a.G, 16) * a.Hk * a.splits <= INT32_MAX, "%s: too many tiles of rows", who);
+    choose(d, a, src);
+    // (a launch has at most 2^32 threads)
+    PS_REQUIRE(prompt_slots(a, a.G, a.rows) * a.Hk * std::max(a.splits, a.splits > 1 ? a.rows / 4 : 1) < (1 << 24), "%s: too many tiles of rows", who);
     const size_t need = part_bytes(a);
     PS_REQUIRE(bytes >= need && (need == 0 || (workspace && ((uintptr_t)workspace & 15) == 0)), "%s: workspace of %zu bytes, %zu needed (16-byte aligned)", who,
                bytes, need);
     a.part = (float*)workspace;
-    return launch_prompt_few(a, d->dtype, src, st);
+    return a.rows == 16 ? launch_prompt_few(a, d->dtype, src, st) : launch_prompt_tile(a, a.rows, src, st);
 }
 
 extern "C" {
@@ -71,8 +79,12 @@ int pserve_prompt_attention_workspace(const pserve_prompt_desc* desc, size_t* by
     PS_REQUIRE(bytes, "pserve_prompt_attention_workspace: NULL argument");
     PS_TRY(check_desc(desc, "pserve_prompt_attention_workspace"));
     PromptArgs a = prompt_args(desc);
-    a.splits = choose_splits(desc, a);
-    *bytes = part_bytes(a);
+    size_t need[2];                             // of pserve_prompt_attention and of pserve_kv8_attention
+    for (int src : {SRC_PACKED, SRC_STORE}) {
+        choose(desc, a, src);
+        need[src] = part_bytes(a);
+    }
+    *bytes = std::max(need[0], need[1]);
     return PSERVE_OK;
 }
 

@@ -23,6 +23,21 @@ constexpr float NEG_INF = -INFINITY;
 // bytes of one wavefront's value tile in LDS: 32 rows
 template <typename T, int DP, int SRC> constexpr int few_v_bytes() { return sizeof(T) == 4 ? 0 : 32 * DP * (SRC == SRC_STORE ? 1 : 2); }
 
+// DV consecutive values of a row, times inv
+template <int DV, typename T>
+__device__ __forceinline__ void store_row(T* p, const float (&o)[DV], float inv) {
+    if constexpr (sizeof(T) == 2) {
+        uint32_t w[DV / 2];
+#pragma unroll
+        for (int i = 0; i < DV / 2; ++i) w[i] = pack_bf16x2(o[2 * i] * inv, o[2 * i + 1] * inv);
+        if constexpr (DV == 8) *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+        else *reinterpret_cast<q8_u32x2*>(p) = q8_u32x2{w[0], w[1]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < DV; i += 4) *reinterpret_cast<f32x4*>(p + i) = f32x4{o[i] * inv, o[i + 1] * inv, o[i + 2] * inv, o[i + 3] * inv};
+    }
+}
+
 template <typename T, int DP, int SRC>
 __global__ void __launch_bounds__(256, 2)
 prompt_few_kernel(PromptArgs a) {
@@ -409,7 +424,7 @@ prompt_few_kernel(PromptArgs a) {
         for (int i = 0; i < DP / 16; ++i) o[i] += buf[(w * 16 + r) * BUF_ROW + d0 + i] * f;
     }
     if (a.splits > 1) {
-        float* part = a.part + (int64_t)blockIdx.x * (16 * (DP + 2));
+        float* part = a.part + ((slot * a.splits + split) * a.Hk + hk) * (int64_t)(16 * (DP + 2));
         if ((tid & 15) == 0) { part[16 * DP + r] = mm; part[16 * DP + 16 + r] = ll; }
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) part[r * DP + d0 + i] = o[i];
@@ -420,40 +435,88 @@ prompt_few_kernel(PromptArgs a) {
     const int tk = (int)(rr / a.G), hd = hk * a.G + (int)(rr - (int64_t)tk * a.G);
     T* op = (T*)a.O + (q.q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
     const float inv = ll == 0.f ? 0.f : 1.f / ll;           // a row without keys: 0
-#pragma unroll
-    for (int i = 0; i < DP / 16; ++i) st_f(op + i, o[i] * inv);
+    store_row<DP / 16>(op, o, inv);
 }
 
-// joins the shares of a tile: one block a tile, 16 threads a row
-template <typename T, int DP>
+// Joins the shares of a tile of R rows.  16 threads a row and group of shares: W = 1 takes 16 rows a block and all shares in turn, W = 4
+// four rows, a quarter of the shares each, which meet in LDS: for few rows of many shares (a decoding step).
+template <typename T, int DP, int W>
 __global__ void __launch_bounds__(256)
-prompt_join_kernel(PromptArgs a, int src) {
-    const int64_t slot = blockIdx.x / a.Hk;
-    const int hk = blockIdx.x % a.Hk;
+prompt_join_kernel(PromptArgs a) {
+    constexpr int RB = 16 / W, DV = DP / 16;
+    __shared__ float s_o[W == 1 ? 1 : W][RB][DP], s_ml[W == 1 ? 1 : W][RB][2];
+    const int R = a.rows, sub = blockIdx.x % (R / RB);
+    const int64_t at = blockIdx.x / (R / RB), slot = at / a.Hk;
+    const int hk = (int)(at % a.Hk);
     int s, tile;
-    if (!prompt_slot(a, a.G, 16, slot, s, tile)) return;
-    const int64_t q0 = prompt_start(a.cu_q, s, a.q_tokens), rows = (prompt_start(a.cu_q, s + 1, a.q_tokens) - q0) * a.G, r0 = (int64_t)tile * 16;
-    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (DP / 16);
-    if (tile < 0 || r0 + r >= rows || d0 >= a.D) return;
-    const float* part = a.part + (slot * a.Hk * a.splits + hk) * (16 * (DP + 2));
-    const int64_t next = (int64_t)a.Hk * (16 * (DP + 2));
-    float mm = NEG_INF, ll = 0.f, o[DP / 16];
-    for (int i = 0; i < a.splits; ++i) mm = fmaxf(mm, part[i * next + 16 * DP + r]);
+    if (!prompt_slot(a, a.G, R, slot, s, tile)) return;
+    const int64_t q0 = prompt_start(a.cu_q, s, a.q_tokens), rows = (prompt_start(a.cu_q, s + 1, a.q_tokens) - q0) * a.G, r0 = (int64_t)tile * R + RB * sub;
+    if (tile < 0 || r0 >= rows) return;
+    const int group = threadIdx.x / (16 * RB), rr = (threadIdx.x >> 4) % RB, d0 = (threadIdx.x & 15) * DV, r = RB * sub + rr;
+    const bool in = r0 + rr < rows;
+    const float* part = a.part + (slot * a.splits * a.Hk + hk) * (int64_t)(R * (DP + 2));
+    const int64_t next = (int64_t)a.Hk * (R * (DP + 2));
+    float mm = NEG_INF, ll = 0.f, o[DV];
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i) o[i] = 0.f;
-    for (int i = 0; i < a.splits; ++i) {
-        const float* p = part + i * next;
-        const float mw = p[16 * DP + r], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
-        ll += p[16 * DP + 16 + r] * f;
+    for (int e = 0; e < DV; ++e) o[e] = 0.f;
+    if (in) {
+#pragma unroll 4
+        for (int i = group; i < a.splits; i += W) mm = fmaxf(mm, part[i * next + R * DP + r]);
+#pragma unroll 4
+        for (int i = group; i < a.splits; i += W) {
+            const float* p = part + i * next;
+            const float mw = p[R * DP + r], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+            ll += p[R * DP + R + r] * f;
 #pragma unroll
-        for (int e = 0; e < DP / 16; ++e) o[e] += p[r * DP + d0 + e] * f;
+            for (int e = 0; e < DV; e += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(p + (int64_t)r * DP + d0 + e);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[e + x] += v[x] * f;
+            }
+        }
     }
-    const int64_t rr = r0 + r;
-    const int tk = (int)(rr / a.G), hd = hk * a.G + (int)(rr - (int64_t)tk * a.G);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 15) == 0) { s_ml[group][rr][0] = mm; s_ml[group][rr][1] = ll; }
+#pragma unroll
+        for (int e = 0; e < DV; ++e) s_o[group][rr][d0 + e] = o[e];
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int i = 1; i < W; ++i) mm = fmaxf(mm, s_ml[i][rr][0]);
+        ll = 0.f;
+#pragma unroll
+        for (int e = 0; e < DV; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float mw = s_ml[i][rr][0], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+            ll += s_ml[i][rr][1] * f;
+#pragma unroll
+            for (int e = 0; e < DV; ++e) o[e] += s_o[i][rr][d0 + e] * f;
+        }
+    }
+    if (!in || d0 >= a.D) return;
+    const int64_t row = r0 + rr;
+    const int tk = (int)(row / a.G), hd = hk * a.G + (int)(row - (int64_t)tk * a.G);
     T* op = (T*)a.O + (q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
     const float inv = ll == 0.f ? 0.f : 1.f / ll;
-#pragma unroll
-    for (int e = 0; e < DP / 16; ++e) st_f(op + e, o[e] * inv);
+    store_row<DV>(op, o, inv);
+}
+
+int launch_prompt_join(const PromptArgs& a, int dtype, hipStream_t st) {
+    const bool wide = a.splits > 8;
+    const unsigned grid = (unsigned)(prompt_slots(a, a.G, a.rows) * a.Hk * (a.rows / (wide ? 4 : 16)));
+#define PS_JOIN(T_, DP_)                                                        \
+    if (wide) prompt_join_kernel<T_, DP_, 4><<<grid, 256, 0, st>>>(a);          \
+    else prompt_join_kernel<T_, DP_, 1><<<grid, 256, 0, st>>>(a)
+    if (dtype == PSERVE_BF16) {
+        if (a.D <= 64) { PS_JOIN(uint16_t, 64); }
+        else { PS_JOIN(uint16_t, 128); }
+    } else {
+        if (a.D <= 64) { PS_JOIN(float, 64); }
+        else { PS_JOIN(float, 128); }
+    }
+#undef PS_JOIN
+    return check_launch("prompt_join_kernel");
 }
 
 template <typename T, int DP>
@@ -462,11 +525,7 @@ static int launch_few(const PromptArgs& a, int src, hipStream_t st) {
     if (src == SRC_STORE) prompt_few_kernel<T, DP, SRC_STORE><<<tiles * a.splits, 256, 0, st>>>(a);
     else prompt_few_kernel<T, DP, SRC_PACKED><<<tiles * a.splits, 256, 0, st>>>(a);
     PS_TRY(check_launch("prompt_few_kernel"));
-    if (a.splits > 1) {
-        prompt_join_kernel<T, DP><<<tiles, 256, 0, st>>>(a, src);
-        PS_TRY(check_launch("prompt_join_kernel"));
-    }
-    return PSERVE_OK;
+    return a.splits > 1 ? launch_prompt_join(a, sizeof(T) == 2 ? PSERVE_BF16 : PSERVE_F32, st) : PSERVE_OK;
 }
 
 int launch_prompt_few(const PromptArgs& a, int dtype, int src, hipStream_t st) {

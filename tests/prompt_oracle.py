@@ -50,3 +50,22 @@ def attention_tolerance(out, bound, size, dtype, D, Lk):
     if dtype == torch.bfloat16:
         share = share + HALF[dtype]
     return share * bound + HALF[dtype] * out.abs() + 1e-30
+
+
+def attention_by_heads(q, k, v, scale, causal=True):
+    """`attention` a head at a time, on the tensors' device: for longer sequences."""
+    q, k, v = q.double(), k.double(), v.double()
+    (Lq, H, D), Lk, G = q.shape, k.shape[0], q.shape[1] // k.shape[1]
+    out, bound, size = torch.zeros_like(q), torch.zeros_like(q), torch.zeros((Lq, H, 1), dtype=torch.float64, device=q.device)
+    seen = torch.ones((Lq, Lk), dtype=torch.bool, device=q.device)
+    if causal:
+        seen = seen.tril(Lk - Lq)
+    some = seen.any(1, keepdim=True)
+    for h in range(H):
+        kh, vh = k[:, h // G].contiguous(), v[:, h // G].contiguous()
+        s = (q[:, h].contiguous() @ kh.t().contiguous()) * scale
+        p = torch.softmax(s.masked_fill(~seen, float("-inf")), 1)
+        p = torch.where(some, p, torch.zeros_like(p))
+        out[:, h], bound[:, h] = p @ vh, p @ vh.abs()
+        size[:, h] = ((q[:, h].abs().contiguous() @ kh.abs().t().contiguous()) * abs(scale)).masked_fill(~seen, 0.0).amax(1, keepdim=True)
+    return out, bound, size
