@@ -58,7 +58,8 @@ linear8_pack_kernel(const T* w, int32_t K, int32_t N, int32_t Kp, const uint32_t
     *reinterpret_cast<u32x4*>(out + (int64_t)(n0 + j) * Kp + k0 + 16 * q) = u32x4{v[0], v[1], v[2], v[3]};
 }
 
-// ---- rows of x: TPR threads a row, CH chunks of eight values a thread in registers; chunks behind those are read twice
+// ---- rows of x: TPR threads a row, CH chunks of eight values a thread in registers; chunks behind those are read twice.
+// A wavefront a row needs no barrier and, from a few hundred rows on, fills the chip; fewer rows take a block each.
 template <typename T, int TPR, int CH, bool VEC>
 __global__ void __launch_bounds__(256)
 linear8_rows_kernel(Linear8Args a) {
@@ -67,31 +68,43 @@ linear8_rows_kernel(Linear8Args a) {
     const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
     if (TPR < 256 && row >= a.rows) return;
     const T* x = (const T*)a.x + row * a.ldx;
-    auto get = [&](int c, float (&v)[8]) {
+    constexpr int W = 8 * sizeof(T) / 16;                   // 16-byte words of a chunk
+    struct Chunk { u32x4 w[W]; };
+    auto get = [&](int c) -> Chunk {
+        Chunk r;
         if (VEC) {
-            if (8 * c < a.K) { load8(x + 8 * c, v); return; }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 0.f;
+            for (int i = 0; i < W; ++i) r.w[i] = 8 * c < a.K ? *reinterpret_cast<const u32x4*>(x + 8 * c + i * (8 / W)) : u32x4{0, 0, 0, 0};
         } else {
+            T v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = 8 * c + i < a.K ? load1(x + 8 * c + i) : 0.f;
+            for (int i = 0; i < 8; ++i) v[i] = 8 * c + i < a.K ? x[8 * c + i] : T(0);
+            __builtin_memcpy(&r, v, sizeof r);
+        }
+        return r;
+    };
+    auto values = [](const Chunk& r, float (&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? r.w[0][i / 2] & 0xffff0000u : r.w[0][i / 2] << 16);
+            else v[i] = __uint_as_float(r.w[i / 4][i % 4]);
         }
     };
+    auto largest = [&](uint32_t m, const Chunk& r) {
+        float v[8];
+        values(r, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+        return m;
+    };
     const int chunks = a.Kp / 8;
-    float v[CH][8];
+    Chunk held[CH];
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-        get(t + i * TPR, v[i]);
+    for (int i = 0; i < CH; ++i) held[i] = get(t + i * TPR);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, abs_bits(v[i][e]));
-    }
-    for (int c = t + CH * TPR; c < chunks; c += TPR) {
-        float u[8];
-        get(c, u);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, abs_bits(u[e]));
-    }
+    for (int i = 0; i < CH; ++i) m = largest(m, held[i]);
+    for (int c = t + CH * TPR; c < chunks; c += TPR) m = largest(m, get(c));
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
     if (TPR == 256) {
@@ -102,20 +115,23 @@ linear8_rows_kernel(Linear8Args a) {
     const Quant8 z(m);
     if (t == 0) a.x_scale[row] = z.scale;
     int8_t* o = a.x8 + row * a.Kp;
+    auto put = [&](int c, const Chunk& r) {
+        float v[8];
+        values(r, v);
+        *reinterpret_cast<q8_u32x2*>(o + 8 * c) = pack8(z, v);
+    };
 #pragma unroll
     for (int i = 0; i < CH; ++i)
-        if (t + i * TPR < chunks) *reinterpret_cast<q8_u32x2*>(o + 8 * (t + i * TPR)) = pack8(z, v[i]);
-    for (int c = t + CH * TPR; c < chunks; c += TPR) {
-        float u[8];
-        get(c, u);
-        *reinterpret_cast<q8_u32x2*>(o + 8 * c) = pack8(z, u);
-    }
+        if (t + i * TPR < chunks) put(t + i * TPR, held[i]);
+    for (int c = t + CH * TPR; c < chunks; c += TPR) put(c, get(c));
 }
 
 template <typename T, bool VEC>
 static int launch_rows_as(const Linear8Args& a, hipStream_t st) {
-    if (a.Kp <= 1024) linear8_rows_kernel<T, 64, 2, VEC><<<(unsigned)cdiv(a.rows, 4), 256, 0, st>>>(a);
-    else linear8_rows_kernel<T, 256, 4, VEC><<<(unsigned)a.rows, 256, 0, st>>>(a);
+    if (a.rows < 512 && a.Kp > 512) linear8_rows_kernel<T, 256, 4, VEC><<<(unsigned)a.rows, 256, 0, st>>>(a);
+    else if (a.Kp <= 1024) linear8_rows_kernel<T, 64, 2, VEC><<<(unsigned)cdiv(a.rows, 4), 256, 0, st>>>(a);
+    else if (a.Kp <= 2048) linear8_rows_kernel<T, 64, 4, VEC><<<(unsigned)cdiv(a.rows, 4), 256, 0, st>>>(a);
+    else linear8_rows_kernel<T, 64, 8, VEC><<<(unsigned)cdiv(a.rows, 4), 256, 0, st>>>(a);
     return check_launch("linear8_rows_kernel");
 }
 template <typename T>
@@ -124,103 +140,273 @@ static int launch_rows(const Linear8Args& a, hipStream_t st) {
     return vec ? launch_rows_as<T, true>(a, st) : launch_rows_as<T, false>(a, st);
 }
 
-// ---- the product: tiles of 128 rows x 128 channels, four wavefronts of 64 x 64, two stages of 128 values of K
+// ---- the product: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, two stages of 128 values of K
 __device__ __forceinline__ int l8_kperm(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }   // as in the bf16 layers
 
-template <typename T>
-__device__ __forceinline__ void l8_store(const Linear8Args& a, int64_t row, int n, const float (&v)[8], bool vec) {
-    T* y = (T*)a.y + row * a.N + n;
-    if (vec && n + 8 <= a.N) { store8(y, v); return; }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (n + i < a.N) store1(y + i, v[i]);
-}
+template <int WGM, int WGN, int TM, int TN>
+struct L8Cfg {
+    static constexpr int NW = WGM * WGN, WM = 32 * TM, WN = 32 * TN, BM = WGM * WM, BN = WGN * WN;
+    static constexpr int STAGE = (BM + BN) * 128;           // bytes
+    static constexpr int LDS = 2 * STAGE + 2 * 2 * BN * 4;  // ring; scales and biases of a tile's channels, of this tile and the next
+    static_assert(STAGE >= NW * 4096, "the output staging (4 KB a wavefront) reuses a stage");
+};
 
-template <typename T>
-__global__ void __launch_bounds__(256, 2)
-linear8_tile_kernel(Linear8Args a, int m_tiles) {
-    constexpr int BM = 128, BN = 128, LD = (BM + BN) / 32, STAGE_V = (BM + BN) * 8;
-    __shared__ __attribute__((aligned(16))) uint8_t smem[2 * STAGE_V * 16];
-    u32x4* ring = reinterpret_cast<u32x4*>(smem);           // [2][rows of x, rows of w][8 chunks], chunk ^ ((row >> 1) & 7)
+// The accumulators of a lane are eight consecutive channels of one row (kperm), so a piece of 32 rows x 128 bytes passes LDS in 16-byte
+// pieces and leaves in stores of whole 128-byte lines.
+// VEC: rows of y and of the residual lie on the 16-byte grid.
+template <typename T, bool RES, bool VEC, int WGM, int WGN, int TM, int TN>
+__global__ void __launch_bounds__(64 * WGM * WGN, 2)
+linear8_tile_kernel(Linear8Args a, int m_tiles, int total) {
+    using Cfg = L8Cfg<WGM, WGN, TM, TN>;
+    constexpr int NW = Cfg::NW, WM = Cfg::WM, WN = Cfg::WN, BM = Cfg::BM, BN = Cfg::BN;
+    constexpr int RP = 8 * NW, A_LD = BM / RP, B_LD = BN / RP, LD = A_LD + B_LD, STAGE_V = Cfg::STAGE / 16;
+    constexpr int GM = 8;                                   // row tiles of a group, see below
+    extern __shared__ __attribute__((aligned(16))) uint8_t l8_smem[];
+    float* s_cols = reinterpret_cast<float*>(l8_smem + 2 * Cfg::STAGE);
+    u32x4* ring = reinterpret_cast<u32x4*>(l8_smem);        // [2][rows of x, rows of w][8 chunks], chunk ^ ((row >> 1) & 7)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave & 1, wn = wave >> 1, fr = lane & 31, fh = lane >> 5;
-    const int64_t m0 = (int64_t)(blockIdx.x % m_tiles) * BM;
-    const int n0 = (int)(blockIdx.x / m_tiles) * BN;
+    const int wm = wave % WGM, wn = wave / WGM, fr = lane & 31, fh = lane >> 5;
+    const int n_tiles = total / m_tiles, KT = a.Kp / 128;
+
+    // Tiles are numbered in groups of GM row tiles, rows fastest; XCD x (block id mod 8) takes the x-th eighth of the numbers, so
+    // the blocks of an XCD run on neighbouring tiles and share the panels in its L2.
+    const int xcd = blockIdx.x & 7, t_end = (int)((int64_t)total * (xcd + 1) / 8), t_step = gridDim.x >> 3;
+    int t = (int)((int64_t)total * xcd / 8) + (blockIdx.x >> 3);
+    if (t >= t_end) return;
+
     const int lc = lane & 7, lr = 8 * wave + (lane >> 3), gc = lc ^ ((lr >> 1) & 7);
-    const int8_t* src[LD];
-#pragma unroll
-    for (int l = 0; l < LD; ++l) {
-        const int r = lr + 32 * l;
-        src[l] = (r < BM ? a.x8 + min(m0 + r, a.rows - 1) * a.Kp : a.w8 + (int64_t)(n0 + r - BM) * a.Kp) + gc * 16;
-    }
-    auto load_stage = [&](int kt, int stage) {
-#pragma unroll
-        for (int l = 0; l < LD; ++l)
-            __builtin_amdgcn_global_load_lds((const void*)(src[l] + (int64_t)kt * 128), (lds_void*)(ring + stage * STAGE_V + (8 * wave + 32 * l) * 8), 16, 0, 0);
+    int a_off[A_LD], b_off[B_LD];                           // byte offsets from the tile's first row
+    const int8_t *a_base, *b_base;
+    int64_t m0 = 0;
+    int n0 = 0;
+    auto decode = [&](int tt) {
+        const int grp = tt / (GM * n_tiles), r = tt - grp * (GM * n_tiles), gm = min(GM, m_tiles - grp * GM), nt = r / gm;
+        m0 = (int64_t)(grp * GM + r - nt * gm) * BM;
+        n0 = nt * BN;
     };
-    i32x16 acc[2][2];
+    int buf = 0;
+    auto setup = [&](int to) {
+        a_base = a.x8 + m0 * a.Kp;
+        b_base = a.w8 + (int64_t)n0 * a.Kp;
+        const int last = (int)min((int64_t)BM, a.rows - m0) - 1;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int l = 0; l < A_LD; ++l) a_off[l] = min(lr + l * RP, last) * a.Kp + gc * 16;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int l = 0; l < B_LD; ++l) b_off[l] = min(lr + l * RP, a.Np - 1 - n0) * a.Kp + gc * 16;
+        for (int c = tid; c < BN; c += 64 * NW) {           // (both are filled up to Np)
+            const int n = min(n0 + c, a.Np - 1);
+            s_cols[to * 2 * BN + c] = a.w_scale[n];
+            s_cols[to * 2 * BN + BN + c] = a.b ? a.b[n] : 0.f;
+        }
+    };
+    auto load_stage = [&](int kt, int stage) {
+        u32x4* dst = ring + stage * STAGE_V + wave * 64;
+        const int8_t *ap = a_base + (int64_t)kt * 128, *bp = b_base + (int64_t)kt * 128;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
-    const int KT = a.Kp / 128;
+        for (int l = 0; l < A_LD; ++l) __builtin_amdgcn_global_load_lds((const void*)(ap + a_off[l]), (lds_void*)(dst + l * (64 * NW)), 16, 0, 0);
+#pragma unroll
+        for (int l = 0; l < B_LD; ++l) __builtin_amdgcn_global_load_lds((const void*)(bp + b_off[l]), (lds_void*)(dst + BM * 8 + l * (64 * NW)), 16, 0, 0);
+    };
+    const int rowA = wm * WM + fr, rowB = wn * WN + l8_kperm(fr);
+    const u32x4 *pA = ring + rowA * 8, *pB = ring + BM * 8 + rowB * 8;
+    const int swA = (rowA >> 1) & 7, swB = (rowB >> 1) & 7;
+
+    // One load instruction a call, so that the refill of a stage is spread over the matrix instructions behind the barrier that frees
+    // it: the wavefronts' loads in one burst queue at the address unit and hold what stands behind them.
+    auto load_one = [&](int kt, int stage, int l) {
+        u32x4* dst = ring + stage * STAGE_V + wave * 64;
+        if (l < A_LD) __builtin_amdgcn_global_load_lds((const void*)(a_base + (int64_t)kt * 128 + a_off[l < A_LD ? l : 0]), (lds_void*)(dst + l * (64 * NW)), 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((const void*)(b_base + (int64_t)kt * 128 + b_off[l >= A_LD ? l - A_LD : 0]),
+                                              (lds_void*)(dst + BM * 8 + (l - A_LD) * (64 * NW)), 16, 0, 0);
+    };
+    constexpr int NM = TM * TN, NR = TM + TN, QB = NM - NR < 2 ? NM - NR : 2;   // MFMAs, fragment reads of a sub-step; MFMAs in front of the barrier
+    constexpr int SP = NM >= 8 ? 2 : 1;                     // MFMAs between two loads
+    static_assert(QB >= 0 && LD * SP <= NM - QB + 3 * NM, "loads of a step");
+    i32x4 fa[2][TM], fb[2][TN];
+    // fragment r of sub-step ks: a row tile first, the channel tiles, the other row tiles
+    auto read = [&](int set, int stage, int ks, int r) {
+        const u32x4 *sA = pA + stage * STAGE_V, *sB = pB + stage * STAGE_V;
+        const int c = 2 * ks + fh;
+        if (r == 0) fa[set][0] = __builtin_bit_cast(i32x4, sA[c ^ swA]);
+        else if (r <= TN) fb[set][r - 1] = __builtin_bit_cast(i32x4, sB[(r - 1) * 256 + (c ^ swB)]);
+        else fa[set][r - TN] = __builtin_bit_cast(i32x4, sA[(r - TN) * 256 + (c ^ swA)]);
+    };
+
+    decode(t);
+    setup(0);
     load_stage(0, 0);
-    for (int kt = 0; kt < KT; ++kt) {
-        if (kt + 1 < KT) {
-            load_stage(kt + 1, (kt + 1) & 1);
-            asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LD) : "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        }
-        const u32x4* st = ring + (kt & 1) * STAGE_V;
+    if (KT > 1) load_stage(1, 1);
+#pragma unroll 1
+    for (;;) {
+        i32x16 acc[TM][TN];
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            i32x4 fx[2], fw[2];
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int rx = 64 * wm + 32 * i + fr, rw = 64 * wn + 32 * i + l8_kperm(fr);
-                fx[i] = __builtin_bit_cast(i32x4, st[rx * 8 + ((2 * ks + fh) ^ ((rx >> 1) & 7))]);
-                fw[i] = __builtin_bit_cast(i32x4, st[(BM + rw) * 8 + ((2 * ks + fh) ^ ((rw >> 1) & 7))]);
-            }
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+        if (KT > 1) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(LD) : "memory");    // the first step has landed
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fw[j], fx[i], acc[i][j], 0, 0, 0);
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");     // the stage is free for the next load
-    }
-    // the lane has row 32 i + fr and the channels 32 j + 16 c + 8 fh .. + 7
-    const bool vec = a.N % (16 / sizeof(T)) == 0 && !((uintptr_t)a.y & 15);
+        for (int r = 0; r < NR; ++r) read(0, 0, 0, r);
+#pragma unroll 1
+        for (int kt = 0; kt < KT; ++kt) {
+            const int cur = kt & 1, nxt = cur ^ 1;
+            const bool refill = kt + 2 < KT, late = kt > 0 && kt + 1 < KT;      // loads into `cur` behind the barrier; the rest of the step before's
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t row = m0 + 64 * wm + 32 * i + fr;
-        if (row >= a.rows) continue;
-        const float sx = a.x_scale[row];
+            for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+                for (int q = 0; q < NM; ++q) {
+                    const int i = q / TN, j = q % TN, f = ks & 1;
+                    // every fragment of this step is read (its stage is free) and the next step has landed
+                    if (ks == 3 && q == QB) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[f][j], fa[f][i], acc[i][j], 0, 0, 0);
+                    const int r = ks == 3 ? q - QB : q;
+                    if (r >= 0 && r < NR) {
+                        if (ks < 3) read(f ^ 1, cur, ks + 1, r);
+                        else read(f ^ 1, nxt, 0, r);
+                    }
+                    const int sl = ks == 3 ? q - QB : NM - QB + ks * NM + q;    // place behind the barrier
+                    if (ks == 3 && q >= QB && refill) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const int n = n0 + 64 * wn + 32 * j + 16 * c + 8 * fh;
-                if (n >= a.N) continue;
-                float v[8];
+                        for (int l = 0; l < LD; ++l) if (l * SP == sl) load_one(kt + 2, cur, l);
+                    }
+                    if (ks < 3 && late) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    v[e] = (float)acc[i][j][8 * c + e] * (sx * a.w_scale[n + e]);
-                    if (a.b) v[e] += a.b[n + e];
-                    if (a.res && n + e < a.N) v[e] += load1((const T*)a.res + row * a.N + n + e);
+                        for (int l = 0; l < LD; ++l) if (l * SP == sl) load_one(kt + 1, nxt, l);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                l8_store<T>(a, row, n, v, vec);
+        }
+        // ---- output in pieces of 32 rows x 128 bytes, through the second stage
+        const int64_t r0 = m0 + wm * WM;
+        const int c0 = n0 + wn * WN;
+        constexpr int CV = 16 / sizeof(T), PC = 8 * CV;     // values of a 16-byte chunk, columns of a piece
+        constexpr int PJ = PC / 32, NP = TN / PJ;           // accumulator tiles of a piece, pieces of 32 rows
+        const int nt = t + t_step;
+        u32x4 rres[RES ? 2 : 1][4];
+        // the lane's residual of piece p: row fr of the piece, chunks in the accumulators' order
+        auto res_load = [&](int p) {
+            const int64_t row = min(r0 + 32 * (p / NP) + fr, a.rows - 1);
+            const T* rp = (const T*)a.res + row * a.N;
+            const int c = c0 + PC * (p % NP) + 8 * fh;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int at = sizeof(T) == 2 ? c + 16 * q : c + 16 * (q >> 1) + 4 * (q & 1);
+                rres[p & 1][q] = *reinterpret_cast<const u32x4*>(rp + (at < a.N ? at : 0));
             }
+        };
+        if constexpr (RES && VEC) res_load(0);
+        float sx[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sx[i] = a.x_scale[min(r0 + 32 * i + fr, a.rows - 1)];
+        const float* cs = s_cols + buf * 2 * BN + wn * WN + 8 * fh;             // scales of the lane's channels; the biases BN further
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // every wavefront has read its last fragments
+        if (nt < t_end) {                                   // the first step of the next tile comes in beside the end of this one
+            decode(nt);
+            setup(buf ^ 1);
+            load_stage(0, 0);
+        }
+        u32x4* ep = ring + STAGE_V + wave * 256;            // [32 rows][8 chunks], chunk ^ ((row >> 1) & 7)
+        const int er = lane >> 3, ec = lane & 7, sw = (fr >> 1) & 7;
+        // chunk of the lane's 16-byte word q of a piece: words 2 jj + c (bf16), 2 c + h (fp32)
+        auto chunk = [&](int q) { return (sizeof(T) == 2 ? 2 * q + fh : 4 * (q >> 1) + 2 * fh + (q & 1)) ^ sw; };
+        // value `lane % PC` of row r of a piece
+        constexpr int RI = 64 / PC;                         // rows an instruction covers where the rows are off the 16-byte grid
+        auto cell = [&](int r) -> T* { return reinterpret_cast<T*>(ep + r * 8 + (((lane % PC) / CV) ^ ((r >> 1) & 7))) + lane % CV; };
+#pragma unroll
+        for (int p = 0; p < TM * NP; ++p) {
+            const int i = p / NP, jp = p % NP, pcol = c0 + PC * jp;
+            if constexpr (RES && VEC) if (p + 1 < TM * NP) res_load(p + 1);
+            if (pcol >= a.N) continue;
+            const bool in = pcol + lane % PC < a.N;
+            if constexpr (RES && !VEC) {                    // whole rows in, a value a lane
+                T v[32 / RI];
+#pragma unroll
+                for (int r = 0; r < 32 / RI; ++r) {
+                    const int64_t row = r0 + 32 * i + lane / PC + r * RI;
+                    v[r] = in && row < a.rows ? ((const T*)a.res)[row * a.N + pcol + lane % PC] : T(0);
+                }
+#pragma unroll
+                for (int r = 0; r < 32 / RI; ++r) *cell(lane / PC + r * RI) = v[r];
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) rres[p & 1][q] = ep[fr * 8 + chunk(q)];
+                __builtin_amdgcn_wave_barrier();
+            }
+#pragma unroll
+            for (int jj = 0; jj < PJ; ++jj)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float* sp = cs + PC * jp + 32 * jj + 16 * c;
+                    float v[8], w[8], b[8];
+                    load8(sp, w);
+                    load8(sp + BN, b);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = (float)acc[i][jp * PJ + jj][8 * c + e] * (sx[i] * w[e]) + b[e];
+                        if constexpr (RES && sizeof(T) == 2) {
+                            const uint32_t r = rres[p & 1][2 * jj + c][e / 2];
+                            v[e] += e & 1 ? __uint_as_float(r & 0xffff0000u) : __uint_as_float(r << 16);
+                        } else if constexpr (RES) {
+                            v[e] += __uint_as_float(rres[p & 1][2 * c + e / 4][e % 4]);
+                        }
+                    }
+                    if constexpr (sizeof(T) == 2) {
+                        ep[fr * 8 + chunk(2 * jj + c)] = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            ep[fr * 8 + chunk(2 * c + h)] = u32x4{__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
+                    }
+                }
+            __builtin_amdgcn_wave_barrier();
+            if constexpr (VEC) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int rr = 8 * k + er, n = pcol + CV * ec;
+                    const int64_t row = r0 + 32 * i + rr;
+                    const u32x4 o = ep[rr * 8 + (ec ^ ((rr >> 1) & 7))];
+                    // (past the L2, which holds the panels)
+                    if (row < a.rows && n < a.N) __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>((T*)a.y + row * a.N + n));
+                }
+            } else {
+#pragma unroll 8
+                for (int r = lane / PC; r < 32; r += RI) {
+                    const int64_t row = r0 + 32 * i + r;
+                    if (in && row < a.rows) ((T*)a.y)[row * a.N + pcol + lane % PC] = *cell(r);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (nt >= t_end) break;
+        t = nt;
+        buf ^= 1;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the staging is done with
+        if (KT > 1) load_stage(1, 1);
     }
 }
 
+template <typename T, bool RES, bool VEC, int WGM, int WGN, int TM, int TN>
+static int launch_tile_as(const Linear8Args& a, hipStream_t st) {
+    using Cfg = L8Cfg<WGM, WGN, TM, TN>;
+    PS_SET_LDS_ONCE((linear8_tile_kernel<T, RES, VEC, WGM, WGN, TM, TN>), Cfg::LDS);
+    const int64_t mt = cdiv(a.rows, Cfg::BM), total = mt * cdiv(a.N, Cfg::BN);
+    const unsigned grid = (unsigned)(8 * cdiv(std::min<int64_t>(total, Cfg::LDS > 80 * 1024 ? 256 : 512), 8));
+    linear8_tile_kernel<T, RES, VEC, WGM, WGN, TM, TN><<<grid, 64 * Cfg::NW, Cfg::LDS, st>>>(a, (int)mt, (int)total);
+    return check_launch("linear8_tile_kernel");
+}
+
+template <typename T, bool RES, bool VEC>
+static int launch_tile_vec(const Linear8Args& a, hipStream_t st) {
+    if (cdiv(a.rows, 256) * cdiv(a.N, 256) >= 256) return launch_tile_as<T, RES, VEC, 4, 2, 2, 4>(a, st);
+    return launch_tile_as<T, RES, VEC, 2, 2, 2, 2>(a, st);
+}
 template <typename T>
 static int launch_tile(const Linear8Args& a, hipStream_t st) {
-    const int64_t mt = cdiv(a.rows, 128), nt = cdiv(a.N, 128);
-    linear8_tile_kernel<T><<<(unsigned)(mt * nt), 256, 0, st>>>(a, (int)mt);
-    return check_launch("linear8_tile_kernel");
+    const bool vec = a.N % (16 / sizeof(T)) == 0 && !(((uintptr_t)a.y | (uintptr_t)a.res) & 15);
+    if (a.res) return vec ? launch_tile_vec<T, true, true>(a, st) : launch_tile_vec<T, true, false>(a, st);
+    return vec ? launch_tile_vec<T, false, true>(a, st) : launch_tile_vec<T, false, false>(a, st);
 }
 
 }  // namespace pserve
