@@ -135,9 +135,10 @@ static int launch_rows_as(const Linear8Args& a, hipStream_t st) {
     return check_launch("linear8_rows_kernel");
 }
 template <typename T>
+static bool rows_vec(const Linear8Args& a) { return a.K % 8 == 0 && a.ldx % (16 / sizeof(T)) == 0 && !((uintptr_t)a.x & 15); }
+template <typename T>
 static int launch_rows(const Linear8Args& a, hipStream_t st) {
-    const bool vec = a.K % 8 == 0 && a.ldx % (16 / sizeof(T)) == 0 && !((uintptr_t)a.x & 15);
-    return vec ? launch_rows_as<T, true>(a, st) : launch_rows_as<T, false>(a, st);
+    return rows_vec<T>(a) ? launch_rows_as<T, true>(a, st) : launch_rows_as<T, false>(a, st);
 }
 
 // ---- the product: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, two stages of 128 values of K
@@ -397,8 +398,89 @@ static int launch_tile_as(const Linear8Args& a, hipStream_t st) {
     return check_launch("linear8_tile_kernel");
 }
 
+// ---- few rows or few tiles: 16 MT rows x 16 NT channels, eight wavefronts that share K and read their operands from memory in the layout
+// of v_mfma_i32_16x16x64_i8 (16 rows x 64 bytes a load), the next step's in flight; the sums meet in LDS.  Quantising the rows of x in
+// here as well, in one launch, took 21 .. 25 us for 1 .. 12 rows x 4096 x 4096 where the two launches take 9 .. 10: every block of
+// channels does it again.
+template <typename T, int MT, int NT>
+__global__ void __launch_bounds__(512)
+linear8_few_kernel(Linear8Args a, int m_tiles) {
+    constexpr int BM = 16 * MT, BN = 16 * NT, RS = BN + 4, WV = 8;      // RS: ints of a row in LDS
+    __shared__ __attribute__((aligned(16))) int32_t s_sum[WV][BM * RS];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4;
+    const int64_t m0 = (int64_t)(blockIdx.x % m_tiles) * BM;
+    const int n0 = (int)(blockIdx.x / m_tiles) * BN;
+    const int KT = a.Kp / 64;                                           // steps, dealt to the wavefronts in shares
+    const int per = (KT + WV - 1) / WV, k0 = min(KT, wave * per), k1 = min(KT, k0 + per);
+    const int8_t *wp[NT], *xp[MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) wp[j] = a.w8 + (int64_t)min(n0 + 16 * j + col, a.Np - 1) * a.Kp + 16 * g4;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xp[i] = a.x8 + min(m0 + 16 * i + col, a.rows - 1) * a.Kp + 16 * g4;
+    i32x4 acc[MT][NT], w[2][NT], x[2][MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+    auto load = [&](int set, int k) {
+        k = min(k, KT - 1);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) w[set][j] = *reinterpret_cast<const i32x4*>(wp[j] + (int64_t)k * 64);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) x[set][i] = *reinterpret_cast<const i32x4*>(xp[i] + (int64_t)k * 64);
+    };
+    auto mma = [&](int set) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[set][j], x[set][i], acc[i][j], 0, 0, 0);
+    };
+    if (k0 < k1) load(0, k0);
+    for (int k = k0; k < k1; k += 2) {
+        load(1, k + 1);
+        mma(0);
+        if (k + 1 >= k1) break;
+        load(0, k + 2);
+        mma(1);
+    }
+    // ---- the wavefronts' sums meet: the lane has row `col` of a tile and channels 4 g4 .. + 3
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) *reinterpret_cast<i32x4*>(&s_sum[wave][(16 * i + col) * RS + 16 * j + 4 * g4]) = acc[i][j];
+    __syncthreads();
+    for (int idx = tid; idx < BM * BN / 4; idx += 64 * WV) {
+        const int r = idx / (BN / 4), c = idx % (BN / 4) * 4, n = n0 + c;
+        const int64_t row = m0 + r;
+        if (row >= a.rows || n >= a.N) continue;
+        i32x4 s = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < WV; ++i) s += *reinterpret_cast<const i32x4*>(&s_sum[i][r * RS + c]);
+        const float sx = a.x_scale[row];
+        const f32x4 sw = *reinterpret_cast<const f32x4*>(a.w_scale + n);
+        const f32x4 b = a.b ? *reinterpret_cast<const f32x4*>(a.b + n) : f32x4{0.f, 0.f, 0.f, 0.f};
+        T* yp = (T*)a.y + row * a.N + n;
+        const T* rp = (const T*)a.res + row * a.N + n;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (n + e >= a.N) break;
+            float v = (float)s[e] * (sx * sw[e]) + b[e];
+            if (a.res) v += load1(rp + e);
+            store1(yp + e, v);
+        }
+    }
+}
+
+template <typename T, int MT, int NT>
+static int launch_few(const Linear8Args& a, hipStream_t st) {
+    const int64_t mt = cdiv(a.rows, 16 * MT);
+    linear8_few_kernel<T, MT, NT><<<(unsigned)(mt * cdiv(a.N, 16 * NT)), 512, 0, st>>>(a, (int)mt);
+    return check_launch("linear8_few_kernel");
+}
+
 template <typename T, bool RES, bool VEC>
 static int launch_tile_vec(const Linear8Args& a, hipStream_t st) {
+    // (a tile a CU: 12,544 x 1536 x 6144 179 us with 128 x 128 tiles, 156 with these)
     if (cdiv(a.rows, 256) * cdiv(a.N, 256) >= 256) return launch_tile_as<T, RES, VEC, 4, 2, 2, 4>(a, st);
     return launch_tile_as<T, RES, VEC, 2, 2, 2, 2>(a, st);
 }
@@ -407,6 +489,17 @@ static int launch_tile(const Linear8Args& a, hipStream_t st) {
     const bool vec = a.N % (16 / sizeof(T)) == 0 && !(((uintptr_t)a.y | (uintptr_t)a.res) & 15);
     if (a.res) return vec ? launch_tile_vec<T, true, true>(a, st) : launch_tile_vec<T, true, false>(a, st);
     return vec ? launch_tile_vec<T, false, true>(a, st) : launch_tile_vec<T, false, false>(a, st);
+}
+
+template <typename T>
+static int forward(const Linear8Args& a, hipStream_t st) {
+    PS_TRY(launch_rows<T>(a, st));
+    // us of both launches, 16 x 16 / 32 x 32 / 128 x 128 tiles: 12 x 4096 x 4096 10.1 / 12.7 / 24.4, 32 x 4096 x 4096 14.4 / 14.3 / 24.8,
+    // 64 x 4096 x 4096 22.6 / 15.9 / 25.7, 200 x 2048 x 2048 20.5 / 14.9 / 17.6, 500 x 1280 x 1280 (40 tiles) 18.5 / 14.0 / 14.6,
+    // 256 x 1280 x 5120 (80 tiles) 31.4 / 21.0 / 14.5
+    if (a.rows <= 32) return launch_few<T, 1, 1>(a, st);
+    if (cdiv(a.rows, 128) * cdiv(a.N, 128) <= 64) return launch_few<T, 2, 2>(a, st);
+    return launch_tile<T>(a, st);
 }
 
 }  // namespace pserve
@@ -485,12 +578,7 @@ int pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t ld
     a.w8 = op->w; a.w_scale = op->scale; a.b = op->b;
     a.K = op->K; a.N = op->N; a.Kp = op->Kp; a.Np = op->Np;
     hipStream_t st = (hipStream_t)stream;
-    if (op->dtype == PSERVE_BF16) {
-        PS_TRY(launch_rows<uint16_t>(a, st));
-        return launch_tile<uint16_t>(a, st);
-    }
-    PS_TRY(launch_rows<float>(a, st));
-    return launch_tile<float>(a, st);
+    return op->dtype == PSERVE_BF16 ? forward<uint16_t>(a, st) : forward<float>(a, st);
 }
 
 }  // extern "C"

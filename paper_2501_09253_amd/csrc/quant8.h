@@ -66,15 +66,28 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
-// eight whole numbers as bytes
+// Eight whole numbers as bytes.  t + 1.5 * 2^23 is rounded to a whole number, whose low byte is the two's complement form; only where
+// one of the eight is next to a border (or the group is one of tiny values) does the exact form above decide: as a branch for each
+// value it took most of the time (12,544 rows of 1536 bf16 values 19 us against 13).
 __device__ __forceinline__ q8_u32x2 pack8(const Quant8& z, const float (&v)[8]) {
+    constexpr float MAGIC = 12582912.f;
+    uint32_t s[8];
+    float far = 0.f;                                            // largest distance to the whole number
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = v[i] * z.inv, r = t + MAGIC;
+        s[i] = __float_as_uint(r);
+        far = fmaxf(far, fabsf(t - (r - MAGIC)));
+    }
+    if (far > 0.5f - 0x1p-14f || z.mul > 1.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = (uint32_t)z(v[i]);
+    }
     q8_u32x2 o;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w |= ((uint32_t)z(v[4 * h + i]) & 255u) << (8 * i);
-        o[h] = w;
+        const uint32_t lo = __builtin_amdgcn_perm(s[4 * h + 1], s[4 * h], 0x0c0c0400), hi = __builtin_amdgcn_perm(s[4 * h + 3], s[4 * h + 2], 0x04000c0c);
+        o[h] = lo | hi;
     }
     return o;
 }
