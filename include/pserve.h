@@ -331,7 +331,8 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   number of shares of the keys depends on them, never which keys count.
  *   workspace DEVICE, at least pserve_prompt_attention_workspace bytes (0 where none is needed; it holds the partial results
  *   of the shares and may be used for something else after the call in stream order).  o must not overlap an input.
- * Errors: EINVAL (NULL, n <= 0, heads % kv_heads, head_dim not a multiple of 16 or above 128, unknown dtype, negative sizes,
+ * Errors: EINVAL (NULL, n <= 0, heads % kv_heads, head_dim not a multiple of 16 or above 128, unknown dtype, negative sizes, more
+ * than 2^30 keys,
  * pointers or strides that are no multiples of 16 bytes, a scale that is not finite, workspace too small), EHIP.
  *
  * pserve_kv8: keys and values of `places` tokens in 8 bits.  A token's head is a group of head_dim values with one fp32 scale

@@ -16,7 +16,9 @@ struct PromptArgs {
     float* part;                        // partial results of the key shares
     int64_t q_tokens, k_tokens;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;     // strides in elements
-    int32_t n, H, Hk, G, D, causal, rows, splits;      // rows of a tile, shares of its keys
+    int32_t n, H, Hk, G, D, causal;
+    int32_t rows, splits;               // rows of a tile, shares of its keys (wide tiles)
+    int32_t unit, blocks;               // tiles of 16 rows: keys of a unit of work, blocks that share the units
     int32_t max_pages, page_shift, pages;
     float scale2;                       // scale * log2(e)
 };
@@ -66,6 +68,84 @@ __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, i
 }
 inline int64_t prompt_slots(const PromptArgs& a, int G, int R) { return a.q_tokens * G / R + a.n; }
 
+// The work of the 16-row tiles in units of `unit` keys of one tile: sequence s has tiles x Hk x U_s of them, the blocks take equal runs of
+// the numbered units, whatever the sequences' lengths are.  Every wavefront walks the sequences by itself, 64 at a time, one a lane.
+__device__ __forceinline__ int64_t uniform64(int64_t v) {      // the same in all lanes: into scalar registers
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+__device__ __forceinline__ int64_t lane64(int64_t v, int l) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, l));
+}
+template <int SRC>
+struct PromptWalk {
+    const PromptArgs& a;
+    int first = 0;                      // sequence of lane 0
+    int64_t before = 0;                 // units of the sequences in front of it
+    PromptSeq q;                        // the lane's sequence
+    int U = 1;                          // units of one of its tiles
+    int64_t units = 0, upto = 0;        // its units; those from `first` up to its end
+    // of the unit found: sequence and the number of its first unit
+    int s = 0;
+    int64_t base = 0;
+
+    __device__ __forceinline__ explicit PromptWalk(const PromptArgs& a_) : a(a_) { load(); }
+    __device__ __forceinline__ void load() {
+        const int lane = threadIdx.x & 63;
+        units = 0;
+        if (first + lane < a.n) {
+            q = prompt_seq<SRC>(a, first + lane);
+            U = max(1, (int)(((int64_t)q.Lk + a.unit - 1) / a.unit));
+            units = ((int64_t)q.Lq * a.G + 15) / 16 * a.Hk * U;
+        }
+        upto = units;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+    }
+    __device__ __forceinline__ int64_t total() {                // units of all sequences; the walk starts over
+        int64_t sum = lane64(upto, 63);
+        if (a.n > 64) {
+            for (first = 64; first < a.n; first += 64) {
+                load();
+                sum += lane64(upto, 63);
+            }
+            first = 0;
+            load();
+        }
+        return sum;
+    }
+    // the sequence that holds unit w, which lies behind the unit found before; false: none
+    __device__ __forceinline__ bool find(int64_t w) {
+        for (;;) {
+            const uint64_t past = __ballot(before + upto > w);
+            if (past) {
+                const int l = __ffsll((unsigned long long)past) - 1;
+                s = first + l;
+                base = before + lane64(upto, l) - lane64(units, l);
+                return true;
+            }
+            if (first + 64 >= a.n) return false;
+            before += lane64(upto, 63);
+            first += 64;
+            load();
+        }
+    }
+    __device__ __forceinline__ PromptSeq seq() const {
+        const int l = s - first;
+        PromptSeq r;
+        r.q0 = lane64(q.q0, l);
+        r.k0 = lane64(q.k0, l);
+        r.Lq = __builtin_amdgcn_readlane(q.Lq, l);
+        r.Lk = __builtin_amdgcn_readlane(q.Lk, l);
+        return r;
+    }
+    __device__ __forceinline__ int tile_units() const { return __builtin_amdgcn_readlane(U, s - first); }
+};
+// first unit of block b of W units; no more blocks than units have any
+__device__ __forceinline__ int64_t prompt_block_begin(const PromptArgs& a, int64_t W, int64_t b) { return W * b / min((int64_t)a.blocks, W); }
+
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
@@ -76,7 +156,7 @@ __device__ __forceinline__ uint32_t bf16_of_i8(uint32_t w, int h) {
 }
 
 int launch_prompt_tile(const PromptArgs& a, int rows, int src, hipStream_t st);
-int launch_prompt_join(const PromptArgs& a, int dtype, hipStream_t st);
+int launch_prompt_join(const PromptArgs& a, hipStream_t st);
 int launch_prompt_few(const PromptArgs& a, int dtype, int src, hipStream_t st);
 
 }  // namespace pserve

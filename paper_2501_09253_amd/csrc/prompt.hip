@@ -52,20 +52,28 @@ static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
         return;
     }
     a.rows = 16;
-    const int64_t tiles = prompt_slots(a, a.G, 16) * a.Hk, s = std::min(cdiv(1024, tiles), keys / 256);
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>(s, 128));
+    a.splits = 1;
+    const int64_t items = prompt_slots(a, a.G, 16) * a.Hk;
+    if (keys <= 512 || items >= 768) {         // a tile is one unit, nothing to join
+        a.unit = INT32_MAX;
+        a.blocks = (int32_t)std::min<int64_t>(items, 1 << 23);
+    } else {
+        a.unit = 128;
+        a.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512, items * cdiv(keys, 128) / 2));
+    }
 }
 
 static size_t part_bytes(const PromptArgs& a) {
-    const int dp = a.D <= 64 ? 64 : 128;
-    return a.splits == 1 ? 0 : (size_t)prompt_slots(a, a.G, a.rows) * a.Hk * a.splits * a.rows * (dp + 2) * sizeof(float);
+    const size_t tile = (size_t)a.rows * ((a.D <= 64 ? 64 : 128) + 2) * sizeof(float);
+    if (a.rows == 16) return a.unit == INT32_MAX ? 0 : 2 * (size_t)a.blocks * tile;
+    return a.splits == 1 ? 0 : (size_t)prompt_slots(a, a.G, a.rows) * a.Hk * a.splits * tile;
 }
 
 static int run(const pserve_prompt_desc* d, PromptArgs& a, int src, void* workspace, size_t bytes, hipStream_t st, const char* who) {
     if (d->q_tokens == 0) return PSERVE_OK;
     choose(d, a, src);
     // (a launch has at most 2^32 threads)
-    PS_REQUIRE(prompt_slots(a, a.G, a.rows) * a.Hk * std::max(a.splits, a.splits > 1 ? a.rows / 4 : 1) < (1 << 24), "%s: too many tiles of rows", who);
+    PS_REQUIRE(prompt_slots(a, a.G, a.rows) * a.Hk * std::max(a.splits, 16) < (1 << 24), "%s: too many tiles of rows", who);
     const size_t need = part_bytes(a);
     PS_REQUIRE(bytes >= need && (need == 0 || (workspace && ((uintptr_t)workspace & 15) == 0)), "%s: workspace of %zu bytes, %zu needed (16-byte aligned)", who,
                bytes, need);
@@ -92,7 +100,7 @@ int pserve_prompt_attention(const pserve_prompt_desc* desc, const void* q, const
                             const int32_t* cu_k, void* workspace, size_t workspace_bytes, void* o, void* stream) {
     static const char who[] = "pserve_prompt_attention";
     PS_TRY(check_desc(desc, who));
-    PS_REQUIRE(desc->k_tokens >= 0 && desc->k_tokens <= INT32_MAX, "%s: negative or too large sizes", who);
+    PS_REQUIRE(desc->k_tokens >= 0 && desc->k_tokens <= (1 << 30), "%s: negative or too large sizes", who);
     if (desc->q_tokens == 0) return PSERVE_OK;
     PS_REQUIRE(q && o && cu_q && cu_k && ((k && v) || desc->k_tokens == 0), "%s: NULL buffer", who);
     PS_TRY(check_tensor(desc, q, desc->q_stride, "q", who));
@@ -116,7 +124,7 @@ int pserve_kv8_attention(const pserve_kv8_t* store, const pserve_prompt_desc* de
     PS_TRY(check_desc(desc, who));
     PS_REQUIRE(desc->kv_heads == store->heads && desc->head_dim == store->dim, "%s: the store has %d heads of %d values", who, store->heads, store->dim);
     PS_REQUIRE(page > 0 && (page & (page - 1)) == 0, "%s: page %d is no power of two", who, page);
-    PS_REQUIRE(max_pages >= 0 && (int64_t)max_pages * page <= INT32_MAX, "%s: %d pages of %d tokens", who, max_pages, page);
+    PS_REQUIRE(max_pages >= 0 && (int64_t)max_pages * page <= (1 << 30), "%s: %d pages of %d tokens", who, max_pages, page);
     if (desc->q_tokens == 0) return PSERVE_OK;
     PS_REQUIRE(q && o && cu_q && key_len && (table || max_pages == 0), "%s: NULL buffer", who);
     int dev;

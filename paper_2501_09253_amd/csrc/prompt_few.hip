@@ -54,14 +54,24 @@ prompt_few_kernel(PromptArgs a) {
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g4 = lane >> 4;
-    const int per = a.Hk * a.splits;
-    const int64_t slot = blockIdx.x / per;
-    const int rest = blockIdx.x % per, split = rest / a.Hk, hk = rest % a.Hk;
-    int s, tile;
-    if (!prompt_slot(a, a.G, 16, slot, s, tile)) return;
-    const PromptSeq q = prompt_seq<SRC>(a, s);
+    PromptWalk<SRC> walk(a);
+    const int64_t W = walk.total();
+    if ((int64_t)blockIdx.x >= W) return;
+    // where tiles are not cut the last ones come first: under a causal mask they have the most keys
+    const int64_t b = a.unit == INT32_MAX ? min((int64_t)a.blocks, W) - 1 - blockIdx.x : (int64_t)blockIdx.x;
+    int64_t w = prompt_block_begin(a, W, b);
+    const int64_t w_lo = w, w_end = prompt_block_begin(a, W, b + 1);
+    for (bool again = false; w < w_end; again = true) {
+    if (again) __syncthreads();                             // LDS is taken again
+    // ---- the next run of units: a tile's, or what the block has of it
+    if (!walk.find(w)) return;
+    const PromptSeq q = walk.seq();
+    const int s = walk.s, U = walk.tile_units(), off = (int)((w - walk.base) % U);
+    const int item = (int)((w - walk.base) / U), tile = item / a.Hk, hk = item - tile * a.Hk;
+    const int take = (int)min((int64_t)(U - off), w_end - w);
+    const bool first = w == w_lo;
+    w += take;
     const int64_t rows = (int64_t)q.Lq * a.G, r0 = (int64_t)tile * 16;
-    if (tile < 0 || r0 >= rows) return;
     const int nrow = (int)min((int64_t)16, rows - r0);
 
     // the lane's row, and the end of the keys it sees
@@ -71,8 +81,7 @@ prompt_few_kernel(PromptArgs a) {
     const int row_end = a.causal ? max(0, min(q.Lk, tok + ahead + 1)) : q.Lk;
     const int tok_last = (int)((r0 + nrow - 1) / a.G);
     const int all = a.causal ? max(0, min(q.Lk, tok_last + ahead + 1)) : q.Lk;      // keys of the tile
-    const int share = ((all + a.splits - 1) / a.splits + KT - 1) / KT * KT;
-    const int kbeg = (int)min((int64_t)all, (int64_t)split * share), kend = (int)min((int64_t)all, (int64_t)kbeg + share);
+    const int kbeg = (int)min((int64_t)all, (int64_t)off * a.unit), kend = (int)min((int64_t)all, (int64_t)(off + take) * a.unit);
     const int lim = min(row_end, kend);                     // the row's keys are those below
 
     // ---- query fragments, in the order of the contraction that the key loads below give
@@ -192,6 +201,9 @@ prompt_few_kernel(PromptArgs a) {
     };
 
     auto step = [&](const Step& f, int kb) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));                        // LDS addresses are formed here, not ahead of the loop (registers)
+        const int col = ln & 15, g4 = ln >> 4;
         // ---- scores of the lane's row and its NV keys kb + NV g4 ..
         float x[NV];
         if constexpr (F32) {
@@ -227,7 +239,7 @@ prompt_few_kernel(PromptArgs a) {
         }
         float vs[NV];
         if constexpr (ST) {
-            s_scale[wave][lane] = f.scale;
+            s_scale[wave][ln] = f.scale;
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int j = 0; j < NV; j += 4) {
@@ -317,7 +329,7 @@ prompt_few_kernel(PromptArgs a) {
             bool odd = false;
 #pragma unroll
             for (int i = 0; i < NVL; ++i) {
-                const int idx = 64 * i + lane, j = idx / CP, c = idx % CP;
+                const int idx = 64 * i + ln, j = idx / CP, c = idx % CP;
                 *reinterpret_cast<u32x4*>(sv + j * RB + ((c ^ swz(j)) << 4)) = f.v[i];
                 if (!ST && masks) {
 #pragma unroll
@@ -370,22 +382,22 @@ prompt_few_kernel(PromptArgs a) {
         }
     };
 
-    // ---- the wavefront's steps, one ahead in registers
+    // ---- the wavefront's steps, one ahead in registers (behind the last one the last keys again).  Loads come back in order, so the table
+    // entries of the step after the next are asked for in front of the next one's keys and values
     int kb = kbeg + wave * KT;
     if (kb < kend) {
         Step cur, nxt;
         int place = 0;
         if constexpr (ST) place = place_of(kb);
+        int after = 0;
+        if constexpr (ST) after = place_of(kb + 4 * KT);
         load(cur, kb, place);
-        if constexpr (ST) place = place_of(kb + 4 * KT);
-        for (;; kb += 4 * KT) {
-            const bool more = kb + 4 * KT < kend;
-            if (more) {
-                load(nxt, kb + 4 * KT, place);
-                if constexpr (ST) place = place_of(kb + 8 * KT);
-            }
+#pragma unroll 1
+        for (; kb < kend; kb += 4 * KT) {
+            place = after;
+            if constexpr (ST) after = place_of(kb + 8 * KT);
+            load(nxt, kb + 4 * KT, place);
             step(cur, kb);
-            if (!more) break;
             cur = nxt;
         }
     }
@@ -397,135 +409,170 @@ prompt_few_kernel(PromptArgs a) {
     float* buf = reinterpret_cast<float*>(smem);
     if (g4 == 0) { s_ml[wave][col][0] = m; s_ml[wave][col][1] = l; }
     {
-        float* b = buf + (wave * 16 + col) * BUF_ROW;
+        float* to = buf + (wave * 16 + col) * BUF_ROW;
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
             if constexpr (F32) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) b[(4 * g4 + e) * (DP / 16) + t] = acc[t][e];
+                for (int e = 0; e < 4; ++e) to[(4 * g4 + e) * (DP / 16) + t] = acc[t][e];
             } else {
-                *reinterpret_cast<f32x4*>(b + 16 * t + 4 * g4) = acc[t];
+                *reinterpret_cast<f32x4*>(to + 16 * t + 4 * g4) = acc[t];
             }
         }
     }
     __syncthreads();
     const int r = tid >> 4, d0 = (tid & 15) * (DP / 16);
-    if (r >= nrow) return;
+    if (r >= nrow) continue;
     float mm = NEG_INF, ll = 0.f, o[DP / 16];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mm = fmaxf(mm, s_ml[w][r][0]);
+    for (int i = 0; i < 4; ++i) mm = fmaxf(mm, s_ml[i][r][0]);
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) o[i] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float mw = s_ml[w][r][0], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
-        ll += s_ml[w][r][1] * f;
+    for (int i = 0; i < 4; ++i) {
+        const float mw = s_ml[i][r][0], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+        ll += s_ml[i][r][1] * f;
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) o[i] += buf[(w * 16 + r) * BUF_ROW + d0 + i] * f;
+        for (int e = 0; e < DP / 16; ++e) o[e] += buf[(i * 16 + r) * BUF_ROW + d0 + e] * f;
     }
-    if (a.splits > 1) {
-        float* part = a.part + ((slot * a.splits + split) * a.Hk + hk) * (int64_t)(16 * (DP + 2));
+    if (take < U) {
+        float* part = a.part + (2 * b + !first) * (16 * (DP + 2));
         if ((tid & 15) == 0) { part[16 * DP + r] = mm; part[16 * DP + 16 + r] = ll; }
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) part[r * DP + d0 + i] = o[i];
-        return;
+        for (int e = 0; e < DP / 16; e += 4) *reinterpret_cast<f32x4*>(part + r * DP + d0 + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+        continue;
     }
-    if (d0 >= a.D) return;
+    if (d0 >= a.D) continue;
     const int64_t rr = r0 + r;
     const int tk = (int)(rr / a.G), hd = hk * a.G + (int)(rr - (int64_t)tk * a.G);
     T* op = (T*)a.O + (q.q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
-    const float inv = ll == 0.f ? 0.f : 1.f / ll;           // a row without keys: 0
-    store_row<DP / 16>(op, o, inv);
+    store_row<DP / 16>(op, o, ll == 0.f ? 0.f : 1.f / ll);  // a row without keys: 0
+    }
 }
 
-// Joins the shares of a tile of R rows.  16 threads a row and group of shares: W = 1 takes 16 rows a block and all shares in turn, W = 4
-// four rows, a quarter of the shares each, which meet in LDS: for few rows of many shares (a decoding step).
-template <typename T, int DP, int W>
+// Joins the runs of the tiles that more than one block has.  Such a tile holds the first unit of a block: block b takes the tile that
+// holds its own first unit, unless the one before it does already.  16 threads a row; few rows share out the runs between them.
+template <typename T, int DP, int SRC>
 __global__ void __launch_bounds__(256)
-prompt_join_kernel(PromptArgs a) {
-    constexpr int RB = 16 / W, DV = DP / 16;
-    __shared__ float s_o[W == 1 ? 1 : W][RB][DP], s_ml[W == 1 ? 1 : W][RB][2];
-    const int R = a.rows, sub = blockIdx.x % (R / RB);
-    const int64_t at = blockIdx.x / (R / RB), slot = at / a.Hk;
-    const int hk = (int)(at % a.Hk);
-    int s, tile;
-    if (!prompt_slot(a, a.G, R, slot, s, tile)) return;
-    const int64_t q0 = prompt_start(a.cu_q, s, a.q_tokens), rows = (prompt_start(a.cu_q, s + 1, a.q_tokens) - q0) * a.G, r0 = (int64_t)tile * R + RB * sub;
-    if (tile < 0 || r0 >= rows) return;
-    const int group = threadIdx.x / (16 * RB), rr = (threadIdx.x >> 4) % RB, d0 = (threadIdx.x & 15) * DV, r = RB * sub + rr;
-    const bool in = r0 + rr < rows;
-    const float* part = a.part + (slot * a.splits * a.Hk + hk) * (int64_t)(R * (DP + 2));
-    const int64_t next = (int64_t)a.Hk * (R * (DP + 2));
+prompt_meet_kernel(PromptArgs a) {
+    constexpr int DV = DP / 16;
+    __shared__ float s_o[16][DP], s_ml[16][2];
+    PromptWalk<SRC> walk(a);
+    const int64_t W = walk.total(), sharers = min((int64_t)a.blocks, W), b0 = blockIdx.x;       // b0: the first block that has the tile
+    if (b0 + 1 >= sharers) return;
+    const int64_t lo = prompt_block_begin(a, W, b0), w = prompt_block_begin(a, W, b0 + 1);
+    if (!walk.find(w)) return;
+    const int U = walk.tile_units(), off = (int)((w - walk.base) % U);
+    const int64_t w0 = w - off, w1 = w0 + U;
+    if (off == 0 || (b0 > 0 && lo > w0)) return;            // no tile is cut here, or it is cut further in front, too
+    const PromptSeq q = walk.seq();
+    const int item = (int)((w - walk.base) / U), tile = item / a.Hk, hk = item - tile * a.Hk;
+    int64_t b1 = (w1 - 1) * sharers / W;                    // the last block that has it
+    while (prompt_block_begin(a, W, b1 + 1) <= w1 - 1) ++b1;
+    while (prompt_block_begin(a, W, b1) > w1 - 1) --b1;
+    const int runs = (int)(b1 - b0) + 1;
+    const int64_t rows = (int64_t)q.Lq * a.G, r0 = (int64_t)tile * 16;
+    const int nrow = (int)min((int64_t)16, rows - r0), per = nrow <= 2 ? 2 : nrow <= 4 ? 4 : nrow <= 8 ? 8 : 16, groups = 16 / per;
+    const int part_row = threadIdx.x >> 4, r = part_row % per, group = part_row / per, d0 = (threadIdx.x & 15) * DV;
+    // a block's run of this tile is its first one (2 b), but for a first block that begins with another tile
+    const int late = lo < w0 ? 1 : 0;
+    auto part_of = [&](int i) { return a.part + (2 * (b0 + i) + (i == 0 ? late : 0)) * (16 * (DP + 2)); };
     float mm = NEG_INF, ll = 0.f, o[DV];
 #pragma unroll
     for (int e = 0; e < DV; ++e) o[e] = 0.f;
-    if (in) {
-#pragma unroll 4
-        for (int i = group; i < a.splits; i += W) mm = fmaxf(mm, part[i * next + R * DP + r]);
-#pragma unroll 4
-        for (int i = group; i < a.splits; i += W) {
-            const float* p = part + i * next;
-            const float mw = p[R * DP + r], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
-            ll += p[R * DP + R + r] * f;
+    if (r < nrow) {
+#pragma unroll 8
+        for (int i = group; i < runs; i += groups) mm = fmaxf(mm, part_of(i)[16 * DP + r]);
+#pragma unroll 8
+        for (int i = group; i < runs; i += groups) {
+            const float* p = part_of(i);
+            const float mw = p[16 * DP + r], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+            ll += p[16 * DP + 16 + r] * f;
 #pragma unroll
             for (int e = 0; e < DV; e += 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(p + (int64_t)r * DP + d0 + e);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(p + r * DP + d0 + e);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) o[e + x] += v[x] * f;
             }
         }
     }
-    if constexpr (W > 1) {
-        if ((threadIdx.x & 15) == 0) { s_ml[group][rr][0] = mm; s_ml[group][rr][1] = ll; }
+    if ((threadIdx.x & 15) == 0) { s_ml[part_row][0] = mm; s_ml[part_row][1] = ll; }
 #pragma unroll
-        for (int e = 0; e < DV; ++e) s_o[group][rr][d0 + e] = o[e];
-        __syncthreads();
-        if (group) return;
+    for (int e = 0; e < DV; ++e) s_o[part_row][d0 + e] = o[e];
+    __syncthreads();
+    if (group || r >= nrow || d0 >= a.D) return;
+    for (int i = 1; i < groups; ++i) mm = fmaxf(mm, s_ml[i * per + r][0]);
+    ll = 0.f;
 #pragma unroll
-        for (int i = 1; i < W; ++i) mm = fmaxf(mm, s_ml[i][rr][0]);
-        ll = 0.f;
+    for (int e = 0; e < DV; ++e) o[e] = 0.f;
+    for (int i = 0; i < groups; ++i) {
+        const float mw = s_ml[i * per + r][0], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+        ll += s_ml[i * per + r][1] * f;
 #pragma unroll
-        for (int e = 0; e < DV; ++e) o[e] = 0.f;
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float mw = s_ml[i][rr][0], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
-            ll += s_ml[i][rr][1] * f;
-#pragma unroll
-            for (int e = 0; e < DV; ++e) o[e] += s_o[i][rr][d0 + e] * f;
-        }
+        for (int e = 0; e < DV; ++e) o[e] += s_o[i * per + r][d0 + e] * f;
     }
-    if (!in || d0 >= a.D) return;
-    const int64_t row = r0 + rr;
+    const int64_t row = r0 + r;
     const int tk = (int)(row / a.G), hd = hk * a.G + (int)(row - (int64_t)tk * a.G);
-    T* op = (T*)a.O + (q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
-    const float inv = ll == 0.f ? 0.f : 1.f / ll;
-    store_row<DV>(op, o, inv);
+    T* op = (T*)a.O + (q.q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
+    store_row<DV>(op, o, ll == 0.f ? 0.f : 1.f / ll);
 }
 
-int launch_prompt_join(const PromptArgs& a, int dtype, hipStream_t st) {
-    const bool wide = a.splits > 8;
-    const unsigned grid = (unsigned)(prompt_slots(a, a.G, a.rows) * a.Hk * (a.rows / (wide ? 4 : 16)));
-#define PS_JOIN(T_, DP_)                                                        \
-    if (wide) prompt_join_kernel<T_, DP_, 4><<<grid, 256, 0, st>>>(a);          \
-    else prompt_join_kernel<T_, DP_, 1><<<grid, 256, 0, st>>>(a)
-    if (dtype == PSERVE_BF16) {
-        if (a.D <= 64) { PS_JOIN(uint16_t, 64); }
-        else { PS_JOIN(uint16_t, 128); }
-    } else {
-        if (a.D <= 64) { PS_JOIN(float, 64); }
-        else { PS_JOIN(float, 128); }
+// Joins the shares of a wide tile (bf16): 16 rows a block, 16 threads a row.
+template <int DP>
+__global__ void __launch_bounds__(256)
+prompt_join_kernel(PromptArgs a) {
+    constexpr int DV = DP / 16;
+    const int R = a.rows, sub = blockIdx.x % (R / 16);
+    const int64_t at = blockIdx.x / (R / 16), slot = at / a.Hk;
+    const int hk = (int)(at % a.Hk);
+    int s, tile;
+    if (!prompt_slot(a, a.G, R, slot, s, tile)) return;
+    const int64_t q0 = prompt_start(a.cu_q, s, a.q_tokens), rows = (prompt_start(a.cu_q, s + 1, a.q_tokens) - q0) * a.G;
+    const int r = 16 * sub + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * DV;
+    const int64_t row = (int64_t)tile * R + r;
+    if (tile < 0 || row >= rows || d0 >= a.D) return;
+    const float* part = a.part + (slot * a.splits * a.Hk + hk) * (int64_t)(R * (DP + 2));
+    const int64_t next = (int64_t)a.Hk * (R * (DP + 2));
+    float mm = NEG_INF, ll = 0.f, o[DV];
+#pragma unroll
+    for (int e = 0; e < DV; ++e) o[e] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < a.splits; ++i) mm = fmaxf(mm, part[i * next + R * DP + r]);
+#pragma unroll 4
+    for (int i = 0; i < a.splits; ++i) {
+        const float* p = part + i * next;
+        const float mw = p[R * DP + r], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
+        ll += p[R * DP + R + r] * f;
+#pragma unroll
+        for (int e = 0; e < DV; e += 4) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(p + (int64_t)r * DP + d0 + e);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[e + x] += v[x] * f;
+        }
     }
-#undef PS_JOIN
+    const int tk = (int)(row / a.G), hd = hk * a.G + (int)(row - (int64_t)tk * a.G);
+    uint16_t* op = (uint16_t*)a.O + (q0 + tk) * a.o_row + (int64_t)hd * a.o_head + d0;
+    store_row<DV>(op, o, ll == 0.f ? 0.f : 1.f / ll);
+}
+
+int launch_prompt_join(const PromptArgs& a, hipStream_t st) {
+    const unsigned grid = (unsigned)(prompt_slots(a, a.G, a.rows) * a.Hk * (a.rows / 16));
+    if (a.D <= 64) prompt_join_kernel<64><<<grid, 256, 0, st>>>(a);
+    else prompt_join_kernel<128><<<grid, 256, 0, st>>>(a);
     return check_launch("prompt_join_kernel");
 }
 
+template <typename T, int DP, int SRC>
+static int launch_few_as(const PromptArgs& a, hipStream_t st) {
+    prompt_few_kernel<T, DP, SRC><<<(unsigned)a.blocks, 256, 0, st>>>(a);
+    PS_TRY(check_launch("prompt_few_kernel"));
+    if (a.unit == INT32_MAX) return PSERVE_OK;
+    prompt_meet_kernel<T, DP, SRC><<<(unsigned)a.blocks, 256, 0, st>>>(a);
+    return check_launch("prompt_meet_kernel");
+}
 template <typename T, int DP>
 static int launch_few(const PromptArgs& a, int src, hipStream_t st) {
-    const unsigned tiles = (unsigned)(prompt_slots(a, a.G, 16) * a.Hk);
-    if (src == SRC_STORE) prompt_few_kernel<T, DP, SRC_STORE><<<tiles * a.splits, 256, 0, st>>>(a);
-    else prompt_few_kernel<T, DP, SRC_PACKED><<<tiles * a.splits, 256, 0, st>>>(a);
-    PS_TRY(check_launch("prompt_few_kernel"));
-    return a.splits > 1 ? launch_prompt_join(a, sizeof(T) == 2 ? PSERVE_BF16 : PSERVE_F32, st) : PSERVE_OK;
+    return src == SRC_STORE ? launch_few_as<T, DP, SRC_STORE>(a, st) : launch_few_as<T, DP, SRC_PACKED>(a, st);
 }
 
 int launch_prompt_few(const PromptArgs& a, int dtype, int src, hipStream_t st) {

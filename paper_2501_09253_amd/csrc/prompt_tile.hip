@@ -581,7 +581,7 @@ static int launch_tile_as(const PromptArgs& a, hipStream_t st) {
     const int64_t slots = prompt_slots(a, a.G, Cfg::BM);
     prompt_tile_kernel<DP, QT, SRC><<<(unsigned)(slots * a.Hk * a.splits), 256, Cfg::LDS, st>>>(a, slots);
     PS_TRY(check_launch("prompt_tile_kernel"));
-    return a.splits > 1 ? launch_prompt_join(a, PSERVE_BF16, st) : PSERVE_OK;
+    return a.splits > 1 ? launch_prompt_join(a, st) : PSERVE_OK;
 }
 
 int launch_prompt_tile(const PromptArgs& a, int rows, int src, hipStream_t st) {

@@ -67,8 +67,7 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 // Eight whole numbers as bytes.  t + 1.5 * 2^23 is rounded to a whole number, whose low byte is the two's complement form; only where
-// one of the eight is next to a border (or the group is one of tiny values) does the exact form above decide: as a branch for each
-// value it took most of the time (12,544 rows of 1536 bf16 values 19 us against 13).
+// one of the eight is next to a border (or the group is one of tiny values) does the exact form above decide.
 __device__ __forceinline__ q8_u32x2 pack8(const Quant8& z, const float (&v)[8]) {
     constexpr float MAGIC = 12582912.f;
     uint32_t s[8];
