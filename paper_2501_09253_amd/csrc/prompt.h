@@ -18,7 +18,7 @@ struct PromptArgs {
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;     // strides in elements
     int32_t n, H, Hk, G, D, causal;
     int32_t rows, splits;               // rows of a tile, shares of its keys (wide tiles)
-    int32_t unit, blocks;               // tiles of 16 rows: keys of a unit of work, blocks that share the units
+    int32_t unit, lead, blocks;         // tiles of 16 rows: keys of a unit of work, units a tile costs besides, blocks that share the units
     int32_t max_pages, page_shift, pages;
     float scale2;                       // scale * log2(e)
 };
@@ -69,7 +69,8 @@ __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, i
 inline int64_t prompt_slots(const PromptArgs& a, int G, int R) { return a.q_tokens * G / R + a.n; }
 
 // The work of the 16-row tiles in units of `unit` keys of one tile: sequence s has tiles x Hk x U_s of them, the blocks take equal runs of
-// the numbered units, whatever the sequences' lengths are.  Every wavefront walks the sequences by itself, 64 at a time, one a lane.
+// the numbered units, whatever the sequences' lengths are.  The first `lead` units of a tile stand for what it costs besides its keys (its
+// queries, the way to the first keys, the meeting of the wavefronts): without them a block of short sequences is the last to end.  Every wavefront walks the sequences by itself, 64 at a time, one a lane.
 __device__ __forceinline__ int64_t uniform64(int64_t v) {      // the same in all lanes: into scalar registers
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
 }
@@ -94,7 +95,7 @@ struct PromptWalk {
         units = 0;
         if (first + lane < a.n) {
             q = prompt_seq<SRC>(a, first + lane);
-            U = max(1, (int)(((int64_t)q.Lk + a.unit - 1) / a.unit));
+            U = max(1, (int)(((int64_t)q.Lk + a.unit - 1) / a.unit)) + a.lead;
             units = ((int64_t)q.Lq * a.G + 15) / 16 * a.Hk * U;
         }
         upto = units;
@@ -143,8 +144,39 @@ struct PromptWalk {
     }
     __device__ __forceinline__ int tile_units() const { return __builtin_amdgcn_readlane(U, s - first); }
 };
-// first unit of block b of W units; no more blocks than units have any
-__device__ __forceinline__ int64_t prompt_block_begin(const PromptArgs& a, int64_t W, int64_t b) { return W * b / min((int64_t)a.blocks, W); }
+// W units over the blocks: block b has those from floor(W b / B) on.  No more blocks than units have any.  (A 64-bit division takes a
+// hundred instructions: there is one here, and none where every block has one unit.)
+struct PromptShares {
+    int64_t W, B, whole;
+    uint32_t rest;
+    __device__ __forceinline__ PromptShares(const PromptArgs& a, int64_t W_) : W(W_), B(min((int64_t)a.blocks, W_)) {
+        whole = 1;
+        rest = 0;
+        if (W > B) {
+            whole = W / B;
+            rest = (uint32_t)(W - whole * B);
+        }
+    }
+    __device__ __forceinline__ int64_t begin(int64_t b) const {
+        return whole * b + (rest == 0 ? 0 : B <= 65536 ? (int64_t)(rest * (uint32_t)b / (uint32_t)B) : (int64_t)rest * b / B);
+    }
+    __device__ __forceinline__ int64_t block_of(int64_t w) const {
+        int64_t b = (int64_t)((double)w * (double)B / (double)W);
+        while (begin(b + 1) <= w) ++b;
+        while (begin(b) > w) --b;
+        return b;
+    }
+};
+// quotient and rest of a run of units by the units of a tile
+__device__ __forceinline__ int prompt_item(int64_t units, int U, int& off) {
+    if (units >> 32 == 0) {
+        const uint32_t i = (uint32_t)units / (uint32_t)U;
+        off = (int)((uint32_t)units - i * (uint32_t)U);
+        return (int)i;
+    }
+    off = (int)(units % U);
+    return (int)(units / U);
+}
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;

@@ -56,9 +56,11 @@ static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
     const int64_t items = prompt_slots(a, a.G, 16) * a.Hk;
     if (keys <= 512 || items >= 768) {         // a tile is one unit, nothing to join
         a.unit = INT32_MAX;
+        a.lead = 0;
         a.blocks = (int32_t)std::min<int64_t>(items, 1 << 23);
     } else {
         a.unit = 128;
+        a.lead = 1;
         a.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512, items * cdiv(keys, 128) / 2));
     }
 }

@@ -58,16 +58,18 @@ prompt_few_kernel(PromptArgs a) {
     const int64_t W = walk.total();
     if ((int64_t)blockIdx.x >= W) return;
     // where tiles are not cut the last ones come first: under a causal mask they have the most keys
-    const int64_t b = a.unit == INT32_MAX ? min((int64_t)a.blocks, W) - 1 - blockIdx.x : (int64_t)blockIdx.x;
-    int64_t w = prompt_block_begin(a, W, b);
-    const int64_t w_lo = w, w_end = prompt_block_begin(a, W, b + 1);
+    const PromptShares shares(a, W);
+    const int64_t b = a.unit == INT32_MAX ? shares.B - 1 - blockIdx.x : (int64_t)blockIdx.x;
+    int64_t w = shares.begin(b);
+    const int64_t w_lo = w, w_end = shares.begin(b + 1);
     for (bool again = false; w < w_end; again = true) {
     if (again) __syncthreads();                             // LDS is taken again
     // ---- the next run of units: a tile's, or what the block has of it
     if (!walk.find(w)) return;
     const PromptSeq q = walk.seq();
-    const int s = walk.s, U = walk.tile_units(), off = (int)((w - walk.base) % U);
-    const int item = (int)((w - walk.base) / U), tile = item / a.Hk, hk = item - tile * a.Hk;
+    const int s = walk.s, U = walk.tile_units();
+    int off;
+    const int item = prompt_item(w - walk.base, U, off), tile = item / a.Hk, hk = item - tile * a.Hk;
     const int take = (int)min((int64_t)(U - off), w_end - w);
     const bool first = w == w_lo;
     w += take;
@@ -81,7 +83,7 @@ prompt_few_kernel(PromptArgs a) {
     const int row_end = a.causal ? max(0, min(q.Lk, tok + ahead + 1)) : q.Lk;
     const int tok_last = (int)((r0 + nrow - 1) / a.G);
     const int all = a.causal ? max(0, min(q.Lk, tok_last + ahead + 1)) : q.Lk;      // keys of the tile
-    const int kbeg = (int)min((int64_t)all, (int64_t)off * a.unit), kend = (int)min((int64_t)all, (int64_t)(off + take) * a.unit);
+    const int kbeg = (int)min((int64_t)all, (int64_t)max(0, off - a.lead) * a.unit), kend = (int)min((int64_t)all, (int64_t)max(0, off + take - a.lead) * a.unit);
     const int lim = min(row_end, kend);                     // the row's keys are those below
 
     // ---- query fragments, in the order of the contraction that the key loads below give
@@ -382,21 +384,24 @@ prompt_few_kernel(PromptArgs a) {
         }
     };
 
-    // ---- the wavefront's steps, one ahead in registers (behind the last one the last keys again).  Loads come back in order, so the table
-    // entries of the step after the next are asked for in front of the next one's keys and values
+    // ---- the wavefront's steps, one ahead in registers (behind the last one the last keys again; two ahead took 42 us where one takes 38,
+    // 32 sequences of 12 .. 8000 tokens).  Loads come back in order, so the table entries of a step are asked for in front of the keys and
+    // values of the step before it
+    constexpr int KS4 = 4 * KT;
     int kb = kbeg + wave * KT;
     if (kb < kend) {
         Step cur, nxt;
-        int place = 0;
-        if constexpr (ST) place = place_of(kb);
-        int after = 0;
-        if constexpr (ST) after = place_of(kb + 4 * KT);
+        int place = 0, after = 0;
+        if constexpr (ST) {
+            place = place_of(kb);
+            after = place_of(kb + KS4);
+        }
         load(cur, kb, place);
 #pragma unroll 1
-        for (; kb < kend; kb += 4 * KT) {
+        for (; kb < kend; kb += KS4) {
             place = after;
-            if constexpr (ST) after = place_of(kb + 8 * KT);
-            load(nxt, kb + 4 * KT, place);
+            if constexpr (ST) after = place_of(kb + 2 * KS4);
+            load(nxt, kb + KS4, place);
             step(cur, kb);
             cur = nxt;
         }
@@ -453,26 +458,25 @@ prompt_few_kernel(PromptArgs a) {
 // Joins the runs of the tiles that more than one block has.  Such a tile holds the first unit of a block: block b takes the tile that
 // holds its own first unit, unless the one before it does already.  16 threads a row; few rows share out the runs between them.
 template <typename T, int DP, int SRC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(512)
 prompt_meet_kernel(PromptArgs a) {
-    constexpr int DV = DP / 16;
-    __shared__ float s_o[16][DP], s_ml[16][2];
+    constexpr int DV = DP / 16, SLOTS = 32, RU = 4;         // rows x groups of runs of a block, runs in flight
+    __shared__ float s_o[SLOTS][DP], s_ml[SLOTS][2];
     PromptWalk<SRC> walk(a);
-    const int64_t W = walk.total(), sharers = min((int64_t)a.blocks, W), b0 = blockIdx.x;       // b0: the first block that has the tile
-    if (b0 + 1 >= sharers) return;
-    const int64_t lo = prompt_block_begin(a, W, b0), w = prompt_block_begin(a, W, b0 + 1);
+    const PromptShares shares(a, walk.total());
+    const int64_t b0 = blockIdx.x;                          // the first block that has the tile
+    if (b0 + 1 >= shares.B) return;
+    const int64_t lo = shares.begin(b0), w = shares.begin(b0 + 1);
     if (!walk.find(w)) return;
-    const int U = walk.tile_units(), off = (int)((w - walk.base) % U);
+    const int U = walk.tile_units();
+    int off;
+    const int item = prompt_item(w - walk.base, U, off), tile = item / a.Hk, hk = item - tile * a.Hk;
     const int64_t w0 = w - off, w1 = w0 + U;
     if (off == 0 || (b0 > 0 && lo > w0)) return;            // no tile is cut here, or it is cut further in front, too
     const PromptSeq q = walk.seq();
-    const int item = (int)((w - walk.base) / U), tile = item / a.Hk, hk = item - tile * a.Hk;
-    int64_t b1 = (w1 - 1) * sharers / W;                    // the last block that has it
-    while (prompt_block_begin(a, W, b1 + 1) <= w1 - 1) ++b1;
-    while (prompt_block_begin(a, W, b1) > w1 - 1) --b1;
-    const int runs = (int)(b1 - b0) + 1;
+    const int runs = (int)(shares.block_of(w1 - 1) - b0) + 1;
     const int64_t rows = (int64_t)q.Lq * a.G, r0 = (int64_t)tile * 16;
-    const int nrow = (int)min((int64_t)16, rows - r0), per = nrow <= 2 ? 2 : nrow <= 4 ? 4 : nrow <= 8 ? 8 : 16, groups = 16 / per;
+    const int nrow = (int)min((int64_t)16, rows - r0), per = nrow <= 2 ? 2 : nrow <= 4 ? 4 : nrow <= 8 ? 8 : 16, groups = SLOTS / per;
     const int part_row = threadIdx.x >> 4, r = part_row % per, group = part_row / per, d0 = (threadIdx.x & 15) * DV;
     // a block's run of this tile is its first one (2 b), but for a first block that begins with another tile
     const int late = lo < w0 ? 1 : 0;
@@ -481,18 +485,32 @@ prompt_meet_kernel(PromptArgs a) {
 #pragma unroll
     for (int e = 0; e < DV; ++e) o[e] = 0.f;
     if (r < nrow) {
-#pragma unroll 8
-        for (int i = group; i < runs; i += groups) mm = fmaxf(mm, part_of(i)[16 * DP + r]);
-#pragma unroll 8
-        for (int i = group; i < runs; i += groups) {
-            const float* p = part_of(i);
-            const float mw = p[16 * DP + r], f = mw == mm ? 1.f : __builtin_amdgcn_exp2f(mw - mm);
-            ll += p[16 * DP + 16 + r] * f;
+        for (int i = group; i < runs; i += RU * groups) {   // (references, sums and values of RU runs in one go)
+            float mw[RU], lw[RU];
+            f32x4 v[RU][DV / 4];
 #pragma unroll
-            for (int e = 0; e < DV; e += 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(p + r * DP + d0 + e);
+            for (int u = 0; u < RU; ++u) {
+                const float* p = part_of(min(i + u * groups, runs - 1));
+                mw[u] = p[16 * DP + r];
+                lw[u] = p[16 * DP + 16 + r];
 #pragma unroll
-                for (int x = 0; x < 4; ++x) o[e + x] += v[x] * f;
+                for (int e = 0; e < DV / 4; ++e) v[u][e] = *reinterpret_cast<const f32x4*>(p + r * DP + d0 + 4 * e);
+            }
+            float m2 = mm;
+#pragma unroll
+            for (int u = 0; u < RU; ++u) m2 = fmaxf(m2, mw[u]);
+            const float f0 = mm == m2 ? 1.f : __builtin_amdgcn_exp2f(mm - m2);
+            mm = m2;
+            ll *= f0;
+#pragma unroll
+            for (int e = 0; e < DV; ++e) o[e] *= f0;
+#pragma unroll
+            for (int u = 0; u < RU; ++u) {
+                if (i + u * groups >= runs) break;
+                const float f = mw[u] == mm ? 1.f : __builtin_amdgcn_exp2f(mw[u] - mm);
+                ll += lw[u] * f;
+#pragma unroll
+                for (int e = 0; e < DV; ++e) o[e] += v[u][e / 4][e % 4] * f;
             }
         }
     }
@@ -567,7 +585,7 @@ static int launch_few_as(const PromptArgs& a, hipStream_t st) {
     prompt_few_kernel<T, DP, SRC><<<(unsigned)a.blocks, 256, 0, st>>>(a);
     PS_TRY(check_launch("prompt_few_kernel"));
     if (a.unit == INT32_MAX) return PSERVE_OK;
-    prompt_meet_kernel<T, DP, SRC><<<(unsigned)a.blocks, 256, 0, st>>>(a);
+    prompt_meet_kernel<T, DP, SRC><<<(unsigned)a.blocks, 512, 0, st>>>(a);
     return check_launch("prompt_meet_kernel");
 }
 template <typename T, int DP>
