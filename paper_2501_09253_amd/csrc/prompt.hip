@@ -42,25 +42,47 @@ static PromptArgs prompt_args(const pserve_prompt_desc* d) {
     return a;
 }
 
-// Rows of a tile and shares of its keys.
+// Rows of a tile, and shares of its keys where the call has few tiles: a tile of 16 rows needs the least work for few rows, one of 256 reads
+// and turns its keys for the most rows but needs the whole register file.  us measured for 16 / 128 / 256 rows, the last two with their best
+// number of shares (bf16, packed; "n of queries x keys", 8 heads of keys with 4 of queries each; heads of 64, then of 128 values):
+//   1 of 256 x 256       9 / 11 / 15      13 / 15 / 24          2 of 1024 x 1024     65 / 34 / 29     125 / 51 / 47
+//   32 of 8 x 2048      29 / 45 / 57      53 / 72 / 71          1 of 512 x 4096      96 / 46 / 41     161 / 80 / 59
+//   8 of 77 x 77        14 /  9 / 12      22 / 11 / 19          32 of 512 x 512     326 / 100 / 84    687 / 242 / 226
+//   8 of 300 x 300      46 / 21 / 22      89 / 39 / 44          1 of 8192 x 8192   1173 / 394 / 278  2372 / 963 / 520
+// and with 12 heads, each with its own keys:
+//   32 of 8 x 2048      33 / 57 / 70      53 / 111 / 126        32 of 512 x 512     135 / 51 / 61     263 / 109 / 164
+//   8 of 77 x 77         8 /  9 / 12      11 / 11 / 20          1 of 8192 x 8192    455 / 164 / 148   905 / 404 / 240
+// So: 16 rows for sequences of up to 32 rows and where there are few tiles with few keys; 256 where they are filled, the mask's diagonal is
+// a small part of them (keys * G) and they keep the chip busy; else 128.  Over the 8-bit store, whose keys are turned into bf16 on their way
+// to the matrix cores, there is no form of 256 rows.
 static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
-    const int64_t max_q = d->max_q ? d->max_q : cdiv(d->q_tokens, d->n), 
-                  keys = d->max_k ? d->max_k : src == SRC_PACKED ? cdiv(std::max<int64_t>(d->k_tokens, 0), d->n) : 1024;
-    if (d->dtype == PSERVE_BF16 && max_q * a.G > 16) {
-        a.rows = src == SRC_PACKED && prompt_slots(a, a.G, 256) * a.Hk >= 512 ? 256 : 128;
-        a.splits = (int)std::max<int64_t>(1, std::min(512 / (prompt_slots(a, a.G, a.rows) * a.Hk), keys / 512));
+    const int64_t max_q = d->max_q ? d->max_q : cdiv(d->q_tokens, d->n),
+                  mean = src == SRC_PACKED ? cdiv(std::max<int64_t>(d->k_tokens, 1), d->n) : 1024, keys = d->max_k ? d->max_k : mean;
+    auto tiles = [&](int rows) { return prompt_slots(a, a.G, rows) * a.Hk; };
+    a.splits = 1;
+    if (d->dtype == PSERVE_BF16 && max_q * a.G > 32 && (keys > 512 || tiles(16) >= 768)) {
+        const bool wide = src == SRC_PACKED && max_q * a.G >= 256 && keys * a.G >= 1024 && tiles(256) * keys >= (1 << 18);
+        a.rows = wide ? 256 : 128;
+        // Shares of the keys fill the chip, with one block a CU or two: 1 of 512 x 4096 in 256 / 512 / 768 blocks takes 32 / 31 / 37 us (12 heads
+        // of 64, packed), 44 / 54 / 65 (of 128); over the store 71 / 53 / 51 and 88 / 65 / 82 (8 x 4 heads).  Where the longest sequence has
+        // more keys than the mean most blocks end early, so more are wanted: 8 of 32 x 100 .. 12800, heads of 128: 191 us in 256, 81 in 768.
+        // Joining the shares has its price: 4 of 20 .. 700 take 21 us in one share, 31 in two; 2 of 1024 x 1024 (12 heads of 64) 27 and 32.
+        int64_t want = wide || (src == SRC_PACKED && a.D > 64) ? 256 : 512;
+        const int64_t t = tiles(a.rows);
+        if (src == SRC_PACKED) want = want * std::min(std::max(keys, mean), 3 * mean) / mean;
+        if (4 * t < 3 * want && 7 * t <= want * keys / 512) a.splits = (int)std::max<int64_t>(1, std::min(cdiv(want, t), keys / (wide ? 512 : 256)));
         return;
     }
     a.rows = 16;
-    a.splits = 1;
-    const int64_t items = prompt_slots(a, a.G, 16) * a.Hk;
-    if (keys <= 512 || items >= 768) {         // a tile is one unit, nothing to join
+    const int64_t items = tiles(16);
+    // up to 512 keys a block has a tile to itself: cutting it costs more than it saves; so it is where there are tiles enough
+    if (keys <= 512 || items >= 768) {
         a.unit = INT32_MAX;
         a.lead = 0;
         a.blocks = (int32_t)std::min<int64_t>(items, 1 << 23);
     } else {
         a.unit = 128;
-        a.lead = 1;
+        a.lead = 1;                             // (32 tokens over 12 .. 8000 keys of the store: 45 us with none, 37, 38, 39 with 1, 2, 3)
         a.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(512, items * cdiv(keys, 128) / 2));
     }
 }
