@@ -326,14 +326,17 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   The queries of a sequence of L_q queries and L_k keys stand at the END of its keys: with causal != 0 query i sees the keys
  *   j <= i + L_k - L_q, else all keys of its sequence.  A query that sees no key gives zeros.  Rows of o in front of the first
  *   and behind the last sequence are left as they are.  A key or value that a query does not see has no part in its result,
- *   whatever it holds; one that is not finite makes the results of the queries that see it NaN or infinite.
+ *   whatever it holds; one that it sees and that is not finite has the part that the formula gives it: a score of +infinity or
+ *   NaN makes the row NaN, one of -infinity weighs nothing (a row with no other score gives zeros), a value makes its column of
+ *   the row NaN or infinite.
  *   max_q, max_k: the longest L_q and L_k as far as the caller knows (0: unknown).  Only the choice of kernel and of the
  *   number of shares of the keys depends on them, never which keys count.
  *   workspace DEVICE, at least pserve_prompt_attention_workspace bytes (0 where none is needed; it holds the partial results
  *   of the shares and may be used for something else after the call in stream order).  o must not overlap an input.
- * Errors: EINVAL (NULL, n <= 0, heads % kv_heads, head_dim not a multiple of 16 or above 128, unknown dtype, negative sizes, more
- * than 2^30 keys,
- * pointers or strides that are no multiples of 16 bytes, a scale that is not finite, workspace too small), EHIP.
+ * Errors: EINVAL (NULL, n <= 0, heads % kv_heads, heads above 4096, head_dim not a multiple of 16 or above 128, unknown dtype,
+ * negative sizes, more than 2^30 keys, pointers or strides that are no multiples of 16 bytes, strides of 2^24 elements and more
+ * between tokens (the stride of a dimension of one is not looked at), a scale that times log2(e) is not finite in fp32, more
+ * tiles of rows than a launch has, workspace too small), EHIP.
  *
  * pserve_kv8: keys and values of `places` tokens in 8 bits.  A token's head is a group of head_dim values with one fp32 scale
  * amax / 127, each value a whole number 127 x / amax rounded to nearest (halves to even; exact); a group with an infinity or a
@@ -347,7 +350,8 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   page table[s][j / page], i.e. place table[s][j / page] * page + j % page; table DEVICE int32 [n][max_pages], key_len DEVICE
  *   int32 [n] (cut to max_pages * page), page a power of two.  Keys on pages outside the store count as not there.  desc's
  *   kv_heads and head_dim are the store's; its k / v fields (k_tokens, strides) are not read.
- * Errors: EINVAL, also for a store of another device than the current one; ENOMEM; EHIP.
+ * Errors: EINVAL, also for a store of another device than the current one and for 2^28 groups (rows x kv_heads) and more in one
+ * write or read; ENOMEM; EHIP.
  *
  * pserve_linear8: y = x W + b (+ residual) with x and W in 8-bit integers.  W [K][N] is quantised once, a scale for each
  * output channel; x [rows][K] in the call, a scale for each token (quantised as the store's groups are: a group is a column of W
@@ -357,7 +361,7 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   kept (rounded up to 128 values, columns to 256); the caller's buffers are not referenced afterwards.
  * pserve_linear8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y),
  *   y DEVICE [rows][N]; workspace DEVICE, 16-byte aligned, at least pserve_linear8_workspace bytes.  y must not overlap x.
- * Errors: EINVAL (NULL, sizes <= 0, K above 131072, ldx < K, workspace too small, another device than the current one),
+ * Errors: EINVAL (NULL, sizes <= 0, K above 131072, N above 2^24, 2^26 rows and more, ldx < K, workspace too small, another device than the current one),
  * ENOMEM, EHIP. */
 typedef struct {
     int32_t n;                      /* sequences */

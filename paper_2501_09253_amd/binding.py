@@ -587,8 +587,9 @@ def _prompt_out(who: str, q, out, *inputs):
         return torch.empty(q.shape, dtype=q.dtype, device=q.device)
     _need(out.shape == q.shape and out.dtype == q.dtype, f"{who}: out must have q's shape and dtype")
     _need(out.stride(2) == 1, f"{who}: the values of a head must be consecutive")
-    _need(out.numel() == 0 or (out.stride(0) >= out.shape[2] or out.shape[0] == 1) and (out.stride(1) >= out.shape[2] or out.shape[1] == 1),
-          f"{who}: rows of out overlap")
+    (T, H, D), (st, sh, _) = out.shape, out.stride()        # heads inside tokens or tokens inside heads
+    _need(out.numel() == 0 or (H == 1 or sh >= D) and (T == 1 or st >= (H - 1) * (sh if H > 1 else 0) + D)
+          or (T == 1 or st >= D) and (H == 1 or sh >= (T - 1) * (st if T > 1 else 0) + D), f"{who}: rows of out overlap")
     _apart(who, out, q, *inputs)
     return out
 
@@ -615,7 +616,7 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optio
         raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
     out = _prompt_out(who, q, out, k, v)
     d, need = _prompt_desc(cu_q.shape[0] - 1, q.shape[1], k.shape[1], q.shape[2], BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), scale,
-                           max_q, max_k, q.shape[0], k.shape[0], q.stride(), sk, sv, out.stride())
+                           int(max_q), int(max_k), q.shape[0], k.shape[0], q.stride(), sk, sv, out.stride())
     ws, nws, keep = _workspace(need, workspace, q.device, who)
     _check(lib().pserve_prompt_attention(d, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
                                          ws, nws, out.data_ptr(), _stream()))
@@ -687,7 +688,7 @@ class KV8:
         _need(q.dim() == 3 and q.shape[1] > 0 and q.shape[2] == self.head_dim, f"{who}: q must be [Tq, heads, {self.head_dim}]")
         out = _prompt_out(who, q, out)
         d, need = _prompt_desc(n, q.shape[1], self.kv_heads, self.head_dim, BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), scale,
-                               max_q, max_k, q.shape[0], 0, q.stride(), (0, 0), (0, 0), out.stride())
+                               int(max_q), int(max_k), q.shape[0], 0, q.stride(), (0, 0), (0, 0), out.stride())
         ws, nws, keep = _workspace(need, workspace, q.device, who)
         _check(lib().pserve_kv8_attention(self._h, d, q.data_ptr(), cu_q.data_ptr(), key_len.data_ptr(), table.data_ptr(),
                                           table.shape[1], page, ws, nws, out.data_ptr(), _stream()))

@@ -138,6 +138,12 @@ static int check_device(const pserve_kv8_t* s, const char* who) {
     return PSERVE_OK;
 }
 
+// up to 16 threads a group, fewer than 2^32 in a launch: refused before the first launch, so that no claim is left behind
+static int check_rows(const pserve_kv8_t* s, int64_t rows, const char* who) {
+    PS_REQUIRE(rows >= 0 && rows < (1 << 28) && rows * s->heads < (1 << 28), "%s: %lld rows of %d heads", who, (long long)rows, s->heads);
+    return PSERVE_OK;
+}
+
 static Kv8Args kv8_args(const pserve_kv8_t* s) {
     Kv8Args a{};
     a.k8 = s->k; a.v8 = s->v; a.ks = s->k_scale; a.vs = s->v_scale; a.owner = s->owner;
@@ -183,14 +189,15 @@ int pserve_kv8_write(pserve_kv8_t* store, const void* k, const void* v, int dtyp
     static const char who[] = "pserve_kv8_write";
     PS_REQUIRE(store && k_stride && v_stride, "%s: NULL argument", who);
     PS_REQUIRE(dtype == PSERVE_F32 || dtype == PSERVE_BF16, "%s: unknown dtype %d", who, dtype);
-    PS_REQUIRE(rows >= 0 && rows <= INT32_MAX && rows * store->heads <= INT32_MAX, "%s: %lld rows", who, (long long)rows);
+    PS_TRY(check_rows(store, rows, who));
     if (rows == 0) return PSERVE_OK;
     PS_REQUIRE(k && v && places, "%s: NULL buffer", who);
     PS_TRY(check_device(store, who));
     PS_REQUIRE(!(((uintptr_t)k | (uintptr_t)v) & 15), "%s: k and v must be 16-byte aligned", who);
     const int64_t vn = 16 / (int64_t)dtype_size(dtype);
-    for (int i = 0; i < 2; ++i)
-        PS_REQUIRE(k_stride[i] >= 0 && v_stride[i] >= 0 && k_stride[i] % vn == 0 && v_stride[i] % vn == 0, "%s: strides must be multiples of 16 bytes", who);
+    for (int i = 0; i < 2; ++i)                             // (that of a dimension of one is any number)
+        PS_REQUIRE((i ? store->heads : rows) == 1 || (k_stride[i] >= 0 && v_stride[i] >= 0 && k_stride[i] % vn == 0 && v_stride[i] % vn == 0),
+                   "%s: strides must be multiples of 16 bytes", who);
     Kv8Args a = kv8_args(store);
     a.k = k; a.v = v; a.places_of = places; a.rows = rows;
     a.k_row = k_stride[0]; a.k_head = k_stride[1]; a.v_row = v_stride[0]; a.v_head = v_stride[1];
@@ -203,7 +210,7 @@ int pserve_kv8_read(const pserve_kv8_t* store, const int64_t* places, int64_t ro
     static const char who[] = "pserve_kv8_read";
     PS_REQUIRE(store, "%s: NULL argument", who);
     PS_REQUIRE(dtype == PSERVE_F32 || dtype == PSERVE_BF16, "%s: unknown dtype %d", who, dtype);
-    PS_REQUIRE(rows >= 0 && rows <= INT32_MAX && rows * store->heads <= INT32_MAX, "%s: %lld rows", who, (long long)rows);
+    PS_TRY(check_rows(store, rows, who));
     if (rows == 0) return PSERVE_OK;
     PS_REQUIRE(k && v && places, "%s: NULL buffer", who);
     PS_TRY(check_device(store, who));

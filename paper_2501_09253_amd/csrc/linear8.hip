@@ -551,7 +551,7 @@ void pserve_linear8_free(pserve_linear8_t* op) { delete op; }
 
 int pserve_linear8_workspace(const pserve_linear8_t* op, int64_t rows, size_t* bytes) {
     PS_REQUIRE(op && bytes, "pserve_linear8_workspace: NULL argument");
-    PS_REQUIRE(rows >= 0 && rows <= INT32_MAX, "pserve_linear8_workspace: %lld rows", (long long)rows);
+    PS_REQUIRE(rows >= 0 && rows < (1 << 26), "pserve_linear8: %lld rows (fewer than 2^26)", (long long)rows);     // 64 threads a row, 2^32 a launch
     *bytes = x8_bytes(op, rows) + (size_t)rows * sizeof(float);
     return PSERVE_OK;
 }

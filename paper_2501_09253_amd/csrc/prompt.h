@@ -18,7 +18,8 @@ struct PromptArgs {
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;     // strides in elements
     int32_t n, H, Hk, G, D, causal;
     int32_t rows, splits;               // rows of a tile, shares of its keys (wide tiles)
-    int32_t unit, lead, blocks;         // tiles of 16 rows: keys of a unit of work, units a tile costs besides, blocks that share the units
+    int32_t unit, lead, blocks;         // tiles of 16 rows: keys of a unit of work (0: tiles are not cut), units a tile costs besides, blocks
+    int32_t items;                      // tiles that are not cut: slots of tiles times key/value heads
     int32_t max_pages, page_shift, pages;
     float scale2;                       // scale * log2(e)
 };
@@ -51,26 +52,31 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs& a, int s) {
 // Tiles of R rows over sequences of cu_q[s + 1] - cu_q[s] tokens of G rows each, without a table made by the host: sequence s has
 // the slots from floor(cu_q[s] G / R) + s on, at least as many as it has tiles.  false: no sequence's.
 __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, int64_t slot, int& s, int& tile) {
+    // the last sequence whose slots begin at `slot` or in front of it, 64 places of the range looked at in one go (a walk over all of them
+    // took 66 ms of a call of 16,384 single tokens over 100 keys each); where the starts do not ascend, any one
     const int lane = threadIdx.x & 63;
-    int count = 0;
-    for (int b = 0; b < a.n; b += 64) {
-        const int i = b + lane;
-        const bool le = i < a.n && prompt_start(a.cu_q, i, a.q_tokens) * G / R + i <= slot;
-        const uint64_t m = __ballot(le);
-        count += __popcll(m);
-        if (m != ~0ull) break;
+    int lo = 0, len = a.n;
+    for (;;) {
+        const int step = (len + 63) / 64, i = lo + lane * step;
+        const bool le = lane * step < len && prompt_start(a.cu_q, i, a.q_tokens) * G / R + i <= slot;
+        const uint64_t past = ~__ballot(le);
+        const int count = past ? __ffsll((unsigned long long)past) - 1 : 64;
+        if (count == 0) return false;
+        lo += (count - 1) * step;
+        len = min(step, len - (count - 1) * step);
+        if (step == 1) break;
     }
-    if (count == 0) return false;
-    s = __builtin_amdgcn_readfirstlane(count - 1);
+    s = __builtin_amdgcn_readfirstlane(lo);
     const int64_t t = slot - (prompt_start(a.cu_q, s, a.q_tokens) * G / R + s);
     tile = (int)t;
     return true;
 }
 inline int64_t prompt_slots(const PromptArgs& a, int G, int R) { return a.q_tokens * G / R + a.n; }
 
-// The work of the 16-row tiles in units of `unit` keys of one tile: sequence s has tiles x Hk x U_s of them, the blocks take equal runs of
+// The work of the 16-row tiles, where they are cut, in units of `unit` keys of one tile: sequence s has tiles x Hk x U_s of them, the blocks take equal runs of
 // the numbered units, whatever the sequences' lengths are.  The first `lead` units of a tile stand for what it costs besides its keys (its
-// queries, the way to the first keys, the meeting of the wavefronts): without them a block of short sequences is the last to end.  Every wavefront walks the sequences by itself, 64 at a time, one a lane.
+// queries, the way to the first keys, the meeting of the wavefronts): without them a block of short sequences is the last to end.  Every
+// wavefront walks the sequences by itself, 64 at a time, one a lane (tiles are cut where there are fewer than 768).
 __device__ __forceinline__ int64_t uniform64(int64_t v) {      // the same in all lanes: into scalar registers
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
 }
@@ -89,7 +95,9 @@ struct PromptWalk {
     int s = 0;
     int64_t base = 0;
 
-    __device__ __forceinline__ explicit PromptWalk(const PromptArgs& a_) : a(a_) { load(); }
+    __device__ __forceinline__ explicit PromptWalk(const PromptArgs& a_) : a(a_) {
+        if (a.unit) load();
+    }
     __device__ __forceinline__ void load() {
         const int lane = threadIdx.x & 63;
         units = 0;

@@ -9,6 +9,8 @@ static int current_device(int* dev) {
     return PSERVE_OK;
 }
 
+static float scale_log2(const pserve_prompt_desc* d) { return (float)((double)d->scale * 1.4426950408889634); }
+
 static int check_desc(const pserve_prompt_desc* d, const char* who) {
     PS_REQUIRE(d, "%s: desc is NULL", who);
     PS_REQUIRE(d->n > 0, "%s: need n > 0 sequences", who);
@@ -16,29 +18,30 @@ static int check_desc(const pserve_prompt_desc* d, const char* who) {
     PS_REQUIRE(d->heads > 0 && d->kv_heads > 0 && d->heads % d->kv_heads == 0, "%s: %d heads over %d key/value heads", who, d->heads, d->kv_heads);
     PS_REQUIRE(d->heads <= 4096, "%s: more than 4096 heads", who);
     PS_REQUIRE(d->head_dim > 0 && d->head_dim % 16 == 0 && d->head_dim <= 128, "%s: head_dim %d is not a multiple of 16 up to 128", who, d->head_dim);
-    PS_REQUIRE(std::isfinite(d->scale), "%s: the scale is not finite", who);
+    PS_REQUIRE(std::isfinite(d->scale) && std::isfinite(scale_log2(d)), "%s: the scale is not finite (or times log2(e) is not)", who);
     PS_REQUIRE(d->q_tokens >= 0 && d->q_tokens <= INT32_MAX && d->max_q >= 0 && d->max_k >= 0, "%s: negative or too large sizes", who);
     return PSERVE_OK;
 }
 
-// strides and pointers of a [tokens][heads][head_dim] tensor: 16-byte rows; the rows of a tile are addressed in 32 bits
-static int check_tensor(const pserve_prompt_desc* d, const void* p, const int64_t* stride, const char* name, const char* who) {
+// strides and pointers of a [tokens][heads][head_dim] tensor: 16-byte rows; the rows of a tile are addressed in 32 bits.  The stride of a
+// dimension of one (or none) is any number: it counts as 0.
+static int check_tensor(const pserve_prompt_desc* d, const void* p, const int64_t* stride, int64_t tokens, int32_t heads, const char* name, const char* who,
+                        int64_t& row, int64_t& head) {
     const int64_t vn = 16 / (int64_t)dtype_size(d->dtype);
     PS_REQUIRE(((uintptr_t)p & 15) == 0, "%s: %s is not 16-byte aligned", who, name);
-    for (int i = 0; i < 2; ++i)
-        PS_REQUIRE(stride[i] >= 0 && stride[i] < (int64_t)1 << (i ? 40 : 24) && stride[i] % vn == 0,
-                   "%s: stride %lld of %s is not a multiple of 16 bytes or too large", who, (long long)stride[i], name);
+    row = tokens > 1 ? stride[0] : 0;
+    head = heads > 1 ? stride[1] : 0;
+    PS_REQUIRE(row >= 0 && row < (int64_t)1 << 24 && row % vn == 0 && head >= 0 && head < (int64_t)1 << 40 && head % vn == 0,
+               "%s: a stride of %s (%lld, %lld) is not a multiple of 16 bytes or too large", who, name, (long long)row, (long long)head);
     return PSERVE_OK;
 }
 
 static PromptArgs prompt_args(const pserve_prompt_desc* d) {
     PromptArgs a{};
     a.q_tokens = d->q_tokens;
-    a.q_row = d->q_stride[0]; a.q_head = d->q_stride[1];
-    a.o_row = d->o_stride[0]; a.o_head = d->o_stride[1];
     a.n = d->n; a.H = d->heads; a.Hk = d->kv_heads; a.G = d->heads / d->kv_heads; a.D = d->head_dim;
     a.causal = d->causal != 0;
-    a.scale2 = (float)((double)d->scale * 1.4426950408889634);
+    a.scale2 = scale_log2(d);
     return a;
 }
 
@@ -57,7 +60,7 @@ static PromptArgs prompt_args(const pserve_prompt_desc* d) {
 // to the matrix cores, there is no form of 256 rows.
 static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
     const int64_t max_q = d->max_q ? d->max_q : cdiv(d->q_tokens, d->n),
-                  mean = src == SRC_PACKED ? cdiv(std::max<int64_t>(d->k_tokens, 1), d->n) : 1024, keys = d->max_k ? d->max_k : mean;
+                  mean = src == SRC_PACKED ? cdiv(std::min<int64_t>(std::max<int64_t>(d->k_tokens, 1), 1 << 30), d->n) : 1024, keys = d->max_k ? d->max_k : mean;
     auto tiles = [&](int rows) { return prompt_slots(a, a.G, rows) * a.Hk; };
     a.splits = 1;
     if (d->dtype == PSERVE_BF16 && max_q * a.G > 32 && (keys > 512 || tiles(16) >= 768)) {
@@ -77,8 +80,8 @@ static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
     const int64_t items = tiles(16);
     // up to 512 keys a block has a tile to itself: cutting it costs more than it saves; so it is where there are tiles enough
     if (keys <= 512 || items >= 768) {
-        a.unit = INT32_MAX;
-        a.lead = 0;
+        a.unit = a.lead = 0;
+        a.items = (int32_t)std::min<int64_t>(items, INT32_MAX);     // (more are refused)
         a.blocks = (int32_t)std::min<int64_t>(items, 1 << 23);
     } else {
         a.unit = 128;
@@ -89,15 +92,16 @@ static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
 
 static size_t part_bytes(const PromptArgs& a) {
     const size_t tile = (size_t)a.rows * ((a.D <= 64 ? 64 : 128) + 2) * sizeof(float);
-    if (a.rows == 16) return a.unit == INT32_MAX ? 0 : 2 * (size_t)a.blocks * tile;
+    if (a.rows == 16) return a.unit == 0 ? 0 : 2 * (size_t)a.blocks * tile;
     return a.splits == 1 ? 0 : (size_t)prompt_slots(a, a.G, a.rows) * a.Hk * a.splits * tile;
 }
 
 static int run(const pserve_prompt_desc* d, PromptArgs& a, int src, void* workspace, size_t bytes, hipStream_t st, const char* who) {
     if (d->q_tokens == 0) return PSERVE_OK;
     choose(d, a, src);
-    // (a launch has at most 2^32 threads)
-    PS_REQUIRE(prompt_slots(a, a.G, a.rows) * a.Hk * std::max(a.splits, 16) < (1 << 24), "%s: too many tiles of rows", who);
+    // (a launch has fewer than 2^32 threads; the blocks of the 16-row tiles share them out, numbered in 31 bits)
+    const int64_t tiles = prompt_slots(a, a.G, a.rows) * a.Hk;
+    PS_REQUIRE(a.rows == 16 ? tiles <= INT32_MAX : tiles * std::max(a.splits, a.rows / 16) < (1 << 24), "%s: too many tiles of rows", who);
     const size_t need = part_bytes(a);
     PS_REQUIRE(bytes >= need && (need == 0 || (workspace && ((uintptr_t)workspace & 15) == 0)), "%s: workspace of %zu bytes, %zu needed (16-byte aligned)", who,
                bytes, need);
@@ -127,16 +131,14 @@ int pserve_prompt_attention(const pserve_prompt_desc* desc, const void* q, const
     PS_REQUIRE(desc->k_tokens >= 0 && desc->k_tokens <= (1 << 30), "%s: negative or too large sizes", who);
     if (desc->q_tokens == 0) return PSERVE_OK;
     PS_REQUIRE(q && o && cu_q && cu_k && ((k && v) || desc->k_tokens == 0), "%s: NULL buffer", who);
-    PS_TRY(check_tensor(desc, q, desc->q_stride, "q", who));
-    PS_TRY(check_tensor(desc, k, desc->k_stride, "k", who));
-    PS_TRY(check_tensor(desc, v, desc->v_stride, "v", who));
-    PS_TRY(check_tensor(desc, o, desc->o_stride, "o", who));
     PromptArgs a = prompt_args(desc);
+    PS_TRY(check_tensor(desc, q, desc->q_stride, desc->q_tokens, desc->heads, "q", who, a.q_row, a.q_head));
+    PS_TRY(check_tensor(desc, k, desc->k_stride, desc->k_tokens, desc->kv_heads, "k", who, a.k_row, a.k_head));
+    PS_TRY(check_tensor(desc, v, desc->v_stride, desc->k_tokens, desc->kv_heads, "v", who, a.v_row, a.v_head));
+    PS_TRY(check_tensor(desc, o, desc->o_stride, desc->q_tokens, desc->heads, "o", who, a.o_row, a.o_head));
     a.Q = q; a.K = k; a.V = v; a.O = o;
     a.cu_q = cu_q; a.cu_k = cu_k;
     a.k_tokens = desc->k_tokens;
-    a.k_row = desc->k_stride[0]; a.k_head = desc->k_stride[1];
-    a.v_row = desc->v_stride[0]; a.v_head = desc->v_stride[1];
     return run(desc, a, SRC_PACKED, workspace, workspace_bytes, (hipStream_t)stream, who);
 }
 
@@ -154,9 +156,9 @@ int pserve_kv8_attention(const pserve_kv8_t* store, const pserve_prompt_desc* de
     int dev;
     PS_TRY(current_device(&dev));
     PS_REQUIRE(dev == store->device, "%s: the store is on device %d, the current one is %d", who, store->device, dev);
-    PS_TRY(check_tensor(desc, q, desc->q_stride, "q", who));
-    PS_TRY(check_tensor(desc, o, desc->o_stride, "o", who));
     PromptArgs a = prompt_args(desc);
+    PS_TRY(check_tensor(desc, q, desc->q_stride, desc->q_tokens, desc->heads, "q", who, a.q_row, a.q_head));
+    PS_TRY(check_tensor(desc, o, desc->o_stride, desc->q_tokens, desc->heads, "o", who, a.o_row, a.o_head));
     a.Q = q; a.O = o; a.cu_q = cu_q;
     a.k8 = store->k; a.v8 = store->v; a.k_scale = store->k_scale; a.v_scale = store->v_scale;
     a.key_len = key_len; a.table = table; a.max_pages = max_pages;

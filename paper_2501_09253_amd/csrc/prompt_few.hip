@@ -1,9 +1,10 @@
 // Causal attention with grouped heads, gfx950: tiles of 16 rows, keys shared out between wavefronts and blocks.
 //
 // A row is a query token's head; the G heads that share a key/value head are neighbouring rows of that head's tile, so one pass
-// over keys and values serves them all.  One block has one tile of 16 rows and a share of its keys; its four wavefronts take 32 keys
-// (fp32: 16) at a time in turn, each with a softmax of its own (running maximum and sum in fp32), and meet in LDS at the end.
-// Where the call has few tiles the keys are shared out between `splits` blocks, whose results a second kernel joins.
+// over keys and values serves them all.  A block's four wavefronts take 32 keys (fp32: 16) of a tile at a time in turn, each with a
+// softmax of its own (running maximum and sum in fp32), and meet in LDS at the end.  Where there are tiles enough a block has whole
+// ones; where there are few, or few with many keys, all tiles' keys are cut into units of 128, the blocks take equal runs of
+// them whatever the sequences' lengths are, and a second kernel joins the tiles that more than one block has.
 //
 // Scores are formed transposed, S^T = K Q^T on 16 x 16 matrix instructions, so a lane owns one row and NV consecutive keys; the keys
 // of a step are assigned to the instruction's rows so that the lane's probabilities are the B operand of O^T = V^T P^T as they lie.
@@ -54,25 +55,47 @@ prompt_few_kernel(PromptArgs a) {
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g4 = lane >> 4;
+    const int64_t b = blockIdx.x;
     PromptWalk<SRC> walk(a);
-    const int64_t W = walk.total();
-    if ((int64_t)blockIdx.x >= W) return;
-    // where tiles are not cut the last ones come first: under a causal mask they have the most keys
-    const PromptShares shares(a, W);
-    const int64_t b = a.unit == INT32_MAX ? shares.B - 1 - blockIdx.x : (int64_t)blockIdx.x;
-    int64_t w = shares.begin(b);
-    const int64_t w_lo = w, w_end = shares.begin(b + 1);
+    int64_t w = b, w_lo = 0, w_end = a.items;
+    if (a.unit) {
+        const int64_t W = walk.total();
+        if (b >= W) return;
+        const PromptShares shares(a, W);
+        w = w_lo = shares.begin(b);
+        w_end = shares.begin(b + 1);
+    }
     for (bool again = false; w < w_end; again = true) {
     if (again) __syncthreads();                             // LDS is taken again
-    // ---- the next run of units: a tile's, or what the block has of it
-    if (!walk.find(w)) return;
-    const PromptSeq q = walk.seq();
-    const int s = walk.s, U = walk.tile_units();
-    int off;
-    const int item = prompt_item(w - walk.base, U, off), tile = item / a.Hk, hk = item - tile * a.Hk;
-    const int take = (int)min((int64_t)(U - off), w_end - w);
-    const bool first = w == w_lo;
-    w += take;
+    PromptSeq q;
+    int s, tile, hk, off = 0, take = 1, U = 1;
+    bool first = true;
+    if (a.unit) {
+        // ---- the next run of units: a tile's, or what the block has of it
+        if (!walk.find(w)) return;
+        q = walk.seq();
+        s = walk.s;
+        U = walk.tile_units();
+        const int item = prompt_item(w - walk.base, U, off);
+        tile = item / a.Hk;
+        hk = item - tile * a.Hk;
+        take = (int)min((int64_t)(U - off), w_end - w);
+        first = w == w_lo;
+        w += take;
+    } else {
+        // ---- a whole tile, the last ones first: under a causal mask they have the most keys
+        const uint32_t item = (uint32_t)(w_end - 1 - w), slot = item / (uint32_t)a.Hk;
+        w += gridDim.x;
+        hk = (int)(item - slot * (uint32_t)a.Hk);
+        if (!prompt_slot(a, a.G, 16, slot, s, tile)) continue;
+        tile = __builtin_amdgcn_readfirstlane(tile);
+        q = prompt_seq<SRC>(a, s);
+        q.q0 = uniform64(q.q0);
+        q.k0 = uniform64(q.k0);
+        q.Lq = __builtin_amdgcn_readfirstlane(q.Lq);
+        q.Lk = __builtin_amdgcn_readfirstlane(q.Lk);
+        if (tile < 0 || (int64_t)tile * 16 >= (int64_t)q.Lq * a.G) continue;
+    }
     const int64_t rows = (int64_t)q.Lq * a.G, r0 = (int64_t)tile * 16;
     const int nrow = (int)min((int64_t)16, rows - r0);
 
@@ -83,7 +106,8 @@ prompt_few_kernel(PromptArgs a) {
     const int row_end = a.causal ? max(0, min(q.Lk, tok + ahead + 1)) : q.Lk;
     const int tok_last = (int)((r0 + nrow - 1) / a.G);
     const int all = a.causal ? max(0, min(q.Lk, tok_last + ahead + 1)) : q.Lk;      // keys of the tile
-    const int kbeg = (int)min((int64_t)all, (int64_t)max(0, off - a.lead) * a.unit), kend = (int)min((int64_t)all, (int64_t)max(0, off + take - a.lead) * a.unit);
+    const int kbeg = (int)min((int64_t)all, (int64_t)max(0, off - a.lead) * a.unit);
+    const int kend = a.unit ? (int)min((int64_t)all, (int64_t)max(0, off + take - a.lead) * a.unit) : all;
     const int lim = min(row_end, kend);                     // the row's keys are those below
 
     // ---- query fragments, in the order of the contraction that the key loads below give
@@ -584,7 +608,7 @@ template <typename T, int DP, int SRC>
 static int launch_few_as(const PromptArgs& a, hipStream_t st) {
     prompt_few_kernel<T, DP, SRC><<<(unsigned)a.blocks, 256, 0, st>>>(a);
     PS_TRY(check_launch("prompt_few_kernel"));
-    if (a.unit == INT32_MAX) return PSERVE_OK;
+    if (a.unit == 0) return PSERVE_OK;
     prompt_meet_kernel<T, DP, SRC><<<(unsigned)a.blocks, 512, 0, st>>>(a);
     return check_launch("prompt_meet_kernel");
 }

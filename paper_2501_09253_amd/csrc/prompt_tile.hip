@@ -585,10 +585,7 @@ static int launch_tile_as(const PromptArgs& a, hipStream_t st) {
 }
 
 int launch_prompt_tile(const PromptArgs& a, int rows, int src, hipStream_t st) {
-    if (src == SRC_STORE) {
-        if (a.D <= 64) return rows == 128 ? launch_tile_as<64, 1, SRC_STORE>(a, st) : launch_tile_as<64, 2, SRC_STORE>(a, st);
-        return rows == 128 ? launch_tile_as<128, 1, SRC_STORE>(a, st) : launch_tile_as<128, 2, SRC_STORE>(a, st);
-    }
+    if (src == SRC_STORE) return a.D <= 64 ? launch_tile_as<64, 1, SRC_STORE>(a, st) : launch_tile_as<128, 1, SRC_STORE>(a, st);
     if (a.D <= 64) return rows == 128 ? launch_tile_as<64, 1, SRC_PACKED>(a, st) : launch_tile_as<64, 2, SRC_PACKED>(a, st);
     return rows == 128 ? launch_tile_as<128, 1, SRC_PACKED>(a, st) : launch_tile_as<128, 2, SRC_PACKED>(a, st);
 }

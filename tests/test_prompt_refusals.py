@@ -81,3 +81,32 @@ def test_binding_refuses_tensors_that_are_not_on_the_device(monkeypatch):
         ps.prompt_attention(q, q, q, cu)
     with pytest.raises(ps.PserveError, match="device"):
         ps.Linear8(torch.zeros(8, 8), None, ps.F32)
+
+
+def test_scales_that_overflow_in_the_kernel():
+    refused(ps.lib().pserve_prompt_attention(C.byref(desc(scale=3e38)), P, P, P, P, P, None, 0, P, None), "scale")
+
+
+def test_more_rows_than_a_launch_has_threads():
+    """Refused by size alone, before any launch: the objects here are images of the fields that the checks read."""
+    L = ps.lib()
+    store = (C.c_int64 * 64)()
+    store[0], store[1] = 1000, 4096 | 128 << 32                         # places; heads, head_dim
+    s = (C.c_int64 * 2)(4096 * 128, 128)
+    for rows in (1 << 16, 1 << 28, 1 << 40):
+        refused(L.pserve_kv8_write(store, P, P, 1, s, s, P, rows, None), "rows")
+        refused(L.pserve_kv8_read(store, P, rows, 1, P, P, None), "rows")
+    layer = (C.c_int64 * 64)()
+    layer[0], layer[1], layer[2] = 1 | 1 << 32, 128 | 256 << 32, 1      # K, N; rounded up; dtype
+    need = C.c_size_t()
+    assert L.pserve_linear8_workspace(layer, (1 << 26) - 1, C.byref(need)) == 0 and need.value == ((1 << 26) - 1) * 132
+    refused(L.pserve_linear8_workspace(layer, 1 << 26, C.byref(need)), "rows")
+    refused(L.pserve_linear8_forward(layer, P, 1, 1 << 26, None, P, 1 << 40, P, None), "rows")
+
+
+def test_too_many_tiles():
+    """2^31 tokens less one of 4096 heads: more 16-row tiles than 31 bits number, more wide ones than a launch has blocks."""
+    L = ps.lib()
+    for dtype in (ps.BF16, ps.F32):
+        d = desc(q_tokens=2 ** 31 - 1, heads=4096, kv_heads=4096, dtype=dtype, max_q=2 ** 20, max_k=2 ** 20)
+        refused(L.pserve_prompt_attention(C.byref(d), P, P, P, P, P, P, 1 << 60, P, None), "tiles")
