@@ -15,6 +15,7 @@
 namespace pserve {
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+typedef float __attribute__((ext_vector_type(4), aligned(4))) f32x4_4;          // of four bytes' alignment
 typedef __attribute__((address_space(3))) q8_u32x2 lds_u32x2;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
@@ -39,13 +40,16 @@ __device__ __forceinline__ void store_row(T* p, const float (&o)[DV], float inv)
     }
 }
 
-template <typename T, int DP, int SRC>
+// DP: the head's values, rounded up to 64 or 128.  DX: sixteenths of a head that are computed.  Packed fp32 heads, which the matrix
+// instructions bound (4096 tokens, 2 x 4 heads of 128: 390 us, 88 of the 154 TFLOP/s of a large product), have D / 16: with heads of 80
+// filled up to 128 they took 388 us, so 264.  The others are bound by what they read and have DP / 16.
+template <typename T, int DP, int SRC, int DX>
 __global__ void __launch_bounds__(256, 2)
 prompt_few_kernel(PromptArgs a) {
-    constexpr bool F32 = sizeof(T) == 4, ST = SRC == SRC_STORE;
-    constexpr int KT = F32 ? 16 : 32, NV = KT / 4, DT = DP / 16;
-    constexpr int KS = F32 ? DP / 4 : DP / 32;              // contraction steps of a score
-    constexpr int NQ = F32 ? DP / 4 : DP / 32;
+    constexpr bool F32 = sizeof(T) == 4, ST = SRC == SRC_STORE, EXACT = F32 && !ST;
+    constexpr int KT = F32 ? 16 : 32, NV = KT / 4, DT = DX;
+    constexpr int KS = F32 ? 4 * DX : DP / 32;              // contraction steps of a score
+    constexpr int NQ = KS;
     constexpr int BUF_ROW = DP + 4;                         // floats of a row in the meeting place (16 bytes of padding: banks)
     constexpr int VB = few_v_bytes<T, DP, SRC>();
     constexpr int MEET = 4 * 16 * BUF_ROW * 4, SMEM = MEET > 4 * VB ? MEET : 4 * VB;
@@ -132,10 +136,11 @@ prompt_few_kernel(PromptArgs a) {
     }
 
     // ---- what a wavefront holds of a step: keys in fragment order, values by rows (bf16) or in operand order (fp32)
-    constexpr int NK = F32 ? (ST ? DP / 64 : DP / 16) : 2 * (ST ? DP / 64 : DP / 32);
-    constexpr int NVL = F32 ? 4 * (ST ? 1 : DP / 64) : (ST ? DP / 32 : DP / 16);
+    constexpr int NK = F32 ? (ST ? DP / 64 : DX) : 2 * (ST ? DP / 64 : DP / 32);
+    constexpr int NVL = F32 ? (ST ? 4 : 1) : (ST ? DP / 32 : DP / 16);
     struct Step {
         u32x4 k[NK], v[NVL];
+        float vf[EXACT ? 4 : 1][DX];
         float scale;
         uint32_t bad;                                       // keys whose page is no page of the store
     };
@@ -172,7 +177,7 @@ prompt_few_kernel(PromptArgs a) {
             for (int t = 0; t < (F32 ? 1 : 2); ++t) {
                 const int j = F32 ? col : 8 * (col >> 2) + 4 * t + (col & 3);
                 const T* p = kb_ + (int64_t)key_at(j) * a.k_row;
-                constexpr int CH = F32 ? 4 : 8, NC = DP / (4 * CH);
+                constexpr int CH = F32 ? 4 : 8, NC = F32 ? DX : DP / 32;
 #pragma unroll
                 for (int i = 0; i < NC; ++i) {
                     const int d = 4 * CH * i + CH * g4;
@@ -198,9 +203,22 @@ prompt_few_kernel(PromptArgs a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const T* p = vb_ + (int64_t)key_at(4 * g4 + i) * a.v_row;
-                const int d = min(col * (DP / 16), a.D - DP / 16);
+                p += col * DX;
+                if constexpr (DX >= 4) {
+                    f32x4 w;
+                    if constexpr (DX % 4 == 0) w = *reinterpret_cast<const f32x4*>(p);
+                    else w = *reinterpret_cast<const f32x4_4*>(p);
 #pragma unroll
-                for (int c = 0; c < DP / 64; ++c) f.v[i * (DP / 64) + c] = *reinterpret_cast<const u32x4*>(p + d + 4 * c);
+                    for (int e = 0; e < 4; ++e) f.vf[i][e] = w[e];
+                }
+                if constexpr (DX == 8) {
+                    const f32x4 w = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f.vf[i][4 + e] = w[e];
+                } else {
+#pragma unroll
+                    for (int e = DX / 4 * 4; e < DX; ++e) f.vf[i][e] = p[e];
+                }
             }
         } else {
             constexpr int CH = ST ? 16 : 8, CP = DP / CH;   // values of a 16-byte chunk, chunks of a row
@@ -321,7 +339,7 @@ prompt_few_kernel(PromptArgs a) {
 #pragma unroll
                 for (int t = 0; t < DT; ++t) {
                     if constexpr (ST) vv[i][t] = (float)(int8_t)(f.v[i][t / 4] >> (8 * (t % 4)));
-                    else vv[i][t] = __uint_as_float(f.v[i * (DP / 64) + t / 4][t % 4]);
+                    else vv[i][t] = f.vf[i][t];
                 }
             if (!ST && masks) {
                 bool odd = false;
@@ -443,7 +461,7 @@ prompt_few_kernel(PromptArgs a) {
         for (int t = 0; t < DT; ++t) {
             if constexpr (F32) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) to[(4 * g4 + e) * (DP / 16) + t] = acc[t][e];
+                for (int e = 0; e < 4; ++e) to[(4 * g4 + e) * DX + t] = acc[t][e];
             } else {
                 *reinterpret_cast<f32x4*>(to + 16 * t + 4 * g4) = acc[t];
             }
@@ -604,22 +622,34 @@ int launch_prompt_join(const PromptArgs& a, hipStream_t st) {
     return check_launch("prompt_join_kernel");
 }
 
-template <typename T, int DP, int SRC>
+template <typename T, int DP, int SRC, int DX>
 static int launch_few_as(const PromptArgs& a, hipStream_t st) {
-    prompt_few_kernel<T, DP, SRC><<<(unsigned)a.blocks, 256, 0, st>>>(a);
+    prompt_few_kernel<T, DP, SRC, DX><<<(unsigned)a.blocks, 256, 0, st>>>(a);
     PS_TRY(check_launch("prompt_few_kernel"));
     if (a.unit == 0) return PSERVE_OK;
     prompt_meet_kernel<T, DP, SRC><<<(unsigned)a.blocks, 512, 0, st>>>(a);
     return check_launch("prompt_meet_kernel");
 }
-template <typename T, int DP>
-static int launch_few(const PromptArgs& a, int src, hipStream_t st) {
-    return src == SRC_STORE ? launch_few_as<T, DP, SRC_STORE>(a, st) : launch_few_as<T, DP, SRC_PACKED>(a, st);
+template <typename T, int SRC>
+static int launch_few(const PromptArgs& a, hipStream_t st) {
+    return a.D <= 64 ? launch_few_as<T, 64, SRC, 4>(a, st) : launch_few_as<T, 128, SRC, 8>(a, st);
+}
+static int launch_few_f32(const PromptArgs& a, hipStream_t st) {
+    switch (a.D / 16) {
+        case 1: return launch_few_as<float, 64, SRC_PACKED, 1>(a, st);
+        case 2: return launch_few_as<float, 64, SRC_PACKED, 2>(a, st);
+        case 3: return launch_few_as<float, 64, SRC_PACKED, 3>(a, st);
+        case 4: return launch_few_as<float, 64, SRC_PACKED, 4>(a, st);
+        case 5: return launch_few_as<float, 128, SRC_PACKED, 5>(a, st);
+        case 6: return launch_few_as<float, 128, SRC_PACKED, 6>(a, st);
+        case 7: return launch_few_as<float, 128, SRC_PACKED, 7>(a, st);
+        default: return launch_few_as<float, 128, SRC_PACKED, 8>(a, st);
+    }
 }
 
 int launch_prompt_few(const PromptArgs& a, int dtype, int src, hipStream_t st) {
-    if (dtype == PSERVE_BF16) return a.D <= 64 ? launch_few<uint16_t, 64>(a, src, st) : launch_few<uint16_t, 128>(a, src, st);
-    return a.D <= 64 ? launch_few<float, 64>(a, src, st) : launch_few<float, 128>(a, src, st);
+    if (dtype == PSERVE_BF16) return src == SRC_STORE ? launch_few<uint16_t, SRC_STORE>(a, st) : launch_few<uint16_t, SRC_PACKED>(a, st);
+    return src == SRC_STORE ? launch_few<float, SRC_STORE>(a, st) : launch_few_f32(a, st);
 }
 
 }  // namespace pserve

@@ -28,6 +28,19 @@ def test_strides_of_dimensions_of_one(L, dtype):
     same(back[1], po.held(v), torch.float32)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim", range(16, 129, 16))
+def test_every_head_size(dim, dtype):
+    """Short prompts and a few tokens over many keys; what lies behind a head in memory is NaN."""
+    lq, lk, H, Hk = [5, 40, 3], [5, 40, 1500], 6, 2
+    wide = lambda seed, n, h: torch.cat([make(seed, (n, h, dim), dtype), torch.full((n, h, 16), float("nan"), dtype=dtype)], 2)
+    q, k, v = wide(1, sum(lq), H), wide(2, sum(lk), Hk), wide(3, sum(lk), Hk)
+    cut = lambda t: t[:, :, :dim]
+    for hint in (40, 1500):
+        got = ps.prompt_attention(cut(q.cuda()), cut(k.cuda()), cut(v.cuda()), ints(starts(lq)), ints(starts(lk)), max_q=40, max_k=hint)
+        check(got, cut(q), cut(k), cut(v), lq, lk)
+
+
 def test_outputs_whose_rows_overlap_are_refused():
     T, H, D = 6, 3, 64
     q = make(1, (T, H, D), torch.bfloat16).cuda()
