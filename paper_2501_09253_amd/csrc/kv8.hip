@@ -1,7 +1,8 @@
 // The 8-bit key/value store: writing and reading rows (pserve_kv8_*).
 //
-// Both passes are bound by memory: a group (a token's head) of D values is 2 D or 4 D bytes on one side, D + 4 on the other.
-// A group is taken by LPG lanes of eight values each, so 16 bytes a lane on the wide side.
+// Both passes move a group (a token's head) of D values as 2 D or 4 D bytes on one side and D + 4 on the other.  A group is taken by LPG
+// lanes of eight values each, so 16 bytes a lane on the wide side.  20,011 tokens of 8 heads of 128, bf16 (125 MB each way): reading
+// 21 us, writing 36 with the claim.
 #include "kv8.h"
 #include "quant8.h"
 
@@ -21,7 +22,8 @@ struct Kv8Args {
 };
 
 // Which row of the call a place gets: the last one.  Calls of few rows look through the rows behind their own; larger ones
-// leave their number in `owner` in a launch of its own, and the writing launch, which finds it, sets the place back to -1.
+// leave their number in `owner` in a launch of its own.  In the writing launch a block has whole rows: the row that finds its own number
+// sets the place back to -1 once the block has looked, and a row that looks later finds -1, which is not its number either.
 constexpr int KV8_LOOK = 128;
 
 __global__ void __launch_bounds__(256)
@@ -31,15 +33,7 @@ kv8_claim_kernel(Kv8Args a) {
     const int64_t p = a.places_of[i];
     if (p >= 0 && p < a.places) atomicMax(a.owner + p, (int32_t)i);
 }
-__global__ void __launch_bounds__(256)
-kv8_release_kernel(Kv8Args a) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.rows) return;
-    const int64_t p = a.places_of[i];
-    if (p >= 0 && p < a.places) a.owner[p] = -1;
-}
-
-template <typename T, int LPG, bool CLAIMED>
+template <typename T, int LPG>
 __global__ void __launch_bounds__(256)
 kv8_write_kernel(Kv8Args a) {
     const int64_t g = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPG;      // group: (row, head)
@@ -50,32 +44,81 @@ kv8_write_kernel(Kv8Args a) {
     const int head = in ? (int)(g - row * a.heads) : 0;
     const int64_t p = a.places_of[row];
     bool mine = in && p >= 0 && p < a.places;
-    if (CLAIMED) {
-        if (mine) mine = a.owner[p] == (int32_t)row;
-    } else if (mine) {
+    if (mine) {
         bool later = false;
         for (int64_t j = row + 1 + l; j < a.rows; j += LPG) later |= a.places_of[j] == p;
         mine = !later;
     }
-    if (!CLAIMED) {
-        int other = !mine;
+    int other = !mine;
 #pragma unroll
-        for (int x = 1; x < LPG; x <<= 1) other |= __shfl_xor(other, x);
-        mine = !other;
-    }
-    float x[8] = {};
+    for (int x = 1; x < LPG; x <<= 1) other |= __shfl_xor(other, x);
+    mine = !other;
+    Raw8<T> raw = {};
     const bool has = 8 * l < a.dim;
-    if (mine && has) load8((vals ? (const T*)a.v + row * a.v_row + head * a.v_head : (const T*)a.k + row * a.k_row + head * a.k_head) + 8 * l, x);
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
-#pragma unroll
-    for (int s = 1; s < LPG; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
+    if (mine && has) load_raw((vals ? (const T*)a.v + row * a.v_row + head * a.v_head : (const T*)a.k + row * a.k_row + head * a.k_head) + 8 * l, raw);
+    const uint32_t m = lanes_max<LPG>(largest8(0, raw));
     if (!mine) return;
+    float x[8];
+    values8(raw, x);
     const Quant8 z(m);
     const int64_t at = p * a.heads + head;
     if (has) *reinterpret_cast<q8_u32x2*>((vals ? a.v8 : a.k8) + at * a.dim + 8 * l) = pack8(z, x);
     if (l == 0) (vals ? a.vs : a.ks)[at] = z.scale;
+}
+
+// Claimed rows: `per` of them a block, KV8_FLY groups a thread in flight (us with 2 and 4, both launches: 20,011 rows x 8 x 128 bf16 36.1 and
+// 37.3, 129 rows 6.5 and 8.8, 20,011 x 12 x 64 fp32 30.8 and 30.1).  fp32 groups pass at the rate of a copy (5.1 TB/s), bf16 ones, half the
+// bytes, at 3.4: what a group costs besides its bytes (addresses, its scale, the rounding) counts there.
+constexpr int KV8_FLY = 2, KV8_PER = 64;
+
+template <typename T, int LPG>
+__global__ void __launch_bounds__(256)
+kv8_write_rows_kernel(Kv8Args a, int32_t per) {
+    __shared__ int32_t s_place[KV8_PER];                    // -1: not written
+    const int64_t row0 = (int64_t)blockIdx.x * per;
+    const int rows = (int)min((int64_t)per, a.rows - row0), tid = threadIdx.x;
+    const int l = tid % LPG, groups = rows * 2 * a.heads;   // (row, keys or values, head)
+    const bool has = 8 * l < a.dim;
+    constexpr int STEP = 256 / LPG;
+    const float per_row = 1.f / (float)(2 * a.heads);       // (a block has fewer than 2^14 groups: the quotient below is exact)
+    Raw8<T> x[KV8_FLY] = {};
+    int32_t row[KV8_FLY], head[KV8_FLY];
+    bool vals[KV8_FLY];
+    auto fetch = [&](int g0) {                              // groups g0 + u STEP; behind the last one the last again
+#pragma unroll
+        for (int u = 0; u < KV8_FLY; ++u) {
+            const int g = min(g0 + u * STEP, groups - 1);
+            row[u] = (int)(((float)g + 0.5f) * per_row);
+            const int h = g - row[u] * 2 * a.heads;
+            vals[u] = h >= a.heads;
+            head[u] = vals[u] ? h - a.heads : h;
+            const int64_t r = row0 + row[u];
+            if (has) load_raw((vals[u] ? (const T*)a.v + r * a.v_row + head[u] * a.v_head : (const T*)a.k + r * a.k_row + head[u] * a.k_head) + 8 * l, x[u]);
+        }
+    };
+    fetch(tid / LPG);                                       // the rows come in beside the look at their places
+    if (tid < rows) {
+        const int64_t p = a.places_of[row0 + tid];
+        s_place[tid] = p >= 0 && p < a.places && a.owner[p] == (int32_t)(row0 + tid) ? (int32_t)p : -1;
+    }
+    __syncthreads();
+    if (tid < rows && s_place[tid] >= 0) a.owner[s_place[tid]] = -1;
+    for (int g0 = tid / LPG; g0 < groups;) {
+#pragma unroll
+        for (int u = 0; u < KV8_FLY; ++u) {
+            const uint32_t m = lanes_max<LPG>(largest8(0, x[u]));
+            const int32_t place = s_place[row[u]];
+            if (g0 + u * STEP >= groups || place < 0) continue;
+            float f[8];
+            values8(x[u], f);
+            const Quant8 z(m);
+            const int64_t at = (int64_t)place * a.heads + head[u];
+            if (has) *reinterpret_cast<q8_u32x2*>((vals[u] ? a.v8 : a.k8) + at * a.dim + 8 * l) = pack8(z, f);
+            if (l == 0) (vals[u] ? a.vs : a.ks)[at] = z.scale;
+        }
+        g0 += KV8_FLY * STEP;
+        if (g0 < groups) fetch(g0);
+    }
 }
 
 template <typename T, int LPG>
@@ -110,18 +153,15 @@ static int fill(void* p, size_t bytes, uint32_t value, hipStream_t st) {
 
 template <typename T, int LPG>
 static int kv8_write_as(const Kv8Args& a, hipStream_t st) {
-    const dim3 grid((unsigned)cdiv(a.rows * a.heads * LPG, 256), 2);
-    const unsigned per_row = (unsigned)cdiv(a.rows, 256);
     if (a.rows <= KV8_LOOK) {
-        kv8_write_kernel<T, LPG, false><<<grid, 256, 0, st>>>(a);
+        kv8_write_kernel<T, LPG><<<dim3((unsigned)cdiv(a.rows * a.heads * LPG, 256), 2), 256, 0, st>>>(a);
         return check_launch("kv8_write_kernel");
     }
-    kv8_claim_kernel<<<per_row, 256, 0, st>>>(a);
+    kv8_claim_kernel<<<(unsigned)cdiv(a.rows, 256), 256, 0, st>>>(a);
     PS_TRY(check_launch("kv8_claim_kernel"));
-    kv8_write_kernel<T, LPG, true><<<grid, 256, 0, st>>>(a);
-    PS_TRY(check_launch("kv8_write_kernel"));
-    kv8_release_kernel<<<per_row, 256, 0, st>>>(a);
-    return check_launch("kv8_release_kernel");
+    const int32_t per = std::max(1, std::min(KV8_PER, KV8_FLY * 256 / (2 * a.heads * LPG)));    // rows of a block: its groups in one go
+    kv8_write_rows_kernel<T, LPG><<<(unsigned)cdiv(a.rows, per), 256, 0, st>>>(a, per);
+    return check_launch("kv8_write_rows_kernel");
 }
 template <typename T, int LPG>
 static int kv8_read_as(const Kv8Args& a, hipStream_t st) {

@@ -68,8 +68,8 @@ linear8_rows_kernel(Linear8Args a) {
     const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
     if (TPR < 256 && row >= a.rows) return;
     const T* x = (const T*)a.x + row * a.ldx;
-    constexpr int W = 8 * sizeof(T) / 16;                   // 16-byte words of a chunk
-    struct Chunk { u32x4 w[W]; };
+    typedef Raw8<T> Chunk;
+    constexpr int W = sizeof(T) / 2;                        // 16-byte words of a chunk
     auto get = [&](int c) -> Chunk {
         Chunk r;
         if (VEC) {
@@ -83,30 +83,15 @@ linear8_rows_kernel(Linear8Args a) {
         }
         return r;
     };
-    auto values = [](const Chunk& r, float (&v)[8]) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? r.w[0][i / 2] & 0xffff0000u : r.w[0][i / 2] << 16);
-            else v[i] = __uint_as_float(r.w[i / 4][i % 4]);
-        }
-    };
-    auto largest = [&](uint32_t m, const Chunk& r) {
-        float v[8];
-        values(r, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
-        return m;
-    };
     const int chunks = a.Kp / 8;
     Chunk held[CH];
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < CH; ++i) held[i] = get(t + i * TPR);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) m = largest(m, held[i]);
-    for (int c = t + CH * TPR; c < chunks; c += TPR) m = largest(m, get(c));
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, s));
+    for (int i = 0; i < CH; ++i) m = largest8(m, held[i]);
+    for (int c = t + CH * TPR; c < chunks; c += TPR) m = largest8(m, get(c));
+    m = lanes_max<64>(m);
     if (TPR == 256) {
         if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = m;
         __syncthreads();
@@ -117,7 +102,7 @@ linear8_rows_kernel(Linear8Args a) {
     int8_t* o = a.x8 + row * a.Kp;
     auto put = [&](int c, const Chunk& r) {
         float v[8];
-        values(r, v);
+        values8(r, v);
         *reinterpret_cast<q8_u32x2*>(o + 8 * c) = pack8(z, v);
     };
 #pragma unroll

@@ -42,7 +42,7 @@ __device__ __forceinline__ void store_row(T* p, const float (&o)[DV], float inv)
 
 // DP: the head's values, rounded up to 64 or 128.  DX: sixteenths of a head that are computed.  Packed fp32 heads, which the matrix
 // instructions bound (4096 tokens, 2 x 4 heads of 128: 390 us, 88 of the 154 TFLOP/s of a large product), have D / 16: with heads of 80
-// filled up to 128 they took 388 us, so 264.  The others are bound by what they read and have DP / 16.
+// filled up to 128 they took 388 us, so 264.  Elsewhere DP / 16.
 template <typename T, int DP, int SRC, int DX>
 __global__ void __launch_bounds__(256, 2)
 prompt_few_kernel(PromptArgs a) {

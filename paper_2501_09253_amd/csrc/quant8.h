@@ -22,12 +22,16 @@ struct Quant8 {
         const float a = __uint_as_float(amax_bits);
         mul = a < 0x1p-60f ? 0x1p64f : 1.f;
         amax = a * mul;
-        scale = fminf(a / 127.f, 0x1.0204060000000p+121f);         // 127 times the scale of the largest number rounds to infinity, one step below it does not
-        inv = a > 0.f ? 127.f / amax : 0.f;
+        // a / 127, correctly rounded: the quotient by the rounded reciprocal and one correction from its exact rest (Markstein 1990; the same
+        // as the division for all 2^23 mantissas at the ends of the exponents taken here), a third of a division's instructions
+        const float by = 1.f / 127.f, q = a * by;
+        scale = a < 0x1p-100f ? a / 127.f : fmaf(fmaf(-127.f, q, a), by, q);
+        scale = fminf(scale, 0x1.0204060000000p+121f);             // 127 times the scale of the largest number rounds to infinity, one step below it does not
+        inv = a > 0.f ? __builtin_amdgcn_rcpf(amax * 0x1p-7f) * (127.f / 128.f) : 0.f;     // to 1.5 steps; the argument keeps off the subnormal results
         if (amax_bits >= 0x7f800000u) { scale = __uint_as_float(0x7fc00000u); mul = 0.f; inv = 0.f; amax = 1.f; }
     }
     __device__ __forceinline__ int operator()(float x) const {
-        const float y = x * mul, t = y * inv;       // |error of t| < 127 * 2^-22.9 < 2^-15
+        const float y = x * mul, t = y * inv;       // |error of t| < 127 * (1.5 * 2^-23 + 2^-24) < 2^-15
         float r = rintf(t);
         if (fabsf(fabsf(t - r) - 0.5f) < 0x1p-14f) {
             const double k = floorf(fabsf(t)), twice = 254.0 * fabs((double)y), border = (2.0 * k + 1.0) * (double)amax;  // exact: 32 bits each
@@ -66,6 +70,49 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
+// Eight values as they lie in memory, their largest magnitude as a bit pattern (bf16: two at a time, whole numbers of 16 bits), the values
+template <typename T> struct Raw8 { u32x4 w[sizeof(T) / 2]; };
+template <typename T>
+__device__ __forceinline__ void load_raw(const T* p, Raw8<T>& r) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = *reinterpret_cast<const u32x4*>(p + i * (16 / sizeof(T)));
+}
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+__device__ __forceinline__ uint32_t largest8(uint32_t m, const Raw8<uint16_t>& r) {
+    u16x2 p = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p = __builtin_elementwise_max(p, __builtin_bit_cast(u16x2, r.w[0][i] & 0x7fff7fffu));
+    return max(m, (uint32_t)max(p[0], p[1]) << 16);
+}
+__device__ __forceinline__ uint32_t largest8(uint32_t m, const Raw8<float>& r) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, r.w[i / 4][i % 4] & 0x7fffffffu);
+    return m;
+}
+template <typename T>
+__device__ __forceinline__ void values8(const Raw8<T>& r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? r.w[0][i / 2] & 0xffff0000u : r.w[0][i / 2] << 16);
+        else v[i] = __uint_as_float(r.w[i / 4][i % 4]);
+    }
+}
+// The largest of L neighbouring lanes (8, 16 or 64) in all of them: within 16 lanes by operands that come from other lanes
+template <int L>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
+#define PS_LANE(ctrl) m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, ctrl, 0xf, 0xf, true))
+    PS_LANE(0xb1);                              // lane ^ 1
+    PS_LANE(0x4e);                              // lane ^ 2
+    PS_LANE(0x141);                             // the other four of eight
+    if (L >= 16) PS_LANE(0x140);                // the other eight of sixteen
+#undef PS_LANE
+    if (L == 64) {
+        m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+        m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+    }
+    return m;
+}
+
 // Eight whole numbers as bytes.  t + 1.5 * 2^23 is rounded to a whole number, whose low byte is the two's complement form; only where
 // one of the eight is next to a border (or the group is one of tiny values) does the exact form above decide.
 __device__ __forceinline__ q8_u32x2 pack8(const Quant8& z, const float (&v)[8]) {
@@ -74,9 +121,9 @@ __device__ __forceinline__ q8_u32x2 pack8(const Quant8& z, const float (&v)[8]) 
     float far = 0.f;                                            // largest distance to the whole number
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float t = v[i] * z.inv, r = t + MAGIC;
+        const float r = fmaf(v[i], z.inv, MAGIC);
         s[i] = __float_as_uint(r);
-        far = fmaxf(far, fabsf(t - (r - MAGIC)));
+        far = fmaxf(far, fabsf(fmaf(v[i], z.inv, MAGIC - r)));
     }
     if (far > 0.5f - 0x1p-14f || z.mul > 1.f) {
 #pragma unroll
