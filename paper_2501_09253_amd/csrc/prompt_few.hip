@@ -369,6 +369,14 @@ prompt_few_kernel(PromptArgs a) {
         } else {
             const bf16x8 fp = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4 % NV], p[5 % NV]),
                                                                pack_bf16x2(p[6 % NV], p[7 % NV])});
+            // what the rounding to bf16 leaves of a probability (up to 2^-8 of it, as much as the output's own rounding) goes through the
+            // matrix cores as a second piece; of that up to 2^-8 is lost in turn
+            const u32x4 hw = __builtin_bit_cast(u32x4, fp);
+            u32x4 lw;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                lw[e] = pack_bf16x2(p[(2 * e) % NV] - __uint_as_float(hw[e] << 16), p[(2 * e + 1) % NV] - __uint_as_float(hw[e] & 0xffff0000u));
+            const bf16x8 fl = __builtin_bit_cast(bf16x8, lw);
             constexpr int CP = DP / (ST ? 16 : 8), RB = DP * (ST ? 1 : 2);      // chunks, bytes of a row
             bool odd = false;
 #pragma unroll
@@ -419,6 +427,7 @@ prompt_few_kernel(PromptArgs a) {
                     }
                 }
                 acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv, fp, acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv, fl, acc[t], 0, 0, 0);
             }
             __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
             __builtin_amdgcn_wave_barrier();                // the next step's rows come after these reads

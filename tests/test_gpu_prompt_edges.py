@@ -100,6 +100,23 @@ def test_two_graphs_and_two_streams_share_nothing():
         assert all(torch.equal(o, w) for o, w in zip(outs, want)) and all(torch.equal(b, want[1 - n % 2]) for b in beside)
 
 
+@pytest.mark.parametrize("heads,dim,dtype", [(40, 128, torch.bfloat16), (300, 16, torch.float32)])
+def test_rows_of_many_heads(heads, dim, dtype):
+    """More groups in a row than a block takes in one go, places taken twice and left out."""
+    rows, total = 200, 150
+    k, v = make(1, (rows, heads, dim), dtype), make(2, (rows, heads, dim), dtype)
+    places = torch.randint(-3, total, (rows,), generator=torch.Generator().manual_seed(3))
+    store = ps.KV8(total, heads, dim)
+    for _ in range(2):
+        store.write(k.cuda(), v.cuda(), places.cuda())
+        last = {p: i for i, p in enumerate(places.tolist()) if p >= 0}
+        at = sorted(last)
+        got = store.read(torch.tensor(at, device="cuda"), ps.F32)
+        same(got[0], po.held(k[[last[p] for p in at]]), torch.float32)
+        same(got[1], po.held(v[[last[p] for p in at]]), torch.float32)
+        k, v, places = v, k, places.flip(0)
+
+
 def test_thousands_of_short_sequences():
     """More sequences than a block looks at in one go, single tokens and short prompts, each over its own keys."""
     n, H, Hk, D, page = 5000, 4, 2, 64, 16
