@@ -49,16 +49,40 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs& a, int s) {
     }
     return q;
 }
-// Tiles of R rows over sequences of cu_q[s + 1] - cu_q[s] tokens of G rows each, without a table made by the host: sequence s has
-// the slots from floor(cu_q[s] G / R) + s on, at least as many as it has tiles.  false: no sequence's.
-__device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, int64_t slot, int& s, int& tile) {
-    // the last sequence whose slots begin at `slot` or in front of it, 64 places of the range looked at in one go (a walk over all of them
-    // took 66 ms of a call of 16,384 single tokens over 100 keys each); where the starts do not ascend, any one
+// The i-th tile of R rows, the last one first (under a causal mask it has the most keys), over sequences of cu_q[s + 1] - cu_q[s] tokens of G
+// rows each, without a table made by the host.  There are at most `slots` = prompt_slots of them; false: i has none.
+// Up to 64 sequences the tiles are numbered without gaps, so the blocks that have none are the last.  More sequences have the slots
+// from floor(cu_q[s] G / R) + s on, at least as many as they have tiles, found by a search.  (Gaps cost a round of blocks where the tiles just
+// fill the chip, as blocks are dealt out in a fixed order: 32 sequences of 8 tokens over 2000 keys, 2 tiles and a gap each, 62 us with gaps,
+// 45 without; 32 prompts of 77 with 12 heads 15 and 11; 32 of 512, where the gaps moved long tiles against each other, 240 and 249.)  (A walk over all of 16,384 sequences in every block takes 66 ms where the search takes 2.)
+__device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, int64_t slots, int64_t i, int& s, int& tile) {
     const int lane = threadIdx.x & 63;
+    if (a.n <= 64) {
+        int tiles = 0;
+        if (lane < a.n) {
+            const int64_t q0 = prompt_start(a.cu_q, lane, a.q_tokens), q1 = prompt_start(a.cu_q, lane + 1, a.q_tokens);
+            tiles = q1 > q0 ? (int)(((q1 - q0) * G + R - 1) / R) : 0;
+        }
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const int t = __builtin_amdgcn_readlane(upto, 63) - 1 - (int)i;
+        const uint64_t past = __ballot(upto > t);
+        if (t < 0 || past == 0) return false;
+        s = __ffsll((unsigned long long)past) - 1;
+        tile = t - (__builtin_amdgcn_readlane(upto, s) - __builtin_amdgcn_readlane(tiles, s));
+        return true;
+    }
+    // the last sequence whose slots begin at `slot` or in front of it, 64 places of the range looked at in one go; where the starts do
+    // not ascend, any one
+    const int64_t slot = slots - 1 - i;
     int lo = 0, len = a.n;
     for (;;) {
-        const int step = (len + 63) / 64, i = lo + lane * step;
-        const bool le = lane * step < len && prompt_start(a.cu_q, i, a.q_tokens) * G / R + i <= slot;
+        const int step = (len + 63) / 64, at = lo + lane * step;
+        const bool le = lane * step < len && prompt_start(a.cu_q, at, a.q_tokens) * G / R + at <= slot;
         const uint64_t past = ~__ballot(le);
         const int count = past ? __ffsll((unsigned long long)past) - 1 : 64;
         if (count == 0) return false;
@@ -67,8 +91,7 @@ __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, i
         if (step == 1) break;
     }
     s = __builtin_amdgcn_readfirstlane(lo);
-    const int64_t t = slot - (prompt_start(a.cu_q, s, a.q_tokens) * G / R + s);
-    tile = (int)t;
+    tile = (int)(slot - (prompt_start(a.cu_q, s, a.q_tokens) * G / R + s));
     return true;
 }
 inline int64_t prompt_slots(const PromptArgs& a, int G, int R) { return a.q_tokens * G / R + a.n; }

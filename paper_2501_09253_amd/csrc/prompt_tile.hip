@@ -49,11 +49,10 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int fr = lane & 31, fh = lane >> 5;
     const int hk = blockIdx.x % a.Hk, split = (blockIdx.x / a.Hk) % a.splits;
-    const int64_t slot = slots - 1 - blockIdx.x / (a.Hk * a.splits);
+    const int64_t slot = blockIdx.x / (a.Hk * a.splits);
     int s, tile;
-    // the last tiles first: they have the most keys.  Neighbouring blocks are the key/value heads, so an XCD (block mod 8) stays
-    // with few of them and finds their keys in its L2
-    if (!prompt_slot(a, a.G, BM, slot, s, tile)) return;
+    // neighbouring blocks are the key/value heads, so an XCD (block mod 8) stays with few of them and finds their keys in its L2
+    if (!prompt_slot(a, a.G, BM, slots, slot, s, tile)) return;
     const PromptSeq q = prompt_seq<SRC>(a, s);
     const int64_t rows = (int64_t)q.Lq * a.G, r0 = (int64_t)tile * BM;
     if (tile < 0 || r0 >= rows) return;
@@ -236,7 +235,7 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
                 }
             }
         }
-        bf16x8 fp[QT][2];
+        bf16x8 fp[QT][2], fl[ST ? QT : 1][2];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             float mx = sc_[t][0];
@@ -264,6 +263,20 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
             for (int k2 = 0; k2 < 2; ++k2)
                 fp[t][k2] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[8 * k2], p[8 * k2 + 1]), pack_bf16x2(p[8 * k2 + 2], p[8 * k2 + 3]),
                                                              pack_bf16x2(p[8 * k2 + 4], p[8 * k2 + 5]), pack_bf16x2(p[8 * k2 + 6], p[8 * k2 + 7])});
+            // Over the store, where a query sees many keys at much the same weight, what the rounding leaves goes along as a second piece: 77 ..
+            // 640 new tokens over up to 4095 keys 77 us instead of 68, error against 64 bits 0.0017 of the output's norm instead of 0.0024
+            // (the output's own rounding is 0.0017).  Packed causal prompts, in one piece, are at 0.0018 .. 0.0020.
+            if constexpr (ST) {
+#pragma unroll
+                for (int k2 = 0; k2 < 2; ++k2) {
+                    const u32x4 hw = __builtin_bit_cast(u32x4, fp[t][k2]);
+                    u32x4 lw;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        lw[e] = pack_bf16x2(p[8 * k2 + 2 * e] - __uint_as_float(hw[e] << 16), p[8 * k2 + 2 * e + 1] - __uint_as_float(hw[e] & 0xffff0000u));
+                    fl[t][k2] = __builtin_bit_cast(bf16x8, lw);
+                }
+            }
         }
 #pragma unroll
         for (int k2 = 0; k2 < 2; ++k2)
@@ -309,7 +322,10 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
                     }
                 }
 #pragma unroll
-                for (int t = 0; t < QT; ++t) acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, fp[t][k2], acc[t][d], 0, 0, 0);
+                for (int t = 0; t < QT; ++t) {
+                    acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, fp[t][k2], acc[t][d], 0, 0, 0);
+                    if constexpr (ST) acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, fl[t][k2], acc[t][d], 0, 0, 0);
+                }
             }
     };
 
