@@ -54,7 +54,8 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs& a, int s) {
 // Up to 64 sequences the tiles are numbered without gaps, so the blocks that have none are the last.  More sequences have the slots
 // from floor(cu_q[s] G / R) + s on, at least as many as they have tiles, found by a search.  (Gaps cost a round of blocks where the tiles just
 // fill the chip, as blocks are dealt out in a fixed order: 32 sequences of 8 tokens over 2000 keys, 2 tiles and a gap each, 62 us with gaps,
-// 45 without; 32 prompts of 77 with 12 heads 15 and 11; 32 of 512, where the gaps moved long tiles against each other, 240 and 249.)  (A walk over all of 16,384 sequences in every block takes 66 ms where the search takes 2.)
+// 45 without; 32 prompts of 77 with 12 heads 15 and 11; 32 of 512, where the gaps moved long tiles against each other, 240 and 249.  A walk
+// over all of 16,384 sequences in every block takes 66 ms where the search takes 2.)
 __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, int64_t slots, int64_t i, int& s, int& tile) {
     const int lane = threadIdx.x & 63;
     if (a.n <= 64) {
@@ -96,8 +97,8 @@ __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, i
 }
 inline int64_t prompt_slots(const PromptArgs& a, int G, int R) { return a.q_tokens * G / R + a.n; }
 
-// The work of the 16-row tiles, where they are cut, in units of `unit` keys of one tile: sequence s has tiles x Hk x U_s of them, the blocks take equal runs of
-// the numbered units, whatever the sequences' lengths are.  The first `lead` units of a tile stand for what it costs besides its keys (its
+// The work of the 16-row tiles, where they are cut, in units of `unit` keys of one tile: sequence s has tiles x Hk x U_s of them, the blocks
+// take equal runs of the numbered units, whatever the sequences' lengths are.  The first `lead` units of a tile stand for what it costs besides its keys (its
 // queries, the way to the first keys, the meeting of the wavefronts): without them a block of short sequences is the last to end.  Every
 // wavefront walks the sequences by itself, 64 at a time, one a lane (tiles are cut where there are fewer than 768).
 __device__ __forceinline__ int64_t uniform64(int64_t v) {      // the same in all lanes: into scalar registers

@@ -66,10 +66,11 @@ static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
     if (d->dtype == PSERVE_BF16 && max_q * a.G > 32 && (keys > 512 || tiles(16) >= 768)) {
         const bool wide = src == SRC_PACKED && max_q * a.G >= 256 && keys * a.G >= 1024 && tiles(256) * keys >= (1 << 18);
         a.rows = wide ? 256 : 128;
-        // Shares of the keys fill the chip, with one block a CU or two: 1 of 512 x 4096 in 256 / 512 / 768 blocks takes 32 / 31 / 37 us (12 heads
-        // of 64, packed), 44 / 54 / 65 (of 128); over the store, with probabilities in one piece, 71 / 53 / 51 and 88 / 65 / 82 (8 x 4 heads).  Where the longest sequence has
-        // more keys than the mean most blocks end early, so more are wanted: 8 of 32 x 100 .. 12800, heads of 128: 191 us in 256, 81 in 768.
-        // Joining the shares has its price: 4 of 20 .. 700 take 21 us in one share, 31 in two; 2 of 1024 x 1024 (12 heads of 64) 27 and 32.
+        // Shares of the keys fill the chip, with one block a CU or two: 1 of 512 x 4096 in 256 / 512 / 768 blocks takes 32 / 31 / 37 us (12
+        // heads of 64, packed), 44 / 54 / 65 (of 128); over the store, with probabilities in one piece, 71 / 53 / 51 and 88 / 65 / 82 (8 x 4
+        // heads).  Where the longest sequence has more keys than the mean most blocks end early, so more are wanted: 8 of 32 x 100 ..
+        // 12800, heads of 128: 191 us in 256, 81 in 768.  Joining the shares has its price: 4 of 20 .. 700 take 21 us in one share, 31 in
+        // two; 2 of 1024 x 1024 (12 heads of 64) 27 and 32.
         int64_t want = wide || (src == SRC_PACKED && a.D > 64) ? 256 : 512;
         const int64_t t = tiles(a.rows);
         if (src == SRC_PACKED) want = want * std::min(std::max(keys, mean), 3 * mean) / mean;

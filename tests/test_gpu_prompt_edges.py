@@ -4,7 +4,7 @@ import torch
 
 import paper_2501_09253_amd as ps
 import prompt_oracle as po
-from test_gpu_kv8 import same
+from test_gpu_kv8 import check_cached, paged, same
 from test_gpu_prompt_attention import check, ints, make, starts
 
 pytestmark = pytest.mark.gpu
@@ -98,6 +98,25 @@ def test_two_graphs_and_two_streams_share_nothing():
         graphs[1 - n % 2].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(o, w) for o, w in zip(outs, want)) and all(torch.equal(b, want[1 - n % 2]) for b in beside)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_more_sequences_than_lanes_in_wide_tiles(dim):
+    """Prompts and extended prompts, some without tokens or keys, in tiles of many rows whose keys are shared out; packed and stored."""
+    n, H, Hk, page = 70, 8, 1, 64
+    lq = [(5 * i) % 23 if i % 7 else 0 for i in range(n)]
+    lq[40] = 90
+    lk = [0 if i % 11 == 5 else lq[i] + (13 * i) % 50 for i in range(n)]
+    lk[40], lk[69] = 2300, 1900
+    q, k, v = make(1, (sum(lq), H, dim), torch.bfloat16), make(2, (sum(lk), Hk, dim), torch.bfloat16), make(3, (sum(lk), Hk, dim), torch.bfloat16)
+    table, places, total = paged(lk, page, 4)
+    store = ps.KV8(total, Hk, dim)
+    store.write(k.cuda(), v.cuda(), places)
+    cu = ints(starts(lq))
+    for causal in (True, False):
+        for hint in (0, 2300, 1 << 20):
+            check(ps.prompt_attention(q.cuda(), k.cuda(), v.cuda(), cu, ints(starts(lk)), causal=causal, max_q=90, max_k=hint), q, k, v, lq, lk, causal)
+            check_cached(store.attention(q.cuda(), cu, ints(lk), table, page, causal=causal, max_q=90, max_k=hint), q, k, v, lq, lk, causal)
 
 
 @pytest.mark.parametrize("heads,dim,dtype", [(40, 128, torch.bfloat16), (300, 16, torch.float32)])
