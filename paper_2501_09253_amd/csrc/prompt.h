@@ -49,32 +49,42 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs& a, int s) {
     }
     return q;
 }
-// The i-th tile of R rows, the last one first (under a causal mask it has the most keys), over sequences of cu_q[s + 1] - cu_q[s] tokens of G
-// rows each, without a table made by the host.  There are at most `slots` = prompt_slots of them; false: i has none.
-// Up to 64 sequences the tiles are numbered without gaps, so the blocks that have none are the last.  More sequences have the slots
-// from floor(cu_q[s] G / R) + s on, at least as many as they have tiles, found by a search.  (Gaps cost a round of blocks where the tiles just
-// fill the chip, as blocks are dealt out in a fixed order: 32 sequences of 8 tokens over 2000 keys, 2 tiles and a gap each, 62 us with gaps,
-// 45 without; 32 prompts of 77 with 12 heads 15 and 11; 32 of 512, where the gaps moved long tiles against each other, 240 and 249.  A walk
-// over all of 16,384 sequences in every block takes 66 ms where the search takes 2.)
+// The i-th tile of R rows in the order that the blocks take them, over sequences of cu_q[s + 1] - cu_q[s] tokens of G rows each, without a
+// table made by the host.  There are at most `slots` = prompt_slots of them; false: i has none.
+// Of a sequence the last tile comes first (under a causal mask it has the most keys).  Up to 64 sequences, one a lane, are numbered without
+// gaps, so the blocks that have no tile are the last; more have the slots from floor(cu_q[s] G / R) + s on, at least as many as they
+// have tiles, found by a search.  Where the keys are cut into shares the sequences with the most keys come first, so that no long tile is left
+// for the end (4 of 77 .. 640 tokens over 717 .. 4095 stored keys, the longest in front: 78 -> 71 us, heads of 128 110 -> 80); else the
+// last sequence does, as ordering them takes 2 us of every block's time with 32 sequences (32 prompts of 512 249 -> 265).
+// (Gaps cost a round of blocks where the tiles just fill the chip, as blocks are dealt out in a fixed order: 32 sequences of 8 tokens over 2000
+// keys, 2 tiles and a gap each, 62 us with gaps, 45 without; 32 prompts of 77 with 12 heads 15 and 11; 32 of 512, where the gaps moved
+// long tiles against each other, 240 and 249.  A walk over all of 16,384 sequences in every block takes 66 ms where the search takes 2.)
+template <int SRC>
 __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, int64_t slots, int64_t i, int& s, int& tile) {
     const int lane = threadIdx.x & 63;
     if (a.n <= 64) {
-        int tiles = 0;
-        if (lane < a.n) {
-            const int64_t q0 = prompt_start(a.cu_q, lane, a.q_tokens), q1 = prompt_start(a.cu_q, lane + 1, a.q_tokens);
-            tiles = q1 > q0 ? (int)(((q1 - q0) * G + R - 1) / R) : 0;
-        }
-        int upto = tiles;
+        PromptSeq q{0, 0, 0, 0};
+        if (lane < a.n) q = prompt_seq<SRC>(a, lane);
+        const int tiles = (int)(((int64_t)q.Lq * G + R - 1) / R);
+        int before = 0;                         // tiles of the sequences in front
+        if (a.splits > 1) {
+            for (int j = 0; j < a.n; ++j) {
+                const int kj = __builtin_amdgcn_readlane(q.Lk, j), tj = __builtin_amdgcn_readlane(tiles, j);
+                if (kj > q.Lk || (kj == q.Lk && j > lane)) before += tj;
+            }
+        } else {
+            int upto = tiles;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int o = __shfl_up(upto, d);
+                if (lane >= d) upto += o;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63) - upto;
         }
-        const int t = __builtin_amdgcn_readlane(upto, 63) - 1 - (int)i;
-        const uint64_t past = __ballot(upto > t);
-        if (t < 0 || past == 0) return false;
-        s = __ffsll((unsigned long long)past) - 1;
-        tile = t - (__builtin_amdgcn_readlane(upto, s) - __builtin_amdgcn_readlane(tiles, s));
+        const uint64_t at = __ballot(i >= before && i < (int64_t)before + tiles);
+        if (at == 0) return false;
+        s = __ffsll((unsigned long long)at) - 1;
+        tile = __builtin_amdgcn_readlane(before, s) + __builtin_amdgcn_readlane(tiles, s) - 1 - (int)i;
         return true;
     }
     // the last sequence whose slots begin at `slot` or in front of it, 64 places of the range looked at in one go; where the starts do
@@ -220,7 +230,7 @@ __device__ __forceinline__ uint32_t bf16_of_i8(uint32_t w, int h) {
 }
 
 int launch_prompt_tile(const PromptArgs& a, int rows, int src, hipStream_t st);
-int launch_prompt_join(const PromptArgs& a, hipStream_t st);
+int launch_prompt_join(const PromptArgs& a, int src, hipStream_t st);
 int launch_prompt_few(const PromptArgs& a, int dtype, int src, hipStream_t st);
 
 }  // namespace pserve

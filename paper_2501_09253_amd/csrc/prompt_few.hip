@@ -91,7 +91,7 @@ prompt_few_kernel(PromptArgs a) {
         const uint32_t item = (uint32_t)w, slot = item / (uint32_t)a.Hk;
         w += gridDim.x;
         hk = (int)(item - slot * (uint32_t)a.Hk);
-        if (!prompt_slot(a, a.G, 16, a.items / a.Hk, slot, s, tile)) continue;
+        if (!prompt_slot<SRC>(a, a.G, 16, a.items / a.Hk, slot, s, tile)) continue;
         tile = __builtin_amdgcn_readfirstlane(tile);
         q = prompt_seq<SRC>(a, s);
         q.q0 = uniform64(q.q0);
@@ -587,7 +587,7 @@ prompt_meet_kernel(PromptArgs a) {
 }
 
 // Joins the shares of a wide tile (bf16): 16 rows a block, 16 threads a row.
-template <int DP>
+template <int DP, int SRC>
 __global__ void __launch_bounds__(256)
 prompt_join_kernel(PromptArgs a, int64_t slots) {
     constexpr int DV = DP / 16;
@@ -595,7 +595,7 @@ prompt_join_kernel(PromptArgs a, int64_t slots) {
     const int64_t at = blockIdx.x / (R / 16), slot = at / a.Hk;
     const int hk = (int)(at % a.Hk);
     int s, tile;
-    if (!prompt_slot(a, a.G, R, slots, slot, s, tile)) return;
+    if (!prompt_slot<SRC>(a, a.G, R, slots, slot, s, tile)) return;
     const int64_t q0 = prompt_start(a.cu_q, s, a.q_tokens), rows = (prompt_start(a.cu_q, s + 1, a.q_tokens) - q0) * a.G;
     const int r = 16 * sub + (threadIdx.x >> 4), d0 = (threadIdx.x & 15) * DV;
     const int64_t row = (int64_t)tile * R + r;
@@ -624,11 +624,12 @@ prompt_join_kernel(PromptArgs a, int64_t slots) {
     store_row<DV>(op, o, ll == 0.f ? 0.f : 1.f / ll);
 }
 
-int launch_prompt_join(const PromptArgs& a, hipStream_t st) {
+int launch_prompt_join(const PromptArgs& a, int src, hipStream_t st) {
     const int64_t slots = prompt_slots(a, a.G, a.rows);
     const unsigned grid = (unsigned)(slots * a.Hk * (a.rows / 16));
-    if (a.D <= 64) prompt_join_kernel<64><<<grid, 256, 0, st>>>(a, slots);
-    else prompt_join_kernel<128><<<grid, 256, 0, st>>>(a, slots);
+    auto kernel = src == SRC_STORE ? a.D <= 64 ? prompt_join_kernel<64, SRC_STORE> : prompt_join_kernel<128, SRC_STORE>
+                                   : a.D <= 64 ? prompt_join_kernel<64, SRC_PACKED> : prompt_join_kernel<128, SRC_PACKED>;
+    kernel<<<grid, 256, 0, st>>>(a, slots);
     return check_launch("prompt_join_kernel");
 }
 

@@ -52,7 +52,7 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
     const int64_t slot = blockIdx.x / (a.Hk * a.splits);
     int s, tile;
     // neighbouring blocks are the key/value heads, so an XCD (block mod 8) stays with few of them and finds their keys in its L2
-    if (!prompt_slot(a, a.G, BM, slots, slot, s, tile)) return;
+    if (!prompt_slot<SRC>(a, a.G, BM, slots, slot, s, tile)) return;
     const PromptSeq q = prompt_seq<SRC>(a, s);
     const int64_t rows = (int64_t)q.Lq * a.G, r0 = (int64_t)tile * BM;
     if (tile < 0 || r0 >= rows) return;
@@ -597,7 +597,7 @@ static int launch_tile_as(const PromptArgs& a, hipStream_t st) {
     const int64_t slots = prompt_slots(a, a.G, Cfg::BM);
     prompt_tile_kernel<DP, QT, SRC><<<(unsigned)(slots * a.Hk * a.splits), 256, Cfg::LDS, st>>>(a, slots);
     PS_TRY(check_launch("prompt_tile_kernel"));
-    return a.splits > 1 ? launch_prompt_join(a, st) : PSERVE_OK;
+    return a.splits > 1 ? launch_prompt_join(a, SRC, st) : PSERVE_OK;
 }
 
 int launch_prompt_tile(const PromptArgs& a, int rows, int src, hipStream_t st) {
