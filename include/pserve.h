@@ -319,7 +319,8 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *
  * pserve_prompt_attention: attention over packed sequences of different lengths, causal, with grouped heads.
  *   q, o  DEVICE [q_tokens][heads][head_dim], k, v DEVICE [k_tokens][kv_heads][head_dim], of desc.dtype (fp32 statistics and
- *   accumulation; bf16: the probabilities are rounded to bf16 for the matrix cores).  Strides in elements between tokens and
+ *   accumulation; bf16: the matrix cores take a probability as one bf16 number, or as
+ *   two that add up to it where rows or tiles are few and over the store).  Strides in elements between tokens and
  *   between heads; a head's values are consecutive.  cu_q, cu_k DEVICE int32 [n + 1]: sequence s has the queries
  *   cu_q[s] .. cu_q[s + 1] - 1 and the keys cu_k[s] .. cu_k[s + 1] - 1 (ascending; what points outside q_tokens / k_tokens is
  *   cut off there).  Head h reads key/value head h / (heads / kv_heads).

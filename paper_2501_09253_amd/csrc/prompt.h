@@ -55,7 +55,7 @@ __device__ __forceinline__ PromptSeq prompt_seq(const PromptArgs& a, int s) {
 // gaps, so the blocks that have no tile are the last; more have the slots from floor(cu_q[s] G / R) + s on, at least as many as they
 // have tiles, found by a search.  Where the keys are cut into shares the sequences with the most keys come first, so that no long tile is left
 // for the end (4 of 77 .. 640 tokens over 717 .. 4095 stored keys, the longest in front: 78 -> 71 us, heads of 128 110 -> 80); else the
-// last sequence does, as ordering them takes 2 us of every block's time with 32 sequences (32 prompts of 512 249 -> 265).
+// last sequence does, as ordering them takes 2 us of every block's time with 32 sequences (32 prompts of 512: 249 us without, 265 with).
 // (Gaps cost a round of blocks where the tiles just fill the chip, as blocks are dealt out in a fixed order: 32 sequences of 8 tokens over 2000
 // keys, 2 tiles and a gap each, 62 us with gaps, 45 without; 32 prompts of 77 with 12 heads 15 and 11; 32 of 512, where the gaps moved
 // long tiles against each other, 240 and 249.  A walk over all of 16,384 sequences in every block takes 66 ms where the search takes 2.)
