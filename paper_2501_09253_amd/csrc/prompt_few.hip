@@ -45,7 +45,9 @@ __device__ __forceinline__ void store_row(T* p, const float (&o)[DV], float inv)
 // DP: the head's values, rounded up to 64 or 128.  DX: sixteenths of a head that are computed.  Packed fp32 heads, which the matrix
 // instructions bound (4096 tokens, 2 x 4 heads of 128: 390 us, 88 of the 154 TFLOP/s of a large product), have D / 16: with heads of 80
 // filled up to 128 they took 388 us, so 264.  Elsewhere DP / 16.
-template <typename T, int DP, int SRC, int DX>
+// PAD (packed bf16): D < DP.  What is read in place of a key's values past the head counts as 0: the queries are 0 there, but 0 times an
+// infinity is NaN.
+template <typename T, int DP, int SRC, int DX, bool PAD>
 __global__ void __launch_bounds__(256, 2)
 prompt_few_kernel(PromptArgs a) {
     constexpr bool F32 = sizeof(T) == 4, ST = SRC == SRC_STORE, EXACT = F32 && !ST;
@@ -275,7 +277,8 @@ prompt_few_kernel(PromptArgs a) {
                         const uint32_t w0 = w[2 * (i % 2)], w1 = w[2 * (i % 2) + 1];
                         fk = __builtin_bit_cast(bf16x8, u32x4{bf16_of_i8(w0, 0), bf16_of_i8(w0, 1), bf16_of_i8(w1, 0), bf16_of_i8(w1, 1)});
                     } else {
-                        fk = __builtin_bit_cast(bf16x8, f.k[t * (DP / 32) + i]);
+                        const u32x4 w = f.k[t * (DP / 32) + i];
+                        fk = __builtin_bit_cast(bf16x8, !PAD || 32 * i + 8 * g4 < a.D ? w : u32x4{0, 0, 0, 0});
                     }
                     sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fk, qb[i], sc, 0, 0, 0);
                 }
@@ -635,9 +638,9 @@ int launch_prompt_join(const PromptArgs& a, int src, hipStream_t st) {
     return check_launch("prompt_join_kernel");
 }
 
-template <typename T, int DP, int SRC, int DX>
+template <typename T, int DP, int SRC, int DX, bool PAD = false>
 static int launch_few_as(const PromptArgs& a, hipStream_t st) {
-    prompt_few_kernel<T, DP, SRC, DX><<<(unsigned)a.blocks, 256, 0, st>>>(a);
+    prompt_few_kernel<T, DP, SRC, DX, PAD><<<(unsigned)a.blocks, 256, 0, st>>>(a);
     PS_TRY(check_launch("prompt_few_kernel"));
     if (a.unit == 0) return PSERVE_OK;
     prompt_meet_kernel<T, DP, SRC><<<(unsigned)a.blocks, 512, 0, st>>>(a);
@@ -645,6 +648,8 @@ static int launch_few_as(const PromptArgs& a, hipStream_t st) {
 }
 template <typename T, int SRC>
 static int launch_few(const PromptArgs& a, hipStream_t st) {
+    if constexpr (SRC == SRC_PACKED)            // (bf16: packed fp32 has launch_few_f32)
+        if (a.D % 64) return a.D <= 64 ? launch_few_as<T, 64, SRC, 4, true>(a, st) : launch_few_as<T, 128, SRC, 8, true>(a, st);
     return a.D <= 64 ? launch_few_as<T, 64, SRC, 4>(a, st) : launch_few_as<T, 128, SRC, 8>(a, st);
 }
 static int launch_few_f32(const PromptArgs& a, hipStream_t st) {

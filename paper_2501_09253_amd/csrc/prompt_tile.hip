@@ -39,7 +39,9 @@ struct PromptTileCfg {
 template <int DP> __device__ __forceinline__ int pt_kswz(int r) { return DP == 128 ? r & 15 : (r >> 1) & 7; }
 template <int DP> __device__ __forceinline__ int pt_vswz(int r) { return DP == 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
 
-template <int DP, int QT, int SRC>
+// PAD (packed): heads of fewer than DP values.  Past the head the queries are 0 and another chunk of the key lies in its place; as 0 times
+// an infinity is NaN it counts as 0.  Only `half` sees to that: NaN in the pipelined loop sends the block through `half` anyway.
+template <int DP, int QT, int SRC, bool PAD>
 __global__ void __launch_bounds__(256, QT == 1 || DP == 64 ? 2 : 1)
 prompt_tile_kernel(PromptArgs a, int64_t slots) {
     using Cfg = PromptTileCfg<DP, QT, SRC>;
@@ -86,7 +88,7 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
         for (int ks = 0; ks < KS; ++ks) {
             const int d = 16 * ks + 8 * fh;
             const u32x4 w = *reinterpret_cast<const u32x4*>(qp + (d < a.D ? d : 0));
-            // past the head: 0, the keys' chunk there is another one again
+            // past the head: 0
             fq[t][ks] = __builtin_bit_cast(bf16x8, d < a.D ? w ^ flip : u32x4{0, 0, 0, 0});
         }
     }
@@ -201,7 +203,8 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
             for (int e = 0; e < 16; ++e) sc_[t][e] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            const bf16x8 fk = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(tk + 16 * ((2 * ks + fh) ^ pt_kswz<DP>(krow + 32 * H))));
+            const u32x4 w = *reinterpret_cast<const u32x4*>(tk + 16 * ((2 * ks + fh) ^ pt_kswz<DP>(krow + 32 * H)));
+            const bf16x8 fk = __builtin_bit_cast(bf16x8, !PAD || 16 * ks < a.D ? w : u32x4{0, 0, 0, 0});
 #pragma unroll
             for (int t = 0; t < QT; ++t) sc_[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fk, fq[t][ks], sc_[t], 0, 0, 0);
         }
@@ -592,19 +595,21 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
     }
 }
 
-template <int DP, int QT, int SRC>
+template <int DP, int QT, int SRC, bool PAD = false>
 static int launch_tile_as(const PromptArgs& a, hipStream_t st) {
     using Cfg = PromptTileCfg<DP, QT, SRC>;
-    PS_SET_LDS_ONCE((prompt_tile_kernel<DP, QT, SRC>), Cfg::LDS);
+    PS_SET_LDS_ONCE((prompt_tile_kernel<DP, QT, SRC, PAD>), Cfg::LDS);
     const int64_t slots = prompt_slots(a, a.G, Cfg::BM);
-    prompt_tile_kernel<DP, QT, SRC><<<(unsigned)(slots * a.Hk * a.splits), 256, Cfg::LDS, st>>>(a, slots);
+    prompt_tile_kernel<DP, QT, SRC, PAD><<<(unsigned)(slots * a.Hk * a.splits), 256, Cfg::LDS, st>>>(a, slots);
     PS_TRY(check_launch("prompt_tile_kernel"));
     return a.splits > 1 ? launch_prompt_join(a, SRC, st) : PSERVE_OK;
 }
 
 int launch_prompt_tile(const PromptArgs& a, int rows, int src, hipStream_t st) {
     if (src == SRC_STORE) return a.D <= 64 ? launch_tile_as<64, 1, SRC_STORE>(a, st) : launch_tile_as<128, 1, SRC_STORE>(a, st);
-    if (a.D <= 64) return rows == 128 ? launch_tile_as<64, 1, SRC_PACKED>(a, st) : launch_tile_as<64, 2, SRC_PACKED>(a, st);
+    if (a.D < 64) return rows == 128 ? launch_tile_as<64, 1, SRC_PACKED, true>(a, st) : launch_tile_as<64, 2, SRC_PACKED, true>(a, st);
+    if (a.D == 64) return rows == 128 ? launch_tile_as<64, 1, SRC_PACKED>(a, st) : launch_tile_as<64, 2, SRC_PACKED>(a, st);
+    if (a.D < 128) return rows == 128 ? launch_tile_as<128, 1, SRC_PACKED, true>(a, st) : launch_tile_as<128, 2, SRC_PACKED, true>(a, st);
     return rows == 128 ? launch_tile_as<128, 1, SRC_PACKED>(a, st) : launch_tile_as<128, 2, SRC_PACKED>(a, st);
 }
 

@@ -1,0 +1,78 @@
+"""Scores that are not finite in the prompt attention, whatever the head size and the kernel: +infinity and NaN make the row NaN, -infinity
+weighs nothing."""
+import pytest
+import torch
+
+import paper_2501_09253_amd as ps
+import prompt_exact as pe
+from test_gpu_prompt_attention import ints, make, starts
+
+pytestmark = pytest.mark.gpu
+
+# queries, keys, heads, key/value heads: tiles of 16 rows (whole, and their keys cut), of 128, of 128 in shares, of 256
+CALLS = {"16 rows": (5, 60, 4, 2), "16 rows, cut": (2, 1500, 6, 2), "128 rows": (77, 77, 160, 160), "128 rows, shares": (90, 1300, 4, 2),
+         "256 rows": (1100, 1100, 64, 8)}
+
+
+def run(q, k, v, scale=None, causal=True):
+    """(got, wanted, tolerance), one sequence."""
+    (Lq, _, D), Lk = q.shape, k.shape[0]
+    scale = D ** -0.5 if scale is None else scale
+    q, k, v = q.cuda(), k.cuda(), v.cuda()
+    got = ps.prompt_attention(q, k, v, ints([0, Lq]), ints([0, Lk]), causal=causal, scale=scale, max_q=Lq, max_k=Lk)
+    out, bound, _, size = pe.attention(q, k, v, scale, causal)
+    return got.double(), out, pe.tolerance(out, bound, size, q.dtype, D, Lk, pe.ONE_PIECE)
+
+
+def same(got, out, tol):
+    assert torch.equal(got.isnan(), out.isnan()), (got.isnan().sum().item(), out.isnan().sum().item())
+    err = (got - out).abs()
+    assert torch.all((err <= tol) | out.isnan()), (err / tol).nan_to_num().max()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("dim", range(16, 129, 16))
+def test_infinite_keys_at_every_head_size(dim, call, dtype):
+    """A key with an infinity in its first values, in the middle and in its last: rows whose query is negative there do not count it, rows
+    whose query is positive there are NaN."""
+    Lq, Lk, H, Hk = CALLS[call]
+    q, k, v = make(1, (Lq, H, dim), dtype), make(2, (Lk, Hk, dim), dtype), make(3, (Lk, Hk, dim), dtype)
+    for at, channel, sign in ((Lk - Lq, 0, 1.0), (Lk - Lq + Lq // 3, 7, -1.0), (Lk - Lq + Lq // 2, dim // 2, 1.0), (0, dim - 1, -1.0), (3, 3, 1.0)):
+        kk, qq = k.clone(), q.clone()
+        kk[at, :, channel] = sign * float("inf")
+        same(*run(qq, kk, v))                                           # queries of either sign
+        qq[:, :, channel] = -sign * (qq[:, :, channel].abs() + 0.125)
+        got, out, tol = run(qq, kk, v)                                  # all of them with a score of -infinity
+        assert not out.isnan().any()
+        same(got, out, tol)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dim", range(16, 129, 16))
+def test_rows_with_no_other_score_are_zero(dim, dtype):
+    """The first token sees one key, of score -infinity; a call in which all scores are -infinity."""
+    for Lq, Lk, H, Hk in CALLS.values():
+        q, k, v = make(1, (Lq, H, dim), dtype), make(2, (Lk, Hk, dim), dtype), make(3, (Lk, Hk, dim), dtype)
+        q[:, :, 2] = -1.0
+        kk = k.clone()
+        kk[:Lk - Lq + 1, :, 2] = float("inf")
+        got, out, tol = run(q, kk, v)
+        assert torch.all(got[0] == 0) and torch.all(out[0] == 0)
+        same(got, out, tol)
+        kk[:, :, 2] = float("inf")
+        assert torch.all(run(q, kk, v)[0] == 0)
+
+
+@pytest.mark.parametrize("dim", [32, 80, 128])
+def test_packed_neighbours_with_infinite_keys(dim):
+    """Sequences side by side: a key of one of them has no part in the others."""
+    lens, H, Hk = [70, 3, 130], 6, 2
+    q, k, v = (make(i, (sum(lens), h, dim), torch.bfloat16).cuda() for i, h in ((1, H), (2, Hk), (3, Hk)))
+    q[:, :, 1] = -1.0
+    k[::11, :, 1] = float("inf")
+    got, at = ps.prompt_attention(q, k, v, ints(starts(lens))).double(), starts(lens)
+    for s, L in enumerate(lens):
+        r = slice(at[s], at[s + 1])
+        out, bound, _, size = pe.attention(q[r], k[r], v[r], dim ** -0.5)
+        same(got[r], out, pe.tolerance(out, bound, size, q.dtype, dim, L, pe.ONE_PIECE))
