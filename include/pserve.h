@@ -329,7 +329,8 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   and behind the last sequence are left as they are.  A key or value that a query does not see has no part in its result,
  *   whatever it holds; one that it sees and that is not finite has the part that the formula gives it: a score of +infinity or
  *   NaN makes the row NaN, one of -infinity weighs nothing (a row with no other score gives zeros), a value makes its column of
- *   the row NaN or infinite.
+ *   the row NaN or infinite.  Scores are formed in fp32, q.k first, then times the scale: one that overflows there counts as infinite.
+ *   So are the sums of weights (at most 1) times values, before they are divided by the sum of the weights.
  *   max_q, max_k: the longest L_q and L_k as far as the caller knows (0: unknown).  Only the choice of kernel and of the
  *   number of shares of the keys depends on them, never which keys count.
  *   workspace DEVICE, at least pserve_prompt_attention_workspace bytes (0 where none is needed; it holds the partial results

@@ -250,7 +250,8 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
             if (__any(mx > m[t])) {
                 const float m2 = fmaxf(m[t], mx), f = m2 == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - m2);
                 m[t] = m2;
-                l[t] *= f;
+                // (a maximum that overflows only with its scale: the fma below would give finite - infinity, weights of 0, where the row is NaN)
+                l[t] = m2 == INFINITY ? __uint_as_float(0x7fc00000u) : l[t] * f;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -474,7 +475,7 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             l[t] = ls[t];
-            wild |= !(ls[t] < 0x1p60f);
+            wild |= !(ls[t] < 0x1p60f) || m[t] == INFINITY;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll

@@ -5,6 +5,8 @@ import torch
 
 import paper_2501_09253_amd as ps
 import prompt_exact as pe
+import prompt_oracle as po
+from test_gpu_kv8 import paged
 from test_gpu_prompt_attention import ints, make, starts
 
 pytestmark = pytest.mark.gpu
@@ -76,3 +78,29 @@ def test_packed_neighbours_with_infinite_keys(dim):
         r = slice(at[s], at[s + 1])
         out, bound, _, size = pe.attention(q[r], k[r], v[r], dim ** -0.5)
         same(got[r], out, pe.tolerance(out, bound, size, q.dtype, dim, L, pe.ONE_PIECE))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("dim", [64, 80, 128])
+def test_scores_that_overflow_with_their_scale(dim, call, dtype):
+    """q.k in the range of fp32, the scale times it not: the score counts as infinite, +: the row is NaN, -: the key weighs nothing."""
+    Lq, Lk, H, Hk = CALLS[call]
+    q, k, v = make(1, (Lq, H, dim), dtype, 0.2), make(2, (Lk, Hk, dim), dtype, 0.2), make(3, (Lk, Hk, dim), dtype)
+    q[:, :, 0], k[:, :, 0] = 2.0 ** 60, 0.0
+    for at in (3, Lk - Lq + Lq // 2):
+        for sign in (1.0, -1.0):
+            big, inf = k.clone(), k.clone()
+            big[at, :, 0], inf[at, :, 0] = sign * 2.0 ** 65, sign * float("inf")    # 2^125 times 8 log2(e): beyond 2^128
+            got = run(q, big, v, scale=8.0)[0]
+            _, out, tol = run(q, inf, v, scale=8.0)
+            assert out.isnan().any() == (sign > 0)
+            same(got, out, tol)
+            table, places, total = paged([Lk], 64, 4)
+            store = ps.KV8(total, Hk, dim)
+            store.write(big.cuda(), v.cuda(), places)
+            got = store.attention(q.cuda(), ints([0, Lq]), ints([Lk]), table, 64, scale=8.0, max_q=Lq, max_k=Lk).double()
+            inf = po.held(k)
+            inf[at], inf[at, :, 0] = 0.0, sign * float("inf")
+            out, bound, _, size = pe.attention(q.cuda(), inf.cuda(), po.held(v).cuda(), 8.0)
+            same(got, out, pe.tolerance(out, bound, size, dtype, dim, Lk, pe.ONE_PIECE, scales=4))
