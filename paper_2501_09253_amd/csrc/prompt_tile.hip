@@ -73,7 +73,8 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
 
     // ---- the lane's rows.  A negative scale is taken as that of the negated queries, so that a row's largest score stays its largest
     const u32x4 flip = a.scale2 < 0.f ? u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u} : u32x4{0, 0, 0, 0};
-    const float scale2 = fmaxf(fabsf(a.scale2), 0x1p-100f);     // (0: all weights alike; -infinity times 0 would be NaN)
+    // (0 is taken as the smallest number, which parts no two scores: a masked one is -infinity, and that times 0 would be NaN)
+    const float scale2 = fmaxf(fabsf(a.scale2), 0x1p-149f);
     int tok[QT], head[QT], lim[QT];
     bf16x8 fq[QT][KS];
 #pragma unroll

@@ -104,3 +104,13 @@ def test_scores_that_overflow_with_their_scale(dim, call, dtype):
             inf[at], inf[at, :, 0] = 0.0, sign * float("inf")
             out, bound, _, size = pe.attention(q.cuda(), inf.cuda(), po.held(v).cuda(), 8.0)
             same(got, out, pe.tolerance(out, bound, size, dtype, dim, Lk, pe.ONE_PIECE, scales=4))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -112, -2.0 ** -112])
+def test_small_scales_of_large_products(scale, call, dtype):
+    """q.k of about 2^114: all keys weigh the same where the scale is 0, and what the formula says where it is small."""
+    Lq, Lk, H, Hk = CALLS[call]
+    q, k, v = make(1, (Lq, H, 64), dtype), make(2, (Lk, Hk, 64), dtype), make(3, (Lk, Hk, 64), dtype)
+    same(*run(q * 2.0 ** 55, k * 2.0 ** 56, v, scale=scale))
