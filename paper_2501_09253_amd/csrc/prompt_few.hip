@@ -295,7 +295,7 @@ prompt_few_kernel(PromptArgs a) {
                 const f32x4 ks = *reinterpret_cast<const f32x4*>(&s_scale[wave][NV * g4 + j]);
                 const f32x4 w = *reinterpret_cast<const f32x4*>(&s_scale[wave][KT + NV * g4 + j]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { x[j + e] *= ks[e] * a.scale2; vs[j + e] = w[e]; }
+                for (int e = 0; e < 4; ++e) { x[j + e] = x[j + e] * ks[e] * a.scale2; vs[j + e] = w[e]; }    // (the scales' product may overflow)
             }
             __builtin_amdgcn_wave_barrier();
         } else {

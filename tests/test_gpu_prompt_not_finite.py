@@ -114,3 +114,21 @@ def test_small_scales_of_large_products(scale, call, dtype):
     Lq, Lk, H, Hk = CALLS[call]
     q, k, v = make(1, (Lq, H, 64), dtype), make(2, (Lk, Hk, 64), dtype), make(3, (Lk, Hk, 64), dtype)
     same(*run(q * 2.0 ** 55, k * 2.0 ** 56, v, scale=scale))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("call", list(CALLS))
+def test_large_keys_of_the_store_with_a_large_scale(call, dtype):
+    """A key's 8-bit scale times the scores' leaves fp32's range, the key's score does not: it is 0."""
+    Lq, Lk, H, Hk = CALLS[call]
+    q, k, v = make(1, (Lq, H, 64), dtype, 0.02), make(2, (Lk, Hk, 64), dtype, 0.02), make(3, (Lk, Hk, 64), dtype)
+    q[:, :, 0] = 0.0
+    k[Lk - Lq:, :, 0] = 2.0 ** 127
+    table, places, total = paged([Lk], 64, 4)
+    store = ps.KV8(total, Hk, 64)
+    store.write(k.cuda(), v.cuda(), places)
+    got = store.attention(q.cuda(), ints([0, Lq]), ints([Lk]), table, 64, scale=1000.0, max_q=Lq, max_k=Lk).double()
+    kk = po.held(k)
+    kk[:, :, 0] = 0.0
+    out, bound, _, size = pe.attention(q.cuda(), kk.cuda(), po.held(v).cuda(), 1000.0)
+    same(got, out, pe.tolerance(out, bound, size, dtype, 64, Lk, pe.ONE_PIECE, scales=4))
