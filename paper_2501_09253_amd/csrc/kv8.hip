@@ -137,6 +137,21 @@ kv8_read_kernel(Kv8Args a) {
         const float s = (vals ? a.vs : a.ks)[at];
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * s;
+        if constexpr (sizeof(T) == 2) {
+            // The product has up to 31 bits.  Where fp32 puts it on the middle of two bf16 numbers (one in 2^16) its rest says which is the nearer one
+            u16x2 low = {0xffff, 0xffff};                               // the low halves, the top bit turned over: 0 in the middle
+#pragma unroll
+            for (int i = 0; i < 8; i += 2)
+                low = __builtin_elementwise_min(low, __builtin_bit_cast(u16x2, __builtin_amdgcn_perm(__float_as_uint(x[i + 1]), __float_as_uint(x[i]), 0x05040100) ^ 0x80008000u));
+            if (low[0] == 0 || low[1] == 0) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float rest = fmaf((float)(int8_t)(w[i / 4] >> (8 * (i % 4))), s, -x[i]);      // exact: all are multiples of 2^-149
+                    const uint32_t u = __float_as_uint(x[i]), to = (rest > 0.f) == (x[i] > 0.f) ? u + 1 : u - 1;
+                    if ((uint16_t)u == 0x8000 && fabsf(rest) > 0.f) x[i] = __uint_as_float(to);
+                }
+            }
+        }
     }
     store8((vals ? (T*)a.vo : (T*)a.ko) + g * a.dim + 8 * l, x);
 }
