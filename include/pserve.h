@@ -350,8 +350,8 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   rounded once to dtype; zeros where the place is out of range.
  * pserve_kv8_attention: pserve_prompt_attention with keys and values in the store.  Key j of sequence s is token j % page of
  *   page table[s][j / page], i.e. place table[s][j / page] * page + j % page; table DEVICE int32 [n][max_pages], key_len DEVICE
- *   int32 [n] (cut to max_pages * page), page a power of two.  Keys on pages outside the store count as not there.  desc's
- *   kv_heads and head_dim are the store's; its k / v fields (k_tokens, strides) are not read.
+ *   int32 [n] (cut to max_pages * page), page a power of two.  Keys whose place is outside the store count as not there (a store's
+ *   last page may be filled in part).  desc's kv_heads and head_dim are the store's; its k / v fields (k_tokens, strides) are not read.
  * Errors: EINVAL, also for a store of another device than the current one and for 2^28 groups (rows x kv_heads) and more in one
  * write or read; ENOMEM; EHIP.
  *

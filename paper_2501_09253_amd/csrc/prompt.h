@@ -20,7 +20,8 @@ struct PromptArgs {
     int32_t rows, splits;               // rows of a tile, shares of its keys (wide tiles)
     int32_t unit, lead, blocks;         // tiles of 16 rows: keys of a unit of work (0: tiles are not cut), units a tile costs besides, blocks
     int32_t items;                      // tiles that are not cut: slots of tiles times key/value heads
-    int32_t max_pages, page_shift, pages;
+    int32_t max_pages, page_shift;
+    uint32_t pages, places;             // SRC_STORE: of the store; the last page may be filled in part
     float scale2;                       // scale * log2(e)
 };
 enum { SRC_PACKED = 0, SRC_STORE = 1 };
@@ -104,6 +105,12 @@ __device__ __forceinline__ bool prompt_slot(const PromptArgs& a, int G, int R, i
     s = __builtin_amdgcn_readfirstlane(lo);
     tile = (int)(slot - (prompt_start(a.cu_q, s, a.q_tokens) * G / R + s));
     return true;
+}
+// SRC_STORE: the place of a sequence's key, -1: none of the store's.  A page of the store starts below `places` <= 2^31 - 1, and has at most 2^30
+__device__ __forceinline__ int prompt_place(const PromptArgs& a, int s, int key) {
+    const uint32_t page = (uint32_t)a.table[(int64_t)s * a.max_pages + (key >> a.page_shift)];
+    const uint32_t place = page << a.page_shift | ((uint32_t)key & ((1u << a.page_shift) - 1));
+    return page < a.pages && place < a.places ? (int)place : -1;
 }
 inline int64_t prompt_slots(const PromptArgs& a, int G, int R) { return a.q_tokens * G / R + a.n; }
 

@@ -164,7 +164,8 @@ int pserve_kv8_attention(const pserve_kv8_t* store, const pserve_prompt_desc* de
     a.k8 = store->k; a.v8 = store->v; a.k_scale = store->k_scale; a.v_scale = store->v_scale;
     a.key_len = key_len; a.table = table; a.max_pages = max_pages;
     while ((1 << a.page_shift) < page) ++a.page_shift;
-    a.pages = (int32_t)(store->places >> a.page_shift);
+    a.places = (uint32_t)store->places;
+    a.pages = (uint32_t)cdiv(store->places, page);
     return run(desc, a, SRC_STORE, workspace, workspace_bytes, (hipStream_t)stream, who);
 }
 

@@ -146,15 +146,13 @@ prompt_few_kernel(PromptArgs a) {
         u32x4 k[NK], v[NVL];
         float vf[EXACT ? 4 : 1][DX];
         float scale;
-        uint32_t bad;                                       // keys whose page is no page of the store
+        uint32_t bad;                                       // keys whose place is none of the store's
     };
     const T* kb_ = ST ? nullptr : (const T*)a.K + q.k0 * a.k_row + (int64_t)hk * a.k_head;
     const T* vb_ = ST ? nullptr : (const T*)a.V + q.k0 * a.v_row + (int64_t)hk * a.v_head;
     // store: the place of key (kb + lane % KT), -1: none
-    auto place_of = [&](int kb) -> int {
-        const int key = min(kb + (lane & (KT - 1)), kend - 1);
-        const int page = a.table[(int64_t)s * a.max_pages + (key >> a.page_shift)];
-        return (uint32_t)page < (uint32_t)a.pages ? (int)(((uint32_t)page << a.page_shift) | ((uint32_t)key & ((1u << a.page_shift) - 1))) : -1;
+    auto place_of = [&](int kb) {
+        return prompt_place(a, s, min(kb + (lane & (KT - 1)), kend - 1));
     };
     auto load = [&](Step& f, int kb, int place) {
         auto key_at = [&](int j) { return min(kb + j, kend - 1); };

@@ -137,11 +137,7 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
     u32x4 rk[ST ? SL : 1], rv[ST ? SL : 1];
     float rs = 0.f;
     bool rbad = false;
-    auto place_of = [&](int key) -> int {
-        key = min(key, kend - 1) + koff;
-        const int page = a.table[(int64_t)s * a.max_pages + (key >> a.page_shift)];
-        return (uint32_t)page < (uint32_t)a.pages ? (int)(((uint32_t)page << a.page_shift) | ((uint32_t)key & ((1u << a.page_shift) - 1))) : -1;
-    };
+    auto place_of = [&](int key) { return prompt_place(a, s, min(key, kend - 1) + koff); };
     int pl[ST ? SL : 1], pls = 0;                               // places of the tile to be fetched next
     auto places = [&](int t) {
 #pragma unroll

@@ -3,8 +3,9 @@ import pytest
 import torch
 
 import paper_2501_09253_amd as ps
+import prompt_exact as pe
 import prompt_oracle as po
-from test_gpu_prompt_attention import make
+from test_gpu_prompt_attention import ints, make
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +34,27 @@ def test_values_are_rounded_once(heads, dim, dtype):
         assert (near != exact.float().bfloat16().double()).sum() >= (3 if dtype == torch.float32 else 0)
         assert torch.equal(half.cpu().double(), near)
         assert torch.equal(whole.cpu(), exact.float())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("places,page", [(100, 16), (1000, 64), (1000, 1024), (700, 512), (33, 32)])
+def test_places_of_a_partly_filled_last_page(places, page, new, dtype):
+    """A store whose places are no multiple of the page: keys on its last page count up to the last place, those behind it do not."""
+    H, Hk, D = 4, 2, 64
+    pages = -(-places // page)
+    k, v = make(2, (places, Hk, D), dtype), make(3, (places, Hk, D), dtype)
+    store = ps.KV8(places, Hk, D)
+    store.write(k.cuda(), v.cuda(), torch.arange(places, device="cuda"))
+    order = [pages - 1] + list(range(pages - 1))                       # the partly filled page first: its missing keys lie in the middle
+    key = [p * page + j for p in order for j in range(page)]
+    length = min(len(key), places + 5)
+    here = [j for j in key[:length] if j < places]
+    q = make(1, (new, H, D), dtype)
+    for hint in (0, length):
+        got = store.attention(q.cuda(), ints([0, new]), ints([length]), ints([order]), page, causal=False, max_q=new, max_k=hint).double()
+        out, bound, _, size = pe.attention(q, po.held(k[here]), po.held(v[here]), D ** -0.5, False)
+        tol = pe.tolerance(out, bound, size, dtype, D, len(here), pe.ONE_PIECE, scales=4)
+        assert torch.all((got.cpu() - out).abs() <= tol), ((got.cpu() - out).abs() / tol).max()
+    far = store.attention(q.cuda(), ints([0, new]), ints([page]), ints([[pages]]), page, causal=False)
+    assert torch.all(far == 0)                                          # a page behind the last
