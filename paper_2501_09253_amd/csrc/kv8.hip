@@ -75,7 +75,8 @@ template <typename T, int LPG>
 __global__ void __launch_bounds__(256)
 kv8_write_rows_kernel(Kv8Args a, int32_t per) {
     __shared__ int32_t s_place[KV8_PER];                    // -1: not written
-    const int64_t row0 = (int64_t)blockIdx.x * per;
+    const int64_t row0 = block_of_lines() * per;
+    if (row0 >= a.rows) return;
     const int rows = (int)min((int64_t)per, a.rows - row0), tid = threadIdx.x;
     const int l = tid % LPG, groups = rows * 2 * a.heads;   // (row, keys or values, head)
     const bool has = 8 * l < a.dim;
@@ -124,9 +125,9 @@ kv8_write_rows_kernel(Kv8Args a, int32_t per) {
 template <typename T, int LPG>
 __global__ void __launch_bounds__(256)
 kv8_read_kernel(Kv8Args a) {
-    const int64_t g = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPG;
+    const int64_t g = (block_of_lines() * 256 + threadIdx.x) / LPG;
     const int l = threadIdx.x % LPG;
-    const bool vals = blockIdx.y != 0;
+    const bool vals = blockIdx.z != 0;
     if (g >= a.rows * a.heads || 8 * l >= a.dim) return;
     const int64_t row = g / a.heads, p = a.places_of[row];
     const int head = (int)(g - row * a.heads);
@@ -175,12 +176,12 @@ static int kv8_write_as(const Kv8Args& a, hipStream_t st) {
     kv8_claim_kernel<<<(unsigned)cdiv(a.rows, 256), 256, 0, st>>>(a);
     PS_TRY(check_launch("kv8_claim_kernel"));
     const int32_t per = std::max(1, std::min(KV8_PER, KV8_FLY * 256 / (2 * a.heads * LPG)));    // rows of a block: its groups in one go
-    kv8_write_rows_kernel<T, LPG><<<(unsigned)cdiv(a.rows, per), 256, 0, st>>>(a, per);
+    kv8_write_rows_kernel<T, LPG><<<block_lines(cdiv(a.rows, per)), 256, 0, st>>>(a, per);
     return check_launch("kv8_write_rows_kernel");
 }
 template <typename T, int LPG>
 static int kv8_read_as(const Kv8Args& a, hipStream_t st) {
-    kv8_read_kernel<T, LPG><<<dim3((unsigned)cdiv(a.rows * a.heads * LPG, 256), 2), 256, 0, st>>>(a);
+    kv8_read_kernel<T, LPG><<<block_lines(cdiv(a.rows * a.heads * LPG, 256), 2), 256, 0, st>>>(a);
     return check_launch("kv8_read_kernel");
 }
 
@@ -193,7 +194,7 @@ static int check_device(const pserve_kv8_t* s, const char* who) {
     return PSERVE_OK;
 }
 
-// up to 16 threads a group, fewer than 2^32 in a launch: refused before the first launch, so that no claim is left behind
+// What no launch is made for is refused before the first one, so that no claim is left behind: 2^28 groups
 static int check_rows(const pserve_kv8_t* s, int64_t rows, const char* who) {
     PS_REQUIRE(rows >= 0 && rows < (1 << 28) && rows * s->heads < (1 << 28), "%s: %lld rows of %d heads", who, (long long)rows, s->heads);
     return PSERVE_OK;

@@ -15,6 +15,14 @@ typedef __attribute__((ext_vector_type(2))) uint32_t q8_u32x2;
 typedef __attribute__((ext_vector_type(16))) int i32x16;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 
+// A launch has fewer than 2^32 threads in a dimension, and whole blocks count: numbers of blocks that may come near that are laid out in lines
+// of equal length.  The blocks of the last line that are too many find no row of theirs.
+inline dim3 block_lines(int64_t blocks, unsigned z = 1) {
+    const int64_t lines = cdiv(blocks, 1 << 20);
+    return dim3((unsigned)cdiv(blocks, lines), (unsigned)lines, z);
+}
+__device__ __forceinline__ int64_t block_of_lines() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 struct Quant8 {
     float mul, amax, inv, scale;                    // x * mul: groups of tiny values are read 2^64 times as large (exact)
     // amax_bits: the largest |x| as its bit pattern (so infinities and NaN come out on top)
