@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(256)
 linear8_rows_kernel(Linear8Args a) {
     __shared__ uint32_t s_max[4];
     const int t = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const int64_t row = block_of_lines() * (256 / TPR) + threadIdx.x / TPR;
     if (TPR < 256 && row >= a.rows) return;
     const T* x = (const T*)a.x + row * a.ldx;
     typedef Raw8<T> Chunk;
@@ -116,9 +116,9 @@ linear8_rows_kernel(Linear8Args a) {
 template <typename T, bool VEC>
 static int launch_rows_as(const Linear8Args& a, hipStream_t st) {
     if (a.rows < 512 && a.Kp > 512) linear8_rows_kernel<T, 256, 4, VEC><<<(unsigned)a.rows, 256, 0, st>>>(a);
-    else if (a.Kp <= 1024) linear8_rows_kernel<T, 64, 2, VEC><<<(unsigned)cdiv(a.rows, 4), 256, 0, st>>>(a);
-    else if (a.Kp <= 2048) linear8_rows_kernel<T, 64, 4, VEC><<<(unsigned)cdiv(a.rows, 4), 256, 0, st>>>(a);
-    else linear8_rows_kernel<T, 64, 8, VEC><<<(unsigned)cdiv(a.rows, 4), 256, 0, st>>>(a);
+    else if (a.Kp <= 1024) linear8_rows_kernel<T, 64, 2, VEC><<<block_lines(cdiv(a.rows, 4)), 256, 0, st>>>(a);
+    else if (a.Kp <= 2048) linear8_rows_kernel<T, 64, 4, VEC><<<block_lines(cdiv(a.rows, 4)), 256, 0, st>>>(a);
+    else linear8_rows_kernel<T, 64, 8, VEC><<<block_lines(cdiv(a.rows, 4)), 256, 0, st>>>(a);
     return check_launch("linear8_rows_kernel");
 }
 template <typename T>
@@ -538,7 +538,7 @@ void pserve_linear8_free(pserve_linear8_t* op) { delete op; }
 
 int pserve_linear8_workspace(const pserve_linear8_t* op, int64_t rows, size_t* bytes) {
     PS_REQUIRE(op && bytes, "pserve_linear8_workspace: NULL argument");
-    PS_REQUIRE(rows >= 0 && rows < (1 << 26), "pserve_linear8: %lld rows (fewer than 2^26)", (long long)rows);     // 64 threads a row, 2^32 a launch
+    PS_REQUIRE(rows >= 0 && rows < (1 << 26), "pserve_linear8: %lld rows (fewer than 2^26)", (long long)rows);
     *bytes = x8_bytes(op, rows) + (size_t)rows * sizeof(float);
     return PSERVE_OK;
 }

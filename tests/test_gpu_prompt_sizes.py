@@ -1,10 +1,11 @@
-"""The largest calls that the 8-bit store takes: launches of 2^24 blocks and more, and where a second line of blocks begins."""
+"""The largest calls that the 8-bit store and the 8-bit layers take: launches of 2^24 blocks and more, and where a second line of blocks begins."""
 import pytest
 import torch
 
 import paper_2501_09253_amd as ps
 import prompt_oracle as po
 from test_gpu_kv8 import same
+from test_gpu_linear8 import check
 from test_gpu_prompt_attention import make
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +54,16 @@ def test_rows_read(rows):
         for part in t[:whole].view(-1, places + 3, 1, dim).split(20000):
             assert torch.all(part == x)
         assert torch.equal(t[whole:], x[:rows - whole])
+
+
+@pytest.mark.parametrize("rows", [(1 << 22) + 1, (1 << 26) - 1])
+def test_rows_of_a_layer(rows):
+    K, N = 8, 8
+    x, w = make(1, (4096, K), torch.bfloat16).cuda(), make(2, (K, N), torch.bfloat16)
+    many = x.repeat(rows // 4096 + 1, 1)[:rows]
+    layer = ps.Linear8(w.cuda(), None, ps.BF16)
+    few = layer.forward(x)
+    check(few, x.cpu(), w, None, None)
+    got = layer.forward(many)
+    whole = rows // 4096 * 4096
+    assert torch.all(got[:whole].view(-1, 4096, N) == few) and torch.equal(got[whole:], few[:rows - whole])
