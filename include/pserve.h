@@ -334,7 +334,8 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   max_q, max_k: the longest L_q and L_k as far as the caller knows (0: unknown).  Only the choice of kernel and of the
  *   number of shares of the keys depends on them, never which keys count.
  *   workspace DEVICE, at least pserve_prompt_attention_workspace bytes (0 where none is needed; it holds the partial results
- *   of the shares and may be used for something else after the call in stream order).  o must not overlap an input.
+ *   of the shares and may be used for something else after the call in stream order): enough for this call and for
+ *   pserve_kv8_attention with the same desc, with k_tokens = 0 for the latter alone.  o must not overlap an input.
  * Errors: EINVAL (NULL, n <= 0, heads % kv_heads, heads above 4096, head_dim not a multiple of 16 or above 128, unknown dtype,
  * negative sizes, more than 2^30 keys, pointers or strides that are no multiples of 16 bytes, strides of 2^24 elements and more
  * between tokens (the stride of a dimension of one is not looked at), a scale that times log2(e) is not finite in fp32, more

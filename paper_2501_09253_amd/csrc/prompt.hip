@@ -60,7 +60,8 @@ static PromptArgs prompt_args(const pserve_prompt_desc* d) {
 // to the matrix cores, there is no form of 256 rows.
 static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
     const int64_t max_q = d->max_q ? d->max_q : cdiv(d->q_tokens, d->n),
-                  mean = src == SRC_PACKED ? cdiv(std::min<int64_t>(std::max<int64_t>(d->k_tokens, 1), 1 << 30), d->n) : 1024, keys = d->max_k ? d->max_k : mean;
+                  mean = src == SRC_PACKED ? cdiv(std::min<int64_t>(std::max<int64_t>(d->k_tokens, 1), 1 << 30), d->n) : 1024,
+                  keys = src == SRC_PACKED && d->k_tokens == 0 ? 0 : d->max_k ? d->max_k : mean;       // (no packed keys: nothing to cut)
     auto tiles = [&](int rows) { return prompt_slots(a, a.G, rows) * a.Hk; };
     a.splits = 1;
     if (d->dtype == PSERVE_BF16 && max_q * a.G > 32 && (keys > 512 || tiles(16) >= 768)) {
