@@ -562,6 +562,11 @@ def _apart(who: str, out, *inputs):
             _need(a1 <= o0 or o1 <= a0, f"{who}: the output overlaps an input")
 
 
+def _number(scale):
+    """The value of a scale that may be an array of one: the descriptors below are kept by value."""
+    return None if scale is None else float(scale)
+
+
 @lru_cache(maxsize=1024)
 def _prompt_desc(n: int, heads: int, kv_heads: int, dim: int, dtype: int, causal: bool, scale: Optional[float], max_q: int, max_k: int,
                  q_tokens: int, k_tokens: int, q_stride, k_stride, v_stride, o_stride):
@@ -615,7 +620,7 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optio
     if sk[2] != 1 or sv[2] != 1:
         raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
     out = _prompt_out(who, q, out, k, v)
-    d, need = _prompt_desc(cu_q.shape[0] - 1, q.shape[1], k.shape[1], q.shape[2], BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), scale,
+    d, need = _prompt_desc(cu_q.shape[0] - 1, q.shape[1], k.shape[1], q.shape[2], BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), _number(scale),
                            int(max_q), int(max_k), q.shape[0], k.shape[0], q.stride(), sk, sv, out.stride())
     ws, nws, keep = _workspace(need, workspace, q.device, who)
     _check(lib().pserve_prompt_attention(d, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
@@ -687,7 +692,7 @@ class KV8:
         _ints(who, table, torch.int32, (n, table.shape[1]), "table")
         _need(q.dim() == 3 and q.shape[1] > 0 and q.shape[2] == self.head_dim, f"{who}: q must be [Tq, heads, {self.head_dim}]")
         out = _prompt_out(who, q, out)
-        d, need = _prompt_desc(n, q.shape[1], self.kv_heads, self.head_dim, BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), scale,
+        d, need = _prompt_desc(n, q.shape[1], self.kv_heads, self.head_dim, BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), _number(scale),
                                int(max_q), int(max_k), q.shape[0], 0, q.stride(), (0, 0), (0, 0), out.stride())
         ws, nws, keep = _workspace(need, workspace, q.device, who)
         _check(lib().pserve_kv8_attention(self._h, d, q.data_ptr(), cu_q.data_ptr(), key_len.data_ptr(), table.data_ptr(),
