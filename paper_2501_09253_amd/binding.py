@@ -522,6 +522,14 @@ def _need(cond, msg: str):
         raise PserveError(EINVAL, msg)
 
 
+def _whole(who: str, name: str, x, least: int = 0, most: int = 2 ** 31 - 1) -> int:
+    """A number that the library takes in 32 bits (or `most`): ctypes would pass on the low half of a larger one."""
+    x = int(x)
+    if not least <= x <= most:
+        raise PserveError(EINVAL, f"{who}: {name} {x}")
+    return x
+
+
 def _here(who: str, *tensors):
     """Tensors (None: absent) on the current device: the library's kernels run there."""
     import torch
@@ -621,7 +629,7 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optio
         raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
     out = _prompt_out(who, q, out, k, v)
     d, need = _prompt_desc(cu_q.shape[0] - 1, q.shape[1], k.shape[1], q.shape[2], BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), _number(scale),
-                           int(max_q), int(max_k), q.shape[0], k.shape[0], q.stride(), sk, sv, out.stride())
+                           _whole(who, "max_q", max_q), _whole(who, "max_k", max_k), q.shape[0], k.shape[0], q.stride(), sk, sv, out.stride())
     ws, nws, keep = _workspace(need, workspace, q.device, who)
     _check(lib().pserve_prompt_attention(d, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
                                          ws, nws, out.data_ptr(), _stream()))
@@ -637,9 +645,9 @@ class KV8:
     """pserve_kv8: keys and values of `places` tokens in 8 bits, a scale for each token and head."""
 
     def __init__(self, places: int, kv_heads: int, head_dim: int):
-        self._h = C.c_void_p()
-        _check(lib().pserve_kv8_create(int(places), int(kv_heads), int(head_dim), _stream(), C.byref(self._h)))
-        self.places, self.kv_heads, self.head_dim = int(places), int(kv_heads), int(head_dim)
+        self._h, who = C.c_void_p(), "KV8"
+        self.places, self.kv_heads, self.head_dim = (_whole(who, name, x, 1) for name, x in (("places", places), ("kv_heads", kv_heads), ("head_dim", head_dim)))
+        _check(lib().pserve_kv8_create(self.places, self.kv_heads, self.head_dim, _stream(), C.byref(self._h)))
 
     def write(self, k, v, places):
         """k and v [T, kv_heads, D] into places int64 [T] (on the device; negative or out of range: not written; the last row
@@ -690,10 +698,11 @@ class KV8:
         _ints(who, key_len, torch.int32, (n,), "key_len")
         _need(table.dim() == 2, f"{who}: table must be int32 [n, max_pages]")
         _ints(who, table, torch.int32, (n, table.shape[1]), "table")
+        page = _whole(who, "page", page, 1)
         _need(q.dim() == 3 and q.shape[1] > 0 and q.shape[2] == self.head_dim, f"{who}: q must be [Tq, heads, {self.head_dim}]")
         out = _prompt_out(who, q, out)
         d, need = _prompt_desc(n, q.shape[1], self.kv_heads, self.head_dim, BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), _number(scale),
-                               int(max_q), int(max_k), q.shape[0], 0, q.stride(), (0, 0), (0, 0), out.stride())
+                               _whole(who, "max_q", max_q), _whole(who, "max_k", max_k), q.shape[0], 0, q.stride(), (0, 0), (0, 0), out.stride())
         ws, nws, keep = _workspace(need, workspace, q.device, who)
         _check(lib().pserve_kv8_attention(self._h, d, q.data_ptr(), cu_q.data_ptr(), key_len.data_ptr(), table.data_ptr(),
                                           table.shape[1], page, ws, nws, out.data_ptr(), _stream()))
