@@ -319,9 +319,10 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *
  * pserve_prompt_attention: attention over packed sequences of different lengths, causal, with grouped heads.
  *   q, o  DEVICE [q_tokens][heads][head_dim], k, v DEVICE [k_tokens][kv_heads][head_dim], of desc.dtype (fp32 statistics and
- *   accumulation; bf16: the matrix cores take a probability as one bf16 number, or as
- *   two that add up to it where rows or tiles are few and over the store).  Strides in elements between tokens and
- *   between heads; a head's values are consecutive.  cu_q, cu_k DEVICE int32 [n + 1]: sequence s has the queries
+ *   accumulation; bf16: the matrix cores take a probability as two bf16 numbers that add up to it but for 2^-16 of it, so the error
+ *   is that of the result's rounding, 0.0017 of its norm.  Large packed calls, of 256 rows (L_q * heads / kv_heads) a sequence and more
+ *   whose products fill the chip, take one number, up to 2^-8 off: 0.0020 .. 0.0024 in all).  Strides in elements between tokens
+ *   and between heads; a head's values are consecutive.  cu_q, cu_k DEVICE int32 [n + 1]: sequence s has the queries
  *   cu_q[s] .. cu_q[s + 1] - 1 and the keys cu_k[s] .. cu_k[s + 1] - 1 (ascending; what points outside q_tokens / k_tokens is
  *   cut off there).  Head h reads key/value head h / (heads / kv_heads).
  *   The queries of a sequence of L_q queries and L_k keys stand at the END of its keys: with causal != 0 query i sees the keys

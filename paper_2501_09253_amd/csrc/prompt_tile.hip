@@ -45,7 +45,7 @@ template <int DP, int QT, int SRC, bool PAD>
 __global__ void __launch_bounds__(256, QT == 1 || DP == 64 ? 2 : 1)
 prompt_tile_kernel(PromptArgs a, int64_t slots) {
     using Cfg = PromptTileCfg<DP, QT, SRC>;
-    constexpr bool ST = SRC == SRC_STORE;
+    constexpr bool ST = SRC == SRC_STORE, TWO = ST || QT == 1;
     constexpr int BM = Cfg::BM, ROW = Cfg::ROW, TILE = Cfg::TILE, NS = Cfg::NS;
     constexpr int KS = DP / 16, DT = DP / 32, CP = DP / 8;      // contraction steps, output tiles, chunks of a row
     constexpr int LPO = PT_KB * CP / 256;                       // 16-byte loads a thread and operand
@@ -237,7 +237,7 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
                 }
             }
         }
-        bf16x8 fp[QT][2], fl[ST ? QT : 1][2];
+        bf16x8 fp[QT][2], fl[TWO ? QT : 1][2];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             float mx = sc_[t][0];
@@ -266,10 +266,11 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
             for (int k2 = 0; k2 < 2; ++k2)
                 fp[t][k2] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(p[8 * k2], p[8 * k2 + 1]), pack_bf16x2(p[8 * k2 + 2], p[8 * k2 + 3]),
                                                              pack_bf16x2(p[8 * k2 + 4], p[8 * k2 + 5]), pack_bf16x2(p[8 * k2 + 6], p[8 * k2 + 7])});
-            // Over the store, where a query sees many keys at much the same weight, what the rounding leaves goes along as a second piece: 77 ..
-            // 640 new tokens over up to 4095 keys 77 us instead of 68, error against 64 bits 0.0017 of the output's norm instead of 0.0024
-            // (the output's own rounding is 0.0017).  Packed causal prompts, in one piece, are at 0.0018 .. 0.0020.
-            if constexpr (ST) {
+            // What the rounding leaves goes along as a second piece, so that the result's own rounding is what is left of the error against 64
+            // bits (0.0017 of the norm; with one piece 0.0018 .. 0.0021 for causal prompts, up to 0.0024 where queries see all keys of some
+            // thousand at much the same weight).  us with one piece and two, packed: 22 prompts of 77, 12 heads of 64 9.5 and 9.9, 32 of 512 51
+            // and 56, 4 of 130 over 4000 keys, 8 / 2 heads of 128 54 and 57.  The tiles of 256 rows, which the matrix cores bound, keep one.
+            if constexpr (TWO) {
 #pragma unroll
                 for (int k2 = 0; k2 < 2; ++k2) {
                     const u32x4 hw = __builtin_bit_cast(u32x4, fp[t][k2]);
@@ -327,7 +328,7 @@ prompt_tile_kernel(PromptArgs a, int64_t slots) {
 #pragma unroll
                 for (int t = 0; t < QT; ++t) {
                     acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, fp[t][k2], acc[t][d], 0, 0, 0);
-                    if constexpr (ST) acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, fl[t][k2], acc[t][d], 0, 0, 0);
+                    if constexpr (TWO) acc[t][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fv, fl[t][k2], acc[t][d], 0, 0, 0);
                 }
             }
     };

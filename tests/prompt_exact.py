@@ -44,3 +44,11 @@ def tolerance(out, bound, size, dtype, D, Lk, piece, scales=0):
     the result is rounded once."""
     share = 2 * (2 * D + 4) * U * size + (4 * Lk + 16 + scales) * U + (piece if dtype == torch.bfloat16 else 0.0)
     return share * bound + HALF[dtype] * out.abs() + 1e-30
+
+
+def norm_bound(out, bound, spread, size, dtype, D, Lk, piece):
+    """Norm of the error of all elements, with the roundings of the keys' weights and of the sums' steps taken as independent (they
+    are thousands): what a weight loses adds up as the norm of the weighted values, the steps of a sum as the root of their number, both
+    within a factor of 1.7 (sqrt(3): half a step against its root mean square) and more of what is expected.  The result's own rounding counts in full."""
+    weights = 2 * (2 * D + 4) * U * size.max() + (piece if dtype == torch.bfloat16 else 0.0) + 16 * U
+    return HALF[dtype] * out.norm() + weights * spread.norm() + 4 * (Lk ** 0.5) * U * bound.norm()
