@@ -48,13 +48,17 @@ static PromptArgs prompt_args(const pserve_prompt_desc* d) {
 // Rows of a tile, and shares of its keys where the call has few tiles: a tile of 16 rows needs the least work for few rows, one of 256 reads
 // and turns its keys for the most rows but needs the whole register file.  us measured for 16 / 128 / 256 rows, the last two with their best
 // number of shares (bf16, packed; "n of queries x keys", 8 heads of keys with 4 of queries each; heads of 64, then of 128 values):
-//   1 of 256 x 256       9 / 11 / 15      13 / 15 / 24          2 of 1024 x 1024     65 / 34 / 29     125 / 51 / 47
-//   32 of 8 x 2048      29 / 45 / 57      53 / 72 / 71          1 of 512 x 4096      96 / 46 / 41     161 / 80 / 59
-//   8 of 77 x 77        14 /  9 / 12      22 / 11 / 19          32 of 512 x 512     326 / 100 / 84    687 / 242 / 226
-//   8 of 300 x 300      46 / 21 / 22      89 / 39 / 44          1 of 8192 x 8192   1173 / 394 / 278  2372 / 963 / 520
+//   1 of 256 x 256       9 / 11 / 15      12 / 15 / 23          2 of 1024 x 1024     64 / 37 / 28     124 / 51 / 45
+//   32 of 8 x 2048      32 / 50 / 46      61 / 72 / 76          1 of 512 x 4096      86 / 48 / 38     154 / 81 / 57
+//   8 of 77 x 77        14 /  8 / 12      22 / 11 / 18          32 of 512 x 512     352 / 115 / 88    730 / 271 / 236
+//   8 of 300 x 300      48 / 21 / 21      94 / 39 / 43          1 of 8192 x 8192   1184 / 486 / 277  2445 / 1038 / 516
 // and with 12 heads, each with its own keys:
-//   32 of 8 x 2048      33 / 57 / 70      53 / 111 / 126        32 of 512 x 512     135 / 51 / 61     263 / 109 / 164
-//   8 of 77 x 77         8 /  9 / 12      11 / 11 / 20          1 of 8192 x 8192    455 / 164 / 148   905 / 404 / 240
+//   32 of 8 x 2048      43 / 64 / 67      96 / 133 / 135        32 of 512 x 512     140 / 57 / 62     274 / 121 / 135
+//   8 of 77 x 77         8 /  8 / 12      10 / 11 / 20          1 of 8192 x 8192    453 / 201 / 152   930 / 435 / 234
+// and where 16 rows meet 128, n of queries x keys in 16 / 128 rows (heads of 64, then of 128):
+//   12 heads:    16 of 24 x 1200   28 / 33    41 / 47       16 of 33 x 1200   43 / 33    75 / 47       4 of 64 x 4000   33 / 30    51 / 47
+//                 8 of 24 x 600    18 / 19    25 / 24        8 of 40 x 600    22 / 19    32 / 26      32 of 40 x 700    32 / 30    59 / 60
+//   4 x 8 heads: 16 of 8 x 1200    23 / 26    33 / 39       16 of 9 x 1200    35 / 26    53 / 40       4 of 16 x 4000   26 / 23    39 / 35
 // So: 16 rows for sequences of up to 32 rows and where there are few tiles with few keys; 256 where they are filled, the mask's diagonal is
 // a small part of them (keys * G) and they keep the chip busy; else 128.  Over the 8-bit store, whose keys are turned into bf16 on their way
 // to the matrix cores, there is no form of 256 rows.
@@ -67,11 +71,12 @@ static void choose(const pserve_prompt_desc* d, PromptArgs& a, int src) {
     if (d->dtype == PSERVE_BF16 && max_q * a.G > 32 && (keys > 512 || tiles(16) >= 768)) {
         const bool wide = src == SRC_PACKED && max_q * a.G >= 256 && keys * a.G >= 1024 && tiles(256) * keys >= (1 << 18);
         a.rows = wide ? 256 : 128;
-        // Shares of the keys fill the chip, with one block a CU or two: 1 of 512 x 4096 in 256 / 512 / 768 blocks takes 32 / 31 / 37 us (12
-        // heads of 64, packed), 44 / 54 / 65 (of 128); over the store, with probabilities in one piece, 71 / 53 / 51 and 88 / 65 / 82 (8 x 4
-        // heads).  Where the longest sequence has more keys than the mean most blocks end early, so more are wanted: 8 of 32 x 100 ..
-        // 12800, heads of 128: 191 us in 256, 81 in 768.  Joining the shares has its price: 4 of 20 .. 700 take 21 us in one share, 31 in
-        // two; 2 of 1024 x 1024 (12 heads of 64) 27 and 32.
+        // Shares of the keys fill the chip, with one block a CU or two: 1 of 512 x 4096, 12 heads, in 240 / 480 / 720 blocks takes 34 / 32 / 36 us
+        // packed with heads of 64, 47 / 56 / 65 with heads of 128; over the store 49 / 40 / 45 and 59 / 50 / 58 (8 x 4 heads in 272 / 544 /
+        // 816: 84 / 62 / 75 and 99 / 80 / 96).  Where the longest sequence has more keys than the mean most blocks end early, so more are
+        // wanted: 8 of 32 x 100 .. 12800, 8 x 4 heads of 128: 201 us in 256, 85 in 768.  (Of the store only the longest is known: there the
+        // same call takes 145 us in 512 where 64 is possible in 2048.)  Joining the shares has its price: 4 of 20 .. 700 (8 x 4 heads of 64)
+        // take 21 us in one share, 32 in two; 2 of 1024 x 1024 (12 heads of 64) 28 and 32.
         int64_t want = wide || (src == SRC_PACKED && a.D > 64) ? 256 : 512;
         const int64_t t = tiles(a.rows);
         if (src == SRC_PACKED) want = want * std::min(std::max(keys, mean), 3 * mean) / mean;
