@@ -58,3 +58,27 @@ def test_places_of_a_partly_filled_last_page(places, page, new, dtype):
         assert torch.all((got.cpu() - out).abs() <= tol), ((got.cpu() - out).abs() / tol).max()
     far = store.attention(q.cuda(), ints([0, new]), ints([page]), ints([[pages]]), page, causal=False)
     assert torch.all(far == 0)                                          # a page behind the last
+
+
+def test_captured_writes_of_many_rows():
+    """Replayed with other rows and places, some twice and some outside, between eager writes of the same store."""
+    rows, places, heads, dim = 700, 400, 3, 64
+    k, v = make(1, (rows, heads, dim), torch.bfloat16).cuda(), make(2, (rows, heads, dim), torch.bfloat16).cuda()
+    at = torch.zeros(rows, dtype=torch.int64, device="cuda")
+    store, plain = ps.KV8(places, heads, dim), ps.KV8(places, heads, dim)
+    every = torch.arange(places, device="cuda")
+    store.write(k, v, at)
+    plain.write(k, v, at)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        store.write(k, v, at)
+    for i in range(6):
+        k.copy_(make(10 + i, k.shape, k.dtype))
+        v.copy_(make(20 + i, v.shape, v.dtype))
+        at.copy_(torch.randint(-20, places + 20, (rows,), generator=torch.Generator().manual_seed(i)))
+        graph.replay() if i % 3 else store.write(k, v, at)
+        last = {p: j for j, p in enumerate(at.tolist()) if 0 <= p < places}
+        rest = sorted(last.values())                                    # the rows that count, each place once
+        plain.write(k[rest], v[rest], at[rest])
+        assert all(torch.equal(a, b) for a, b in zip(store.read(every, ps.F32), plain.read(every, ps.F32)))
