@@ -7,7 +7,8 @@
 // qw is kept as [N rounded up to 256][K rounded up to 128], qx as [rows][K rounded up to 128], both filled up with zeros, so a step
 // of K is a row of 128 bytes in eight chunks, whatever K and N are; only the stores look at N.
 // Measured: 8192 x 8192 x 8192 524 us, 2.1 POPS, which the power limit holds (2.7 with zeros); 12,544 x 1536 x 6144 with a residual, bf16, 17 us
-// for the rows (58 MB) and 140 .. 144 for the product; 12 x 4096 x 4096 4.5 and 6.2 (17 MB).
+// for the rows (58 MB) and 140 .. 144 for the product; 12 x 4096 x 4096 4.6 and 6.5 (17 MB).  fp32 layers with a residual and an N that is
+// no multiple of 4 spill 87 registers in the largest tiles: 4096 x 1024 x 4099 135 us, x 4100 79.
 #include "quant8.h"
 
 using namespace pserve;

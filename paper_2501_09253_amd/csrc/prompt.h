@@ -16,7 +16,7 @@ struct PromptArgs {
     float* part;                        // partial results of the key shares
     int64_t q_tokens, k_tokens;
     int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;     // strides in elements
-    int32_t n, H, Hk, G, D, causal;
+    int32_t n, Hk, G, D, causal;
     int32_t rows, splits;               // rows of a tile, shares of its keys (wide tiles)
     int32_t unit, lead, blocks;         // tiles of 16 rows: keys of a unit of work (0: tiles are not cut), units a tile costs besides, blocks
     int32_t items;                      // tiles that are not cut: slots of tiles times key/value heads

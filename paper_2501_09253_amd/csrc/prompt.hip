@@ -39,7 +39,7 @@ static int check_tensor(const pserve_prompt_desc* d, const void* p, const int64_
 static PromptArgs prompt_args(const pserve_prompt_desc* d) {
     PromptArgs a{};
     a.q_tokens = d->q_tokens;
-    a.n = d->n; a.H = d->heads; a.Hk = d->kv_heads; a.G = d->heads / d->kv_heads; a.D = d->head_dim;
+    a.n = d->n; a.Hk = d->kv_heads; a.G = d->heads / d->kv_heads; a.D = d->head_dim;
     a.causal = d->causal != 0;
     a.scale2 = scale_log2(d);
     return a;

@@ -43,8 +43,8 @@ __device__ __forceinline__ void store_row(T* p, const float (&o)[DV], float inv)
 }
 
 // DP: the head's values, rounded up to 64 or 128.  DX: sixteenths of a head that are computed.  Packed fp32 heads, which the matrix
-// instructions bound (4096 tokens, 2 x 4 heads of 128: 390 us, 88 of the 154 TFLOP/s of a large product), have D / 16: with heads of 80
-// filled up to 128 they took 388 us, so 264.  Elsewhere DP / 16.
+// instructions bound (4096 tokens, 2 x 4 heads of 128: 370 us, 93 of the 154 TFLOP/s of a large product), have D / 16: heads of 80 take 255 us,
+// filled up to 128 they took what those do.  Elsewhere DP / 16.
 // PAD (packed bf16): D < DP.  What is read in place of a key's values past the head counts as 0: the queries are 0 there, but 0 times an
 // infinity is NaN.
 template <typename T, int DP, int SRC, int DX, bool PAD>

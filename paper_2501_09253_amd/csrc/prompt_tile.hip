@@ -7,8 +7,10 @@
 // scores of a 16-key step are consecutive keys: they are the B operand of O^T = V^T P^T as they lie.  V^T comes from LDS by transposed reads.
 // What bounds it: per 32 keys and 32 rows 4 DP / 32 matrix instructions of 32 clocks, 16 exponentials and ~40 vector instructions;
 // an LDS fragment feeds QT matrix instructions, so QT = 2 halves the LDS traffic (QT = 1 needs 128 bytes a clock at full rate).
-// Measured: one prompt of 16,384, 32 / 8 heads of 128, QT = 2: 1,900 us, 1,157 TFLOP/s where an 8192^3 product of a library reaches 1,212; 8192
-// tokens, 32 / 8 heads of 64 278 us (QT = 1 394).  Over the store QT = 1, 8192 tokens, 32 / 8 heads of 128: 840 us.
+// Measured: one prompt of 16,384, 32 / 8 heads of 128, QT = 2: 1,890 .. 2,000 us from card to card, 1,930 under the profiler: 1,140 TFLOP/s where an
+// 8192^3 product of a library reaches 1,212; 8192 tokens, 32 / 8 heads of 64 265 .. 277 us (QT = 1, with probabilities in two pieces, 486).
+// Over the store QT = 1, 8192 tokens, 32 / 8 heads of 128: 915 us.  QT = 2 spills, outside the pipelined loop's steps: 38 registers of a lane
+// with heads of 128 (156 bytes of scratch), 15 with heads of 64.
 #include "prompt.h"
 
 namespace pserve {
