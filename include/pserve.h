@@ -344,7 +344,8 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *
  * pserve_kv8: keys and values of `places` tokens in 8 bits.  A token's head is a group of head_dim values with one fp32 scale
  * amax / 127, each value a whole number 127 x / amax rounded to nearest (halves to even; exact); a group with an infinity or a
- * NaN reads back as NaN throughout.  head_dim + 4 bytes a group instead of 2 head_dim.  A new store holds zeros.
+ * NaN reads back as NaN throughout.  head_dim + 4 bytes a group instead of 2 head_dim.  A new store holds zeros; creating it synchronises
+ * `stream`.
  * pserve_kv8_write: k, v DEVICE rows of desc-like strides (elements between tokens, between heads); row i goes to places[i]
  *   (DEVICE int64 [rows]).  A row whose place is negative or not below `places` is not written; of several rows of one call
  *   with the same place the last one is.  Two writes that run at the same time must not share a place.
@@ -360,7 +361,7 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  * pserve_linear8: y = x W + b (+ residual) with x and W in 8-bit integers.  W [K][N] is quantised once, a scale for each
  * output channel; x [rows][K] in the call, a scale for each token (quantised as the store's groups are: a group is a column of W
  * resp. a row of x).  The products are summed in 32-bit integers, exactly; y = sum * (scale_x * scale_w) + b + residual in
- * fp32, rounded once.  A row of x (column of W) with an infinity or a NaN gives NaN.
+ * fp32, rounded once (so scales whose product leaves fp32's range do so here).  A row of x (column of W) with an infinity or a NaN gives NaN.
  * pserve_linear8_create: w DEVICE [K][N], b DEVICE [N] or NULL, of dtype; synchronises `stream`.  K + 4 bytes a column are
  *   kept (rounded up to 128 values, columns to 256); the caller's buffers are not referenced afterwards.
  * pserve_linear8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y),

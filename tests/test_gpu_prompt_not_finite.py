@@ -132,3 +132,22 @@ def test_large_keys_of_the_store_with_a_large_scale(call, dtype):
     kk[:, :, 0] = 0.0
     out, bound, _, size = pe.attention(q.cuda(), kk.cuda(), po.held(v).cuda(), 1000.0)
     same(got, out, pe.tolerance(out, bound, size, dtype, 64, Lk, pe.ONE_PIECE, scales=4))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("call", list(CALLS))
+@pytest.mark.parametrize("dim", [16, 64, 80, 128])
+def test_queries_that_are_not_finite(dim, call, dtype):
+    """NaN and infinities in some queries reach their own rows only: all keys of one sign against an infinite query give NaN or zeros."""
+    Lq, Lk, H, Hk = CALLS[call]
+    q, k, v = make(1, (Lq, H, dim), dtype), make(2, (Lk, Hk, dim), dtype), make(3, (Lk, Hk, dim), dtype)
+    k[:, :, 1] = k[:, :, 1].abs() + 0.125
+    bad = q.clone()
+    bad[Lq // 2, ::2, 1], bad[Lq // 2, 1::2, 1], bad[Lq - 1, :, dim - 1] = float("inf"), float("-inf"), float("nan")
+    finite = [i for i in range(Lq) if i not in (Lq // 2, Lq - 1)]
+    got, _, _ = run(bad, k, v)
+    _, out, tol = run(q, k, v)
+    assert torch.all((got - out).abs()[finite] <= tol[finite])
+    if Lq // 2 != Lq - 1:
+        assert got[Lq // 2, ::2].isnan().all() and torch.all(got[Lq // 2, 1::2] == 0)
+    assert got[Lq - 1].isnan().all()
