@@ -229,12 +229,12 @@ def prepare(case, seed):
 # ------------------------------------------------------------------------------------------------ the plain forms
 def _blocks(x):
     """The values that x [rows, K] stands for in 8 bits: blocks of 128 along K share a power of two, the smallest with which no
-    value of the block passes 448; each value is the nearest number of three fraction bits and exponents from -6."""
+    value of the block passes 448 (2^-100 .. 2^119); each value is the nearest number of three fraction bits and exponents from -6."""
     rows, K = x.shape
     pad = torch.zeros((rows, -K % 128), dtype=torch.float32, device=x.device)
     v = torch.cat([x, pad], 1).view(rows, -1, 128)
     fraction, exponent = torch.frexp(v.abs().amax(-1, keepdim=True))
-    shift = (exponent - 9 + (fraction > 0.875).int()).clamp(min=-127)       # 448 = 0.875 * 2^9
+    shift = (exponent - 9 + (fraction > 0.875).int()).clamp(-100, 119)      # 448 = 0.875 * 2^9
     v = torch.ldexp(v, -shift)
     step = torch.ldexp(torch.ones_like(v), torch.frexp(v).exponent.clamp(min=-5) - 4)
     return torch.ldexp(torch.round(v / step) * step, shift).view(rows, -1)[:, :K].contiguous()
@@ -352,9 +352,9 @@ def _held64(x):
     for c in range(0, x.shape[1], 128):
         part = x[:, c:c + 128]
         peak = part.abs().max(1, keepdim=True).values
-        e = torch.ceil(torch.log2(peak / 448)).clamp(-127, 200)
+        e = torch.ceil(torch.log2(peak / 448)).clamp(-100, 119)
         e = torch.where(peak > 448 * torch.exp2(e), e + 1, e)               # (the logarithm's rounding)
-        e = torch.where((peak <= 448 * torch.exp2(e - 1)) & (e > -127), e - 1, e)
+        e = torch.where((peak <= 448 * torch.exp2(e - 1)) & (e > -100), e - 1, e)
         v = part / torch.exp2(e)
         at = torch.searchsorted(border, v.abs().contiguous())               # a value on a border: the number below it
         up = (at < border.numel()) & (v.abs() == border[at.clamp(max=border.numel() - 1)]) & (at % 2 == 1)
