@@ -400,6 +400,102 @@ int  pserve_linear8_workspace(const pserve_linear8_t* op, int64_t rows, size_t* 
 int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t ldx, int64_t rows, const void* residual,
                             void* workspace, size_t workspace_bytes, void* y, void* stream);
 
+/* ---- the layer side: what a transformer layer over image, video and text tokens needs around its attention besides linear layers:
+ * positions of the queries and keys, the norms, gates and residuals between sub-layers, linear layers in 8-bit floating point.  (The
+ * paper's models have norms, gates and linear layers; their rotary and 8-bit forms are no operation of the paper.)  None of them allocates
+ * device memory after its create call; all can be captured into a graph.
+ *
+ * pserve_rotary: rotary positions with several axes (frame, row, column, say).  Pair p of a head's values, (a, b), becomes
+ *   (a cos t - b sin t, a sin t + b cos t), t = pos[token][axis[p]] * freq[p], the same for every head; values behind the pairs are copied.
+ *   PSERVE_PAIR_HALF: pair p are the values p and p + pairs; PSERVE_PAIR_NEXT: the values 2 p and 2 p + 1.
+ * pserve_rotary_create: axis HOST int32 [pairs] (0 .. axes - 1), freq HOST double [pairs], radians for a unit of position; synchronises `stream`.
+ * pserve_rotary_forward: pos DEVICE float [tokens][axes] (whole or not; what is not finite makes the pairs of its axis NaN); q DEVICE [tokens][heads]
+ *   [head_dim], k DEVICE [tokens][kv_heads][head_dim] (kv_heads = 0: none), any strides in elements between tokens and between heads, a head's
+ *   values consecutive; q_out may be q (with q's strides) and k_out k, nothing else may overlap.  Angles are formed in 64 bits (2^-52
+ *   of an angle off), sines and cosines are good to 2^-22, products and sums fp32, rounded once.
+ * pserve_plan_positions: pos DEVICE float [T][3] of a plan's tokens: (frame of the request, y, x) of a latent pixel; text token j of a request
+ *   has text[i] + j * text[3 + i], i = 0 .. 2.  frame DEVICE float [n], caller order (NULL: 0); text HOST float [6] (NULL: zeros).  Padding rows get 0.
+ * Errors: EINVAL (NULL, axes above 8, pairs above 256, a frequency that is not finite or beyond 1e9, head_dim below 2 pairs or above 512, heads above
+ * 4096, 2^31 tokens and more, negative strides or 2^31 and more, a buffer off its type's alignment, another device than the current one), ENOMEM, EHIP.
+ *
+ * pserve_gated_norm: the end of one sub-layer and the beginning of the next in one pass over the rows.
+ *   y = skip_scale * x + branch_scale * gate_s * (N_post(f) * post_gain + post_bias)
+ *   h = (N_pre(y) * pre_gain + pre_bias) * (1 + scale_s) + shift_s        (of y before its rounding)
+ *   N: PSERVE_NORM_NONE v, PSERVE_NORM_RMS v / sqrt(mean(v^2) + eps), PSERVE_NORM_LAYER (v - mean) / sqrt(variance + eps); statistics and everything
+ *   else in fp32 (sums of squares beyond its range count as infinite), y and h rounded once.
+ *   x, f, y, h DEVICE [rows][C], elements between rows; gains and biases DEVICE [C]; gate, scale, shift DEVICE [n][C], elements between requests; all of
+ *   desc.dtype.  Every pointer but x may be NULL: f, gains, biases, gate, scale and shift are left out of the formula then, y and h are not written
+ *   (one of them must be).  y or h may be x or f (with the same stride); nothing else may overlap.
+ *   cu_rows DEVICE int32 [n + 1], ascending: request s has the rows cu_rows[s] .. cu_rows[s + 1] - 1; NULL (n = 1 only): all rows.  which DEVICE
+ *   int32 [n] or NULL: request s has the vectors which[s] of gate, scale and shift instead of s.  Rows of no request, and those of one whose
+ *   which[s] is outside 0 .. n - 1, are left as they were.  A plan's CU_SEQLENS and PERM serve a plan's rows with vectors in caller order.
+ *   rows8: h goes into 8-bit rows (below) of `rows` rows of C values, rounded once, in the place of h.
+ * Errors: EINVAL (NULL, n <= 0, C above 16384, unknown dtype or norm, eps negative or not finite, scales not finite, 2^31 rows and more, row strides
+ * below C, buffers off their type's alignment, h and rows8 at once, parts of a formula whose f or h is not there), EHIP.
+ *
+ * pserve_f8_rows: rows of K values in 8-bit floating point (e4m3: three fraction bits, largest number 448), a power of two for each block of 128
+ *   consecutive values of a row, the smallest of 2^-100 .. 2^119 with which no value of the block passes 448 (values beyond 448 * 2^119 are cut off
+ *   there); a value is rounded once, to nearest, halves to even.  A block with an infinity or a NaN is NaN throughout.
+ *   rows8 DEVICE, 16-byte aligned, pserve_f8_rows_bytes bytes: numbers [rows][K rounded up to 128] (zeros behind K), then the exponents + 127 as bytes
+ *   [rows][K / 128 rounded up to 4].
+ * pserve_f8_rows_write: x DEVICE [rows][K] of dtype, ldx elements between rows.  pserve_f8_rows_read: the values held, rounded to dtype (exact).
+ * pserve_linear_f8: y = x W + b (+ residual) with rows of x and columns of W in that form.  W [K][N] is rounded once, a power of two for each output
+ *   channel and 128 values of K; x in the call or before it (forward_rows).  Products are exact and summed in fp32; bf16 layers drop, of eight products
+ *   of neighbouring K, what lies below 2^-13 of the largest (1e-4 of a result's size; its rounding takes 1.7e-3).  Then + b + residual, rounded once.
+ *   A row of x (column of W) with an infinity or a NaN gives NaN.
+ * pserve_linear_f8_create: w DEVICE [K][N], b DEVICE [N] or NULL, of dtype; synchronises `stream`; the caller's buffers are not referenced afterwards.
+ * pserve_linear_f8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y), y DEVICE [rows][N];
+ *   workspace DEVICE, 16-byte aligned, at least pserve_linear_f8_workspace bytes.  y must not overlap x.  pserve_linear_f8_forward_rows: the rows as
+ *   rows8, no workspace.
+ * Errors: EINVAL (NULL, sizes <= 0, K above 131072, N above 2^24, 2^26 rows and more, ldx < K, workspace too small, buffers off their alignment, another
+ * device than the current one), ENOMEM, EHIP. */
+#define PSERVE_PAIR_HALF 0
+#define PSERVE_PAIR_NEXT 1
+typedef struct pserve_rotary_s pserve_rotary_t;
+typedef struct {
+    int32_t heads, kv_heads;        /* query heads, key heads (0: no keys) */
+    int32_t head_dim, dtype;        /* PSERVE_F32 | PSERVE_BF16 */
+    int64_t tokens;
+    int64_t q_stride[2], k_stride[2], q_out_stride[2], k_out_stride[2];     /* elements between tokens, between heads */
+} pserve_rotary_desc;
+int  pserve_rotary_create(int32_t axes, int32_t pairs, const int32_t* axis, const double* freq, int layout, void* stream, pserve_rotary_t** out);
+void pserve_rotary_free(pserve_rotary_t* op);
+int  pserve_rotary_forward(const pserve_rotary_t* op, const pserve_rotary_desc* desc, const float* pos, const void* q, const void* k, void* q_out,
+                           void* k_out, void* stream);
+int  pserve_plan_positions(const pserve_plan_t* plan, const float* frame, const float* text, float* pos, void* stream);
+
+#define PSERVE_NORM_NONE  0
+#define PSERVE_NORM_RMS   1
+#define PSERVE_NORM_LAYER 2
+#define PSERVE_GATED_NORM_MAX_C 16384
+typedef struct {
+    int32_t C, dtype;               /* channels; PSERVE_F32 | PSERVE_BF16 */
+    int32_t n;                      /* requests */
+    int32_t post_norm, pre_norm;    /* PSERVE_NORM_* */
+    float   post_eps, pre_eps;
+    float   skip_scale, branch_scale;
+    int64_t rows;
+    int64_t x_stride, f_stride, y_stride, h_stride;         /* elements between rows */
+    int64_t gate_stride, scale_stride, shift_stride;        /* elements between requests */
+} pserve_gated_norm_desc;
+typedef struct {
+    const void *x, *f, *post_gain, *post_bias, *gate, *pre_gain, *pre_bias, *scale, *shift;
+    const int32_t *cu_rows, *which;
+    void *y, *h, *rows8;
+} pserve_gated_norm_buffers;
+int  pserve_gated_norm(const pserve_gated_norm_desc* desc, const pserve_gated_norm_buffers* buffers, void* stream);
+
+int  pserve_f8_rows_bytes(int64_t rows, int32_t K, size_t* bytes);
+int  pserve_f8_rows_write(const void* x, int64_t ldx, int64_t rows, int32_t K, int dtype, void* rows8, void* stream);
+int  pserve_f8_rows_read(const void* rows8, int64_t rows, int32_t K, int dtype, void* x, int64_t ldx, void* stream);
+typedef struct pserve_linear_f8_s pserve_linear_f8_t;
+int  pserve_linear_f8_create(int32_t K, int32_t N, int dtype, const void* w, const void* b, void* stream, pserve_linear_f8_t** out);
+void pserve_linear_f8_free(pserve_linear_f8_t* op);
+int  pserve_linear_f8_workspace(const pserve_linear_f8_t* op, int64_t rows, size_t* bytes);
+int  pserve_linear_f8_forward(const pserve_linear_f8_t* op, const void* x, int64_t ldx, int64_t rows, const void* residual, void* workspace,
+                              size_t workspace_bytes, void* y, void* stream);
+int  pserve_linear_f8_forward_rows(const pserve_linear_f8_t* op, const void* rows8, int64_t rows, const void* residual, void* y, void* stream);
+
 /* ---- host-side scheduler pieces (section "SLO-Aware Scheduler").  All pointers HOST; no GPU work; times in ms.
  *
  * pserve_task: a request as the scheduler sees it.  ddl = its SLO budget counted from arrival (DDL_i), standalone =

@@ -82,6 +82,23 @@ class _PromptDesc(C.Structure):
                 ("o_stride", C.c_int64 * 2)]
 
 
+class _RotaryDesc(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("tokens", C.c_int64),
+                ("q_stride", C.c_int64 * 2), ("k_stride", C.c_int64 * 2), ("q_out_stride", C.c_int64 * 2), ("k_out_stride", C.c_int64 * 2)]
+
+
+class _GatedNormDesc(C.Structure):
+    _fields_ = [("C", C.c_int32), ("dtype", C.c_int32), ("n", C.c_int32), ("post_norm", C.c_int32), ("pre_norm", C.c_int32),
+                ("post_eps", C.c_float), ("pre_eps", C.c_float), ("skip_scale", C.c_float), ("branch_scale", C.c_float), ("rows", C.c_int64),
+                ("x_stride", C.c_int64), ("f_stride", C.c_int64), ("y_stride", C.c_int64), ("h_stride", C.c_int64),
+                ("gate_stride", C.c_int64), ("scale_stride", C.c_int64), ("shift_stride", C.c_int64)]
+
+
+class _GatedNormBuffers(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("x", "f", "post_gain", "post_bias", "gate", "pre_gain", "pre_bias", "scale", "shift",
+                                                "cu_rows", "which", "y", "h", "rows8")]
+
+
 def library_path() -> str:
     return os.path.join(_HERE, "libpserve.so")
 
@@ -160,6 +177,21 @@ def lib() -> C.CDLL:
     L.pserve_linear8_free.restype = None
     L.pserve_linear8_workspace.argtypes = [vp, i64, C.POINTER(C.c_size_t)]
     L.pserve_linear8_forward.argtypes = [vp, vp, i64, i64, vp, vp, C.c_size_t, vp, vp]
+    L.pserve_rotary_create.argtypes = [i32, i32, C.POINTER(i32), C.POINTER(C.c_double), C.c_int, vp, C.POINTER(vp)]
+    L.pserve_rotary_free.argtypes = [vp]
+    L.pserve_rotary_free.restype = None
+    L.pserve_rotary_forward.argtypes = [vp, C.POINTER(_RotaryDesc), vp, vp, vp, vp, vp, vp]
+    L.pserve_plan_positions.argtypes = [vp, vp, C.POINTER(C.c_float), vp, vp]
+    L.pserve_gated_norm.argtypes = [C.POINTER(_GatedNormDesc), C.POINTER(_GatedNormBuffers), vp]
+    L.pserve_f8_rows_bytes.argtypes = [i64, i32, C.POINTER(C.c_size_t)]
+    L.pserve_f8_rows_write.argtypes = [vp, i64, i64, i32, C.c_int, vp, vp]
+    L.pserve_f8_rows_read.argtypes = [vp, i64, i32, C.c_int, vp, i64, vp]
+    L.pserve_linear_f8_create.argtypes = [i32, i32, C.c_int, vp, vp, vp, C.POINTER(vp)]
+    L.pserve_linear_f8_free.argtypes = [vp]
+    L.pserve_linear_f8_free.restype = None
+    L.pserve_linear_f8_workspace.argtypes = [vp, i64, C.POINTER(C.c_size_t)]
+    L.pserve_linear_f8_forward.argtypes = [vp, vp, i64, i64, vp, vp, C.c_size_t, vp, vp]
+    L.pserve_linear_f8_forward_rows.argtypes = [vp, vp, i64, vp, vp, vp]
     _lib = L
     return L
 
@@ -343,6 +375,22 @@ class Plan:
             out = torch.empty(self.P, dtype=torch.float32, device=a.device)
         dt = BF16 if a.dtype == torch.bfloat16 else F32
         _check(lib().pserve_patch_mse_static(self._h, a.data_ptr(), b.data_ptr(), a.shape[1], dt, out.data_ptr(), _stream()))
+        return out
+
+    def positions(self, frame=None, text=None, out=None):
+        """pserve_plan_positions: float32 [T, 3], (frame, y, x) of every token of the plan: frame float32 [n] (caller order, on the device) or None,
+        text six numbers, where the text tokens' positions start and how they step (None: zeros)."""
+        import torch
+        who = "Plan.positions"
+        _here(who, frame, out)
+        _need(frame is None or (frame.dtype == torch.float32 and tuple(frame.shape) == (self.n,) and frame.is_contiguous()), f"{who}: frame must be contiguous float32 [{self.n}]")
+        _need(text is None or len(text) == 6, f"{who}: text must be six numbers")
+        if out is None:
+            out = torch.empty((self.T, 3), dtype=torch.float32, device="cuda")
+        _need(out.dtype == torch.float32 and tuple(out.shape) == (self.T, 3) and out.is_contiguous(), f"{who}: out must be contiguous float32 [{self.T}, 3]")
+        _apart(who, out, frame)
+        _check(lib().pserve_plan_positions(self._h, None if frame is None else frame.data_ptr(), None if text is None else (C.c_float * 6)(*text),
+                                           out.data_ptr(), _stream()))
         return out
 
     def cache_sets(self, ids, old_plan: "Plan", old_ids):
@@ -773,6 +821,298 @@ class Linear8:
             self.close()
         except Exception:
             pass
+
+
+# ---- the layer side: rotary positions with several axes, norms before and after a sub-layer, 8-bit floating-point linear layers
+PAIR_HALF, PAIR_NEXT = 0, 1
+NORM = {None: 0, "rms": 1, "layer": 2}
+
+
+def rotary_ladder(pairs: Sequence[int], base: float = 10000.0, shared: bool = False):
+    """(axis, freq) of each pair, for Rotary: pairs[a] pairs for axis a.  Frequencies fall from 1 towards 1 / base over each axis' own pairs, or
+    (shared) once over all of them."""
+    axis = [a for a, n in enumerate(pairs) for _ in range(n)]
+    if shared:
+        return axis, [base ** (-i / len(axis)) for i in range(len(axis))]
+    return axis, [base ** (-i / n) for n in pairs for i in range(n)]
+
+
+def _dtype_code(who: str, t) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return BF16
+    if t.dtype == torch.float32:
+        return F32
+    raise PserveError(EINVAL, f"{who}: dtype {t.dtype} is neither bfloat16 nor float32")
+
+
+@lru_cache(maxsize=1024)
+def _rotary_desc(heads: int, kv_heads: int, dim: int, dtype: int, tokens: int, q, k, q_out, k_out):
+    d = _RotaryDesc(heads, kv_heads, dim, dtype, tokens)
+    d.q_stride[:], d.k_stride[:], d.q_out_stride[:], d.k_out_stride[:] = q[:2], k[:2], q_out[:2], k_out[:2]
+    return C.byref(d)
+
+
+class Rotary:
+    """pserve_rotary: pair p of a head's values is turned by pos[token][axis[p]] * freq[p] (radians for a unit of position).
+    layout "half": pair p are the values p and p + P of a head, P pairs; "next": 2 p and 2 p + 1; values behind the pairs are copied."""
+
+    def __init__(self, axis: Sequence[int], freq: Sequence[float], layout: str = "half", axes: Optional[int] = None):
+        self._h, who = C.c_void_p(), "Rotary"
+        axis = [int(a) for a in axis]
+        _need(len(axis) == len(freq) and axis, f"{who}: an axis and a frequency for each pair")
+        _need(layout in ("half", "next"), f"{who}: unknown layout {layout!r}")
+        self.pairs, self.axes = len(axis), _whole(who, "axes", max(axis) + 1 if axes is None else axes)
+        for a in axis:
+            _whole(who, "axis", a)
+        _check(lib().pserve_rotary_create(self.axes, self.pairs, (C.c_int32 * self.pairs)(*axis), (C.c_double * self.pairs)(*[float(f) for f in freq]),
+                                          PAIR_HALF if layout == "half" else PAIR_NEXT, _stream(), C.byref(self._h)))
+
+    def forward(self, q, k, pos, q_out=None, k_out=None):
+        """q [T, heads, D] and k [T, kv_heads, D] or None (any strides between tokens and heads), pos float32 [T, axes].  q_out may be q and k_out k
+        (in place).  Returns (q_out, k_out)."""
+        import torch
+        who = "Rotary.forward"
+        _here(who, q, k, pos, q_out, k_out)
+        dtype = _dtype_code(who, q)
+        if q.dim() != 3 or q.shape[1] == 0 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[1] == 0 or k.shape[2] != q.shape[2] or k.dtype != q.dtype)):
+            raise PserveError(EINVAL, f"{who}: q [T, heads, D], k [T, kv_heads, D] of one dtype")
+        _ints(who, pos, torch.float32, (q.shape[0], self.axes), "pos")
+        _need(k is not None or k_out is None, f"{who}: k_out without k")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            self._given(who, q_out, q, pos, k, k_out)
+        if k is not None:
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            else:
+                self._given(who, k_out, k, pos, q, None)
+        for t in (q, k):
+            if t is not None and t.stride(2) != 1 and t.shape[2] > 1:
+                raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
+        d = _rotary_desc(q.shape[1], 0 if k is None else k.shape[1], q.shape[2], dtype, q.shape[0], q.stride(), (0, 0) if k is None else k.stride(),
+                         q_out.stride(), (0, 0) if k is None else k_out.stride())
+        if k is None:
+            _check(lib().pserve_rotary_forward(self._h, d, pos.data_ptr(), q.data_ptr(), None, q_out.data_ptr(), None, _stream()))
+        else:
+            _check(lib().pserve_rotary_forward(self._h, d, pos.data_ptr(), q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _stream()))
+        return q_out, k_out
+
+    @staticmethod
+    def _given(who: str, out, own, *others):
+        """An output of the caller's: `own` itself (its rows apart) or a tensor that shares nothing with the others."""
+        _need(out.shape == own.shape and out.dtype == own.dtype and (out.stride(2) == 1 or out.shape[2] == 1), f"{who}: an output must have its input's shape and dtype, the values of a head consecutive")
+        (T, H, D), (st, sh, _) = out.shape, out.stride()
+        _need(out.numel() == 0 or (H == 1 or sh >= D) and (T == 1 or st >= (H - 1) * (sh if H > 1 else 0) + D)
+              or (T == 1 or st >= D) and (H == 1 or sh >= (T - 1) * (st if T > 1 else 0) + D), f"{who}: rows of an output overlap")
+        if not (out.data_ptr() == own.data_ptr() and out.stride() == own.stride()):
+            _apart(who, out, own)
+        for t in others:
+            if t is not None and not _interleaved(out, t):
+                _apart(who, out, t)
+
+    def close(self):
+        if self._h:
+            lib().pserve_rotary_free(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _interleaved(a, b) -> bool:
+    """Heads of one matrix side by side, as q and k of a q/k/v projection are: the same distance between tokens, the heads of one behind those of the other."""
+    if a.dim() != 3 or b.dim() != 3 or a.dtype != b.dtype or a.stride(0) != b.stride(0) or a.numel() == 0 or b.numel() == 0:
+        return False
+    size, token = a.element_size(), a.stride(0)
+    wa, wb = ((t.shape[1] - 1) * t.stride(1) + t.shape[2] for t in (a, b))
+    gap, rest = divmod(b.data_ptr() - a.data_ptr(), size)
+    return rest == 0 and min(a.stride(1), b.stride(1)) >= 0 and wa <= gap % token and gap % token + wb <= token if token > 0 else False
+
+
+class RowsF8:
+    """pserve_f8_rows: `rows` rows of K values in 8-bit floating point, a power of two for each block of 128."""
+
+    def __init__(self, rows: int, K: int):
+        import torch
+        who = "RowsF8"
+        self.rows, self.K = _whole(who, "rows", rows), _whole(who, "K", K, 1)
+        n = C.c_size_t()
+        _check(lib().pserve_f8_rows_bytes(self.rows, self.K, C.byref(n)))
+        self.buffer = torch.empty(int(n.value), dtype=torch.uint8, device="cuda")
+
+    def write(self, x):
+        """x [rows, K] (rows may lie further apart), rounded to 8 bits."""
+        who = "RowsF8.write"
+        _here(who, x, self.buffer)
+        dtype = _dtype_code(who, x)
+        _need(x.shape == (self.rows, self.K), f"{who}: x must be [{self.rows}, {self.K}]")
+        ldx, one = x.stride()
+        if self.rows <= 1:
+            ldx = self.K
+        _need((one == 1 or self.K == 1) and ldx >= self.K, f"{who}: the values of a row must be consecutive, rows must not overlap")
+        _check(lib().pserve_f8_rows_write(x.data_ptr(), ldx, self.rows, self.K, dtype, self.buffer.data_ptr(), _stream()))
+        return self
+
+    def read(self, dtype: int, x=None):
+        """The values held, as x [rows, K] of dtype F32 or BF16 (exact)."""
+        import torch
+        who = "RowsF8.read"
+        _here(who, x, self.buffer)
+        _need(dtype in (F32, BF16), f"{who}: unknown dtype {dtype}")
+        if x is None:
+            x = torch.empty((self.rows, self.K), dtype=_torch_dtype(dtype), device=self.buffer.device)
+        _need(x.shape == (self.rows, self.K) and x.is_contiguous() and x.dtype == _torch_dtype(dtype), f"{who}: x must be contiguous [{self.rows}, {self.K}] of dtype")
+        _apart(who, x, self.buffer)
+        _check(lib().pserve_f8_rows_read(self.buffer.data_ptr(), self.rows, self.K, dtype, x.data_ptr(), self.K, _stream()))
+        return x
+
+
+class LinearF8:
+    """pserve_linear_f8: y = x W + b (+ residual), x and W in 8-bit floating point with a power of two for each block of 128 along K.
+    w [K, N], b [N] or None; the weights are rounded here, once."""
+
+    def __init__(self, w, b, dtype: int):
+        self._h, who = C.c_void_p(), "LinearF8"
+        _here(who, w, b)
+        _need(dtype in (F32, BF16) and w.dim() == 2 and w.is_contiguous() and w.dtype == _torch_dtype(dtype), f"{who}: w must be contiguous [K, N] of the given dtype")
+        _need(b is None or (tuple(b.shape) == (w.shape[1],) and b.is_contiguous() and b.dtype == w.dtype), f"{who}: b must be contiguous [N] of the given dtype")
+        self.dtype, self.K, self.N = dtype, _whole(who, "K", w.shape[0]), _whole(who, "N", w.shape[1])
+        _check(lib().pserve_linear_f8_create(self.K, self.N, dtype, w.data_ptr(), None if b is None else b.data_ptr(), _stream(), C.byref(self._h)))
+        self._dtype, self._row_bytes = w.dtype, self.workspace_bytes(1)         # (workspace_bytes is linear in the rows)
+
+    def workspace_bytes(self, rows: int) -> int:
+        n = C.c_size_t()
+        _check(lib().pserve_linear_f8_workspace(self._h, rows, C.byref(n)))
+        return int(n.value)
+
+    def forward(self, x, res=None, y=None, workspace=None):
+        """x [rows, K] (rows may lie further apart) or RowsF8 of that size (then no workspace is taken), res [rows, N] or None (it may be y)."""
+        import torch
+        who = "LinearF8.forward"
+        held = isinstance(x, RowsF8)
+        _here(who, x.buffer if held else x, res, y, workspace)
+        if held:
+            _need(x.K == self.K, f"{who}: rows of {x.K} values, K = {self.K}")
+            _need(workspace is None, f"{who}: rows in 8 bits take no workspace")
+            rows, source = x.rows, x.buffer
+        else:
+            if x.dim() != 2 or x.shape[1] != self.K or x.dtype != self._dtype:
+                raise PserveError(EINVAL, f"{who}: x must be [rows, {self.K}] of the layer's dtype")
+            rows, source = x.shape[0], x
+            ldx, one = x.stride()
+            if rows <= 1:
+                ldx = self.K
+            if (one != 1 and self.K > 1) or ldx < self.K:
+                raise PserveError(EINVAL, f"{who}: the values of a row must be consecutive, rows must not overlap")
+        for t in (y, res):
+            if t is not None and (t.shape != (rows, self.N) or not t.is_contiguous() or t.dtype != self._dtype):
+                raise PserveError(EINVAL, f"{who}: res and y must be contiguous [rows, {self.N}] of the layer's dtype")
+        if y is None:
+            y = torch.empty((rows, self.N), dtype=self._dtype, device=source.device)
+        else:
+            _apart(who, y, source, *([res] if res is not None and res.data_ptr() != y.data_ptr() else []))
+        rp = None if res is None else res.data_ptr()
+        if held:
+            _check(lib().pserve_linear_f8_forward_rows(self._h, source.data_ptr(), rows, rp, y.data_ptr(), _stream()))
+            return y
+        ws, nws, keep = _workspace(rows * self._row_bytes, workspace, x.device, who)
+        _check(lib().pserve_linear_f8_forward(self._h, x.data_ptr(), ldx, rows, rp, ws, nws, y.data_ptr(), _stream()))
+        return y
+
+    def close(self):
+        if self._h:
+            lib().pserve_linear_f8_free(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+@lru_cache(maxsize=1024)
+def _gated_norm_desc(*fields):
+    return C.byref(_GatedNormDesc(*fields))
+
+
+def gated_norm(x, f=None, *, post: Optional[str] = None, post_gain=None, post_bias=None, post_eps: float = 1e-5, gate=None, skip_scale: float = 1.0,
+               branch_scale: float = 1.0, pre: Optional[str] = None, pre_gain=None, pre_bias=None, pre_eps: float = 1e-5, scale=None, shift=None,
+               cu_rows=None, which=None, plan: Optional["Plan"] = None, y=None, h=None, rows8: Optional[RowsF8] = None):
+    """pserve_gated_norm: the end of one sub-layer, y = skip_scale * x + branch_scale * gate_s * (N_post(f) * post_gain + post_bias), and the
+    beginning of the next, h = (N_pre(y) * pre_gain + pre_bias) * (1 + scale_s) + shift_s, in one pass over the rows.  N: None, "rms" or "layer".
+    x, f [rows, C] (rows may lie further apart); gains and biases [C]; gate, scale, shift [n, C], one for each request; cu_rows int32 [n + 1]
+    on the device: the rows of the requests (None: all rows are one request's), which int32 [n]: the vectors a request takes instead of its
+    own.  plan: a plan's rows, with vectors in caller order.  What is None is left out.  y is returned where f is given (or y is), h where any part of its formula is
+    (or h is); rows8: h goes there, in 8 bits.  y or h may be x or f.  Rows of no request are not written.  Returns (y, h)."""
+    import torch
+    who = "gated_norm"
+    _here(who, x, f, post_gain, post_bias, gate, pre_gain, pre_bias, scale, shift, cu_rows, which, y, h, None if rows8 is None else rows8.buffer)
+    dtype = _dtype_code(who, x)
+    if x.dim() != 2:
+        raise PserveError(EINVAL, f"{who}: x must be [rows, C]")
+    rows, Cc = x.shape
+    if post not in NORM or pre not in NORM:
+        raise PserveError(EINVAL, f"{who}: unknown norm")
+    n = 1
+    cu_p = which_p = None
+    if plan is not None:
+        _need(cu_rows is None and which is None, f"{who}: plan and cu_rows at once")
+        _need(rows == plan.T, f"{who}: x must have the plan's {plan.T} rows")
+        n, cu_p, which_p = plan.n, plan.table_device_ptr("cu_seqlens"), plan.table_device_ptr("perm")
+    else:
+        if cu_rows is not None:
+            _need(cu_rows.dim() == 1 and cu_rows.shape[0] >= 2, f"{who}: cu_rows must be int32 [n + 1], n > 0")
+            _ints(who, cu_rows, torch.int32, cu_rows.shape, "cu_rows")
+            n, cu_p = cu_rows.shape[0] - 1, cu_rows.data_ptr()
+        if which is not None:
+            _ints(who, which, torch.int32, (n,), "which")
+            which_p = which.data_ptr()
+    ends = f is not None
+    begins = rows8 is not None or h is not None or pre is not None or pre_gain is not None or pre_bias is not None or scale is not None or shift is not None
+    for t in (post_gain, post_bias, pre_gain, pre_bias):
+        if t is not None and (t.shape != (Cc,) or t.dtype != x.dtype or not t.is_contiguous()):
+            raise PserveError(EINVAL, f"{who}: gains and biases must be contiguous [{Cc}] of x's dtype")
+    for t in (gate, scale, shift):
+        if t is not None and (t.shape != (n, Cc) or t.dtype != x.dtype or (t.stride(1) != 1 and Cc > 1)):
+            raise PserveError(EINVAL, f"{who}: gate, scale and shift must be [{n}, {Cc}] of x's dtype, the values of a request consecutive")
+    if rows8 is not None:
+        _need(h is None, f"{who}: h and rows8 at once")
+        _need((rows8.rows, rows8.K) == (rows, Cc), f"{who}: rows8 must have {rows} rows of {Cc} values")
+    for t in (x, f, y, h):
+        if t is not None and (t.shape != (rows, Cc) or t.dtype != x.dtype or (t.stride(1) != 1 and Cc > 1) or (rows > 1 and t.stride(0) < Cc)):
+            raise PserveError(EINVAL, f"{who}: x, f, y and h must be [{rows}, {Cc}] of one dtype, the values of a row consecutive, rows apart")
+    vectors = (post_gain, post_bias, gate, pre_gain, pre_bias, scale, shift, cu_rows, which)
+    for out, other in ((y, h), (h, y)):
+        if out is not None:
+            for t in (x, f):
+                if t is not None and not (t.data_ptr() == out.data_ptr() and (t.stride(0) == out.stride(0) or rows <= 1)):
+                    _apart(who, out, t)
+            _apart(who, out, other, *vectors)
+    if rows8 is not None:
+        _apart(who, rows8.buffer, x, f, y, *vectors)
+    if y is None and ends:
+        y = torch.empty((rows, Cc), dtype=x.dtype, device=x.device)
+    if h is None and begins and rows8 is None:
+        h = torch.empty((rows, Cc), dtype=x.dtype, device=x.device)
+
+    def stride(t):
+        return 0 if t is None else Cc if t.shape[0] <= 1 else t.stride(0)
+
+    def ptr(t):
+        return None if t is None else t.data_ptr()
+
+    d = _gated_norm_desc(Cc, dtype, n, NORM[post], NORM[pre], float(post_eps), float(pre_eps), float(skip_scale), float(branch_scale), rows,
+                         stride(x), stride(f), stride(y), stride(h), stride(gate), stride(scale), stride(shift))
+    b = _GatedNormBuffers(ptr(x), ptr(f), ptr(post_gain), ptr(post_bias), ptr(gate), ptr(pre_gain), ptr(pre_bias), ptr(scale), ptr(shift),
+                          cu_p, which_p, ptr(y), ptr(h), None if rows8 is None else rows8.buffer.data_ptr())
+    _check(lib().pserve_gated_norm(d, C.byref(b), _stream()))
+    return y, h
 
 
 # ---- host-side scheduler pieces (tasks are tuples (id, H, W, steps_left, arrival, ddl, standalone), times in ms)

@@ -1,0 +1,65 @@
+// Rounding to 8-bit floating point (e4m3: sign, four exponent bits, three fraction bits, largest number 448), shared by the rows that the
+// norms write and the 8-bit floating-point layers.
+//
+// A block of 128 consecutive values x_i is held as numbers v_i = e4m3(x_i 2^-e) and one power of two 2^e, e the smallest whole number of
+// -100 .. 119 with max |x_i| <= 448 * 2^e, so e = 119 where none is (what lies beyond 448 * 2^119 = 2.98e38 is held as that; what the block stands
+// for, v_i 2^e, is a normal bf16 number or zero in all cases, which the layers of fp32 tensors use).  A power of two
+// and not amax / 448: multiplying by it does not round, so the one rounding of a value (to the nearest, halves to the even fraction) is that
+// of the conversion instruction; the relative error is the same 2^-4 at most, as the format's numbers lie as dense at both ends of a factor of
+// two; and the matrix instruction takes powers of two (scale byte e + 127) for nothing.  A block with an infinity or a NaN is held as NaN.
+#pragma once
+
+#include "quant8.h"
+
+namespace pserve {
+
+constexpr int F8_BLOCK = 128;
+constexpr uint32_t F8_NAN4 = 0x7f7f7f7fu;
+constexpr uint32_t F8_LARGEST_BITS = 0x7f600000u;      // 448 * 2^119
+constexpr uint32_t F8_FIRST_BYTE = 127 - 100, F8_LAST_BYTE = 127 + 119;
+
+// rows of K values: [rows][f8_width(K)] numbers, then [rows][f8_scales(K)] scale bytes (whole words of four)
+__host__ __device__ inline int32_t f8_width(int32_t K) { return (K + 127) / 128 * 128; }
+__host__ __device__ inline int32_t f8_scales(int32_t K) { return (K + 511) / 512 * 4; }
+inline size_t f8_bytes(int64_t rows, int32_t K) { return (size_t)rows * (size_t)(f8_width(K) + f8_scales(K)); }
+
+struct F8Scale {
+    uint32_t amax, byte;
+    float mul;                                          // 2^-e
+    __device__ __forceinline__ explicit F8Scale(uint32_t amax_bits) : amax(amax_bits) {
+        // the exponent field counts up where the fraction passes 0.75 (448 = 1.75 * 2^8)
+        const uint32_t up = (amax_bits + 0x1fffffu) >> 23;
+        byte = min(max(up, F8_FIRST_BYTE + 8u) - 8u, F8_LAST_BYTE);
+        if (amax_bits >= 0x7f800000u) byte = 127;
+        mul = __uint_as_float((254u - byte) << 23);
+    }
+    __device__ __forceinline__ q8_u32x2 pack8(const float (&v)[8]) const {
+        float s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = v[i] * mul;
+        if (amax > F8_LARGEST_BITS) {                   // (the conversion does not cut off)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = fminf(fmaxf(s[i], -448.f), 448.f);
+        }
+        q8_u32x2 o;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(s[4 * h], s[4 * h + 1], 0, false);
+            w = __builtin_amdgcn_cvt_pk_fp8_f32(s[4 * h + 2], s[4 * h + 3], w, true);
+            o[h] = amax >= 0x7f800000u ? F8_NAN4 : (uint32_t)w;
+        }
+        return o;
+    }
+};
+
+__device__ __forceinline__ float f8_scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// the largest |v| of eight values as a bit pattern (infinities and NaN come out on top)
+__device__ __forceinline__ uint32_t f8_largest(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+    return m;
+}
+
+}  // namespace pserve

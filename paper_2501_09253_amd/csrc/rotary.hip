@@ -1,0 +1,195 @@
+// Rotary positions with several axes (pserve_rotary_*, pserve_plan_positions), gfx950.
+//
+//   theta_p = pos[t][axis_p] * freq_p,   (a, b) -> (a cos theta_p - b sin theta_p, a sin theta_p + b cos theta_p)
+//
+// for each pair p of values of a head.  Bound by memory: every value is read and written once.  The angles are a token's, whatever its
+// heads are: a block computes those of its tokens once, into LDS, then walks its tokens' heads in 16-byte pieces.
+// An angle is taken in revolutions, in 64 bits (positions reach 2^24, and 32 bits leave a position of 2^17 with an angle off by 2^-7); the
+// fraction of a revolution is rounded to fp32, at most 2^-26 off: 2^-23.3 radians.
+#include "quant8.h"
+
+using namespace pserve;
+
+struct pserve_rotary_s {
+    int32_t axes = 0, pairs = 0, layout = 0;
+    int device = 0;
+    double* freq = nullptr;                     // [pairs] revolutions a unit of position
+    int32_t* axis = nullptr;                    // [pairs]
+    pserve::DevicePool pool;
+};
+
+namespace pserve {
+
+struct RotaryArgs {
+    const void *q, *k;
+    void *q_out, *k_out;
+    const float* pos;                           // [tokens][axes]
+    const double* freq;
+    const int32_t* axis;
+    int64_t tokens, qs[2], ks[2], qo[2], ko[2];
+    int32_t heads, kv_heads, D, P, axes, TB;    // TB: tokens of a block
+    int32_t keep;                               // in place: what is not turned stays
+};
+
+// cosine and sine of the angles of a block's tokens: pair p of token t at [t * P + p]
+__device__ __forceinline__ void rotary_angles(const RotaryArgs& a, int64_t t0, int nt, float2* cs) {
+    for (int i = threadIdx.x; i < nt * a.P; i += blockDim.x) {
+        const int t = i / a.P, p = i - t * a.P;
+        const double turn = (double)a.pos[(t0 + t) * a.axes + a.axis[p]] * a.freq[p];
+        const float f = (float)(turn - rint(turn));             // -1/2 .. 1/2 of a revolution
+        float s, c;
+        sincospif(2.f * f, &s, &c);
+        cs[i] = make_float2(c, s);
+    }
+}
+
+// One value pair a thread, whatever the strides
+template <typename T, bool HALF>
+__global__ void __launch_bounds__(256)
+rotary_pairs_kernel(RotaryArgs a) {
+    extern __shared__ float2 s_turn[];
+    const int64_t t0 = block_of_lines() * a.TB;
+    if (t0 >= a.tokens) return;
+    const int nt = (int)min((int64_t)a.TB, a.tokens - t0);
+    rotary_angles(a, t0, nt, s_turn);
+    __syncthreads();
+    const int rest = a.keep ? 0 : a.D - 2 * a.P, items = a.P + rest, H = a.heads + a.kv_heads;
+    for (int i = threadIdx.x; i < nt * H * items; i += 256) {
+        const int line = i / items, p = i - line * items, t = line / H, h = line - t * H;
+        const bool isq = h < a.heads;
+        const int hh = isq ? h : h - a.heads;
+        const T* in = isq ? (const T*)a.q + (t0 + t) * a.qs[0] + hh * a.qs[1] : (const T*)a.k + (t0 + t) * a.ks[0] + hh * a.ks[1];
+        T* out = isq ? (T*)a.q_out + (t0 + t) * a.qo[0] + hh * a.qo[1] : (T*)a.k_out + (t0 + t) * a.ko[0] + hh * a.ko[1];
+        if (p >= a.P) {
+            out[a.P + p] = in[a.P + p];
+            continue;
+        }
+        const int ia = HALF ? p : 2 * p, ib = HALF ? a.P + p : 2 * p + 1;
+        const float2 cs = s_turn[t * a.P + p];
+        const float x = load1(in + ia), y = load1(in + ib);
+        store1(out + ia, x * cs.x - y * cs.y);
+        store1(out + ib, x * cs.y + y * cs.x);
+    }
+}
+
+template <typename T>
+static int launch_rotary(const RotaryArgs& in, int layout, hipStream_t st) {
+    RotaryArgs a = in;
+    const int H = a.heads + a.kv_heads;
+    a.TB = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / std::max(1, H * a.D / 2), 4096 / a.P));
+    const dim3 grid = block_lines(cdiv(a.tokens, a.TB));
+    const size_t lds = (size_t)a.TB * a.P * sizeof(float2);
+    if (layout == PSERVE_PAIR_HALF) rotary_pairs_kernel<T, true><<<grid, 256, lds, st>>>(a);
+    else rotary_pairs_kernel<T, false><<<grid, 256, lds, st>>>(a);
+    return check_launch("rotary_pairs_kernel");
+}
+
+// ---- positions of a plan's tokens
+struct PlanPosArgs {
+    const int32_t *owner, *rc, *perm;
+    const float* frame;
+    float start[3], step[3];
+    float* pos;
+    int64_t T;
+    int32_t S, ph, pw, text_len;
+};
+__global__ void __launch_bounds__(256)
+plan_positions_kernel(PlanPosArgs a) {
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t >= a.T) return;
+    const int p = (int)(t / a.S), r = (int)(t - (int64_t)p * a.S), row = a.rc[2 * p], col = a.rc[2 * p + 1];
+    float* o = a.pos + 3 * t;
+    if (row < 0) {                                              // text patch `col` of its request
+        const int64_t j = (int64_t)col * a.S + r;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) o[i] = j < a.text_len ? a.start[i] + (float)j * a.step[i] : 0.f;
+        return;
+    }
+    const int y = r / a.pw, x = r - y * a.pw;
+    o[0] = a.frame ? a.frame[a.perm[a.owner[p]]] : 0.f;
+    o[1] = (float)(row * a.ph + y);
+    o[2] = (float)(col * a.pw + x);
+}
+
+}  // namespace pserve
+
+extern "C" {
+
+int pserve_rotary_create(int32_t axes, int32_t pairs, const int32_t* axis, const double* freq, int layout, void* stream, pserve_rotary_t** out) {
+    static const char who[] = "pserve_rotary_create";
+    PS_REQUIRE(out, "%s: out is NULL", who);
+    *out = nullptr;
+    PS_REQUIRE(axis && freq, "%s: NULL argument", who);
+    PS_REQUIRE(axes >= 1 && axes <= 8, "%s: %d axes (1 .. 8)", who, axes);
+    PS_REQUIRE(pairs >= 1 && pairs <= 256, "%s: %d pairs (1 .. 256)", who, pairs);
+    PS_REQUIRE(layout == PSERVE_PAIR_HALF || layout == PSERVE_PAIR_NEXT, "%s: unknown layout %d", who, layout);
+    for (int i = 0; i < pairs; ++i) {
+        PS_REQUIRE(axis[i] >= 0 && axis[i] < axes, "%s: axis %d of pair %d (%d axes)", who, axis[i], i, axes);
+        PS_REQUIRE(freq[i] >= -1e9 && freq[i] <= 1e9, "%s: the frequency of pair %d is not finite or beyond 1e9", who, i);
+    }
+    return guarded(who, [&]() -> int {
+        std::unique_ptr<pserve_rotary_t> op(new pserve_rotary_t());
+        op->axes = axes; op->pairs = pairs; op->layout = layout;
+        PS_CHECK_HIP(hipGetDevice(&op->device));
+        PS_TRY(op->pool.alloc_t(&op->freq, pairs));
+        PS_TRY(op->pool.alloc_t(&op->axis, pairs));
+        std::vector<double> turns(pairs);
+        for (int i = 0; i < pairs; ++i) turns[i] = freq[i] / 6.283185307179586476925286766559;
+        hipStream_t st = (hipStream_t)stream;
+        PS_CHECK_HIP(hipMemcpyAsync(op->freq, turns.data(), pairs * sizeof(double), hipMemcpyHostToDevice, st));
+        PS_CHECK_HIP(hipMemcpyAsync(op->axis, axis, pairs * sizeof(int32_t), hipMemcpyHostToDevice, st));
+        PS_CHECK_HIP(hipStreamSynchronize(st));
+        *out = op.release();
+        return PSERVE_OK;
+    });
+}
+
+void pserve_rotary_free(pserve_rotary_t* op) { delete op; }
+
+int pserve_rotary_forward(const pserve_rotary_t* op, const pserve_rotary_desc* d, const float* pos, const void* q, const void* k, void* q_out,
+                          void* k_out, void* stream) {
+    static const char who[] = "pserve_rotary_forward";
+    PS_REQUIRE(op && d, "%s: NULL argument", who);
+    PS_REQUIRE(d->dtype == PSERVE_F32 || d->dtype == PSERVE_BF16, "%s: unknown dtype %d", who, d->dtype);
+    PS_REQUIRE(d->heads > 0 && d->kv_heads >= 0 && d->heads <= 4096 && d->kv_heads <= 4096, "%s: %d and %d heads (1 .. 4096, 0 .. 4096)", who, d->heads, d->kv_heads);
+    PS_REQUIRE(d->head_dim >= 2 * op->pairs && d->head_dim <= 512, "%s: head_dim %d (%d pairs; up to 512)", who, d->head_dim, op->pairs);
+    PS_REQUIRE(d->tokens >= 0 && d->tokens < (1ll << 31), "%s: %lld tokens (fewer than 2^31)", who, (long long)d->tokens);
+    const int64_t* strides[4] = {d->q_stride, d->q_out_stride, d->k_stride, d->k_out_stride};
+    for (int i = 0; i < (d->kv_heads ? 4 : 2); ++i)
+        for (int j = 0; j < 2; ++j)
+            PS_REQUIRE(strides[i][j] >= 0 && strides[i][j] < (1ll << 31), "%s: a stride of %lld elements", who, (long long)strides[i][j]);
+    if (d->tokens == 0) return PSERVE_OK;
+    PS_REQUIRE(pos && q && q_out && (!d->kv_heads || (k && k_out)), "%s: NULL buffer", who);
+    const uintptr_t es = dtype_size(d->dtype);
+    PS_REQUIRE(!(((uintptr_t)q | (uintptr_t)q_out | (d->kv_heads ? (uintptr_t)k | (uintptr_t)k_out : 0)) & (es - 1)) && !((uintptr_t)pos & 3),
+               "%s: a buffer is not aligned to its type", who);
+    int dev;
+    PS_CHECK_HIP(hipGetDevice(&dev));
+    PS_REQUIRE(dev == op->device, "%s: the frequencies are on device %d, the current one is %d", who, op->device, dev);
+    RotaryArgs a{};
+    a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.pos = pos; a.freq = op->freq; a.axis = op->axis;
+    a.tokens = d->tokens; a.heads = d->heads; a.kv_heads = d->kv_heads; a.D = d->head_dim; a.P = op->pairs; a.axes = op->axes;
+    for (int j = 0; j < 2; ++j) {
+        a.qs[j] = d->q_stride[j]; a.qo[j] = d->q_out_stride[j];
+        a.ks[j] = d->k_stride[j]; a.ko[j] = d->k_out_stride[j];
+    }
+    a.keep = q == q_out && (!d->kv_heads || k == k_out);
+    hipStream_t st = (hipStream_t)stream;
+    return d->dtype == PSERVE_BF16 ? launch_rotary<uint16_t>(a, op->layout, st) : launch_rotary<float>(a, op->layout, st);
+}
+
+int pserve_plan_positions(const pserve_plan_t* plan, const float* frame, const float* text, float* pos, void* stream) {
+    static const char who[] = "pserve_plan_positions";
+    PS_REQUIRE(plan && pos, "%s: NULL argument", who);
+    PlanPosArgs a{};
+    a.owner = plan->d_tab[PSERVE_TAB_PATCH_OWNER]; a.rc = plan->d_tab[PSERVE_TAB_PATCH_RC]; a.perm = plan->d_tab[PSERVE_TAB_PERM];
+    a.frame = frame; a.pos = pos; a.T = plan->T; a.S = plan->S; a.ph = plan->ph; a.pw = plan->pw; a.text_len = plan->text_len;
+    for (int i = 0; i < 3; ++i) {
+        a.start[i] = text ? text[i] : 0.f;
+        a.step[i] = text ? text[3 + i] : 0.f;
+    }
+    plan_positions_kernel<<<(unsigned)cdiv(a.T, 256), 256, 0, (hipStream_t)stream>>>(a);
+    return check_launch("plan_positions_kernel");
+}
+
+}  // extern "C"

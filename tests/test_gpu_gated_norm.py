@@ -1,0 +1,231 @@
+"""Norms before and after a sub-layer with its gate and residual scale, against the plain 64-bit form, value by value within the bound of
+tests/layer_oracle.py; into 8-bit rows: the numbers next to h."""
+import pytest
+import torch
+
+import layer_oracle as lo
+import paper_2501_09253_amd as ps
+from test_gpu_prompt_attention import DT, ints, make
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(rows, C, dtype, n, seed=0):
+    d = DT[dtype]
+    sizes = torch.logspace(-2, 2, rows)[:, None]
+    t = dict(x=(make(seed + 1, (rows, C), torch.float32) * sizes).to(d), f=(make(seed + 2, (rows, C), torch.float32) * sizes.flip(0) + 0.5).to(d))
+    for i, name in enumerate(("post_gain", "post_bias", "pre_gain", "pre_bias")):
+        t[name] = make(seed + 3 + i, (C,), d)
+    for i, name in enumerate(("gate", "scale", "shift")):
+        t[name] = make(seed + 7 + i, (n, C), d)
+    return t
+
+
+def gpu(t):
+    return {k: v.cuda() if torch.is_tensor(v) else v for k, v in t.items()}
+
+
+def near(got, want, dtype):
+    tol = want.e + lo.HALF[DT[dtype]] * (want.v.abs() + want.e) + 1e-37
+    err = (got.double().cpu() - want.v).abs()
+    assert torch.all(err <= tol), (err / tol).max().item()
+
+
+def near8(rows8, want):
+    """Held numbers against h: half a step of the number, or of the block's smallest numbers, from h; the block's power of two from its largest."""
+    held = rows8.read(ps.F32).double().cpu()
+    rows, C = held.shape
+    h, e = want.v, want.e
+    tol = torch.zeros_like(h)
+    for c in range(0, C, 128):
+        b = slice(c, c + 128)
+        k = lo.f8_exponent((h[:, b].abs() + e[:, b]).amax(1, keepdim=True))
+        tol[:, b] = e[:, b] + torch.maximum(2.0 ** -4 * (h[:, b].abs() + e[:, b]), 2.0 ** (k - 10))
+    err = (held - h).abs()
+    assert torch.all(err <= tol), (err / tol).max().item()
+
+
+KINDS = [(None, None), ("rms", "rms"), ("rms", "layer"), ("layer", "rms"), ("layer", None), (None, "layer")]
+WIDTHS = [1, 2, 7, 64, 65, 512, 640, 1000, 1024, 1536, 2047, 2560, 4096, 4100, 8192, 16384]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("post,pre", KINDS)
+@pytest.mark.parametrize("C", WIDTHS)
+def test_widths_and_kinds(C, post, pre, dtype):
+    rows = 9
+    t = inputs(rows, C, dtype, 1)
+    kinds = dict(post=post, pre=pre, branch_scale=0.7, skip_scale=1.25, post_eps=1e-6, pre_eps=1e-3)
+    y, h = ps.gated_norm(**gpu(t), **kinds)
+    wy, wh = lo.gated_norm(**t, **kinds)
+    near(y, wy, dtype)
+    near(h, wh, dtype)
+    rows8 = ps.RowsF8(rows, C)
+    y8, none = ps.gated_norm(**gpu(t), **kinds, rows8=rows8)
+    assert none is None and torch.equal(y8, y)
+    near8(rows8, wh)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("left_out", [("f", "post_gain", "post_bias", "gate"), ("post_gain", "pre_gain"), ("post_bias", "pre_bias", "gate"), ("scale",), ("shift", "gate"),
+                                      ("pre_gain", "pre_bias", "scale", "shift"), ("post_gain", "post_bias", "gate", "pre_gain", "pre_bias", "scale", "shift")])
+def test_parts_left_out(left_out, dtype):
+    t = inputs(13, 192, dtype, 1)
+    for name in left_out:
+        t[name] = None
+    kinds = dict(post="rms" if t["f"] is not None else None, pre="layer")
+    if "scale" in left_out and "pre_gain" in left_out and t["f"] is not None:
+        kinds["pre"] = None
+    y, h = ps.gated_norm(**gpu(t), **kinds)
+    wy, wh = lo.gated_norm(**t, **kinds)
+    assert (y is None) == (t["f"] is None)
+    if y is not None:
+        near(y, wy, dtype)
+    begins = kinds["pre"] is not None or any(t[k] is not None for k in ("pre_gain", "pre_bias", "scale", "shift"))
+    assert (h is not None) == begins
+    if begins:
+        near(h, wh, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts", [[1], [0, 3, 0, 5, 1, 0], [1] * 70, [0] * 40 + [7] + [0] * 30 + [2], [3, 0] * 100, [1] * 5000])
+def test_requests(counts, dtype):
+    """Every request has its own vectors; empty requests; rows in front of the first and behind the last are left as they were."""
+    n, C, front, behind = len(counts), 96, 2, 3
+    rows = front + sum(counts) + behind
+    t = inputs(rows, C, dtype, n)
+    cu = [front]
+    for c in counts:
+        cu.append(cu[-1] + c)
+    request = torch.cat([torch.full((c,), i) for i, c in enumerate(counts)])
+    mine = slice(front, rows - behind)
+    for which in (None, torch.randperm(n, generator=torch.Generator().manual_seed(1))):
+        y, h = (torch.full((rows, C), 7.0, dtype=DT[dtype], device="cuda") for _ in range(2))
+        ps.gated_norm(**gpu(t), post="layer", pre="rms", cu_rows=ints(cu), which=None if which is None else which.int().cuda(), y=y, h=h)
+        part = dict(t, x=t["x"][mine], f=t["f"][mine])
+        wy, wh = lo.gated_norm(**part, post="layer", pre="rms", request=request if which is None else which[request])
+        near(y[mine], wy, dtype)
+        near(h[mine], wh, dtype)
+        for out in (y, h):
+            assert torch.all(out[:front] == 7) and torch.all(out[rows - behind:] == 7)
+    rows8 = ps.RowsF8(rows, C)
+    rows8.buffer.fill_(33)
+    ps.gated_norm(**gpu(t), post="layer", pre="rms", cu_rows=ints(cu), rows8=rows8)
+    numbers, scales = rows8.buffer[:rows * 128].view(rows, 128), rows8.buffer[rows * 128:].view(rows, 4)
+    for part in (slice(0, front), slice(rows - behind, rows)):
+        assert torch.all(numbers[part] == 33) and torch.all(scales[part] == 33)
+
+
+def test_vectors_that_are_not_there():
+    """A request whose `which` lies outside: its rows are left as they were."""
+    t = inputs(6, 64, "bf16", 3)
+    y, h = (torch.full((6, 64), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ps.gated_norm(**gpu(t), pre="rms", cu_rows=ints([0, 2, 4, 6]), which=ints([1, 3, -1]), y=y, h=h)
+    wy, _ = lo.gated_norm(**{k: v[:2] if k in "xf" else v for k, v in t.items()}, pre="rms", request=torch.tensor([1, 1]))
+    near(y[:2], wy, "bf16")
+    assert torch.all(y[2:] == 7) and torch.all(h[2:] == 7)
+
+
+@pytest.mark.parametrize("text", [0, 20])
+def test_rows_of_a_plan(text):
+    res = [(16, 16), (8, 24), (16, 8), (8, 8)]
+    plan = ps.Plan(res, 8, 8, text_len=text)
+    t = inputs(plan.T, 128, "bf16", plan.n)
+    y, h = ps.gated_norm(**gpu(t), post="rms", pre="layer", plan=plan)
+    cu, perm = plan.table("cu_seqlens"), plan.table("perm")
+    request = torch.cat([torch.full((int(cu[s + 1] - cu[s]),), int(perm[s])) for s in range(plan.n)])
+    wy, wh = lo.gated_norm(**t, post="rms", pre="layer", request=request)
+    near(y, wy, "bf16")
+    near(h, wh, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C,off", [(160, 0), (160, 8), (160, 3), (77, 1)])
+def test_strides_and_in_place(C, off, dtype):
+    rows, n = 21, 3
+    t = inputs(rows, C, dtype, n)
+    cu = ints([0, 5, 5, rows])
+    request = torch.tensor([0] * 5 + [2] * 16)
+    g = gpu(t)
+    for name in ("x", "f"):
+        wide = torch.zeros((rows, C + 24), dtype=DT[dtype], device="cuda")
+        wide[:, off:off + C] = g[name]
+        g[name] = wide[:, off:off + C]
+    mod = torch.zeros((n, 3 * C + off), dtype=DT[dtype], device="cuda")
+    for i, name in enumerate(("gate", "scale", "shift")):
+        mod[:, off + i * C:off + (i + 1) * C] = g[name]
+        g[name] = mod[:, off + i * C:off + (i + 1) * C]
+    wy, wh = lo.gated_norm(**t, post="layer", pre="layer", request=request)
+    y, h = ps.gated_norm(**g, post="layer", pre="layer", cu_rows=cu)
+    near(y, wy, dtype)
+    near(h, wh, dtype)
+    buf = torch.full((rows, C + 5), 7.0, dtype=DT[dtype], device="cuda")        # an output inside a wider matrix
+    ps.gated_norm(**g, post="layer", pre="layer", cu_rows=cu, h=buf[:, 2:2 + C])
+    assert torch.equal(buf[:, 2:2 + C], h) and torch.all(buf[:, :2] == 7) and torch.all(buf[:, 2 + C:] == 7)
+    base = g["x"]._base.clone()
+    ps.gated_norm(**g, post="layer", pre="layer", cu_rows=cu, y=g["x"], h=g["f"])       # in place, the next sub-layer's input over the last one's output
+    assert torch.equal(g["x"], y) and torch.equal(g["f"], h)
+    g["x"].copy_(base[:, off:off + C])
+    assert torch.equal(g["x"]._base, base)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [64, 1536, 4096])
+def test_constant_rows_zeros_and_what_is_not_finite(C, dtype):
+    t = inputs(8, C, dtype, 1)
+    t["f"][0], t["f"][1], t["x"][1] = 3.0, 0.0, 0.0
+    t["f"][2] = 1e-20
+    clean = ps.gated_norm(**gpu(t), post="layer", pre="rms", post_eps=1e-5, pre_eps=1e-12)
+    wy, wh = lo.gated_norm(**t, post="layer", pre="rms", pre_eps=1e-12)
+    near(clean[0], wy, dtype)
+    near(clean[1], wh, dtype)
+    t["f"][3, 5], t["x"][4, 7], t["f"][5, 0] = float("nan"), float("inf"), float("-inf")
+    y, h = ps.gated_norm(**gpu(t), post="layer", pre="rms", post_eps=1e-5, pre_eps=1e-12)
+    for r in (0, 1, 2, 6, 7):
+        assert torch.equal(y[r], clean[0][r]) and torch.equal(h[r], clean[1][r])
+    assert torch.isnan(y[3]).all() and torch.isnan(h[3]).all() and torch.isnan(y[5]).all()
+    assert torch.isinf(y[4, 7]) and torch.isfinite(y[4]).sum() == C - 1
+    rows8 = ps.RowsF8(8, C)
+    ps.gated_norm(**gpu(t), post="layer", pre="rms", rows8=rows8)
+    held = rows8.read(ps.F32)
+    assert torch.isnan(held[3]).all() and torch.isfinite(held[0]).all() and torch.isfinite(held[6]).all()
+
+
+def test_many_rows():
+    rows, C = 40011, 64
+    t = inputs(rows, C, "bf16", 3)
+    cu = [0, 17, 30000, rows]
+    request = torch.cat([torch.full((cu[i + 1] - cu[i],), i) for i in range(3)])
+    y, h = ps.gated_norm(**gpu(t), post="rms", pre="layer", cu_rows=ints(cu))
+    wy, wh = lo.gated_norm(**t, post="rms", pre="layer", request=request)
+    near(y, wy, "bf16")
+    near(h, wh, "bf16")
+
+
+def test_no_rows():
+    x = torch.empty((0, 64), dtype=torch.bfloat16, device="cuda")
+    y, h = ps.gated_norm(x, x, post="rms", pre="rms")
+    assert y.shape == h.shape == (0, 64)
+
+
+def test_graph_and_streams():
+    t = gpu(inputs(50, 256, "bf16", 2))
+    cu = ints([0, 20, 50])
+    want = ps.gated_norm(**t, post="rms", pre="layer", cu_rows=cu)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = ps.gated_norm(**t, post="rms", pre="layer", cu_rows=cu)
+    side.synchronize()
+    assert torch.equal(other[0], want[0]) and torch.equal(other[1], want[1])
+    y, h = torch.empty_like(want[0]), torch.empty_like(want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ps.gated_norm(**t, post="rms", pre="layer", cu_rows=cu, y=y, h=h)
+    for i in range(3):
+        t["x"].copy_(make(40 + i, (50, 256), torch.bfloat16))
+        cu.copy_(ints([0, 10 + 10 * i, 50]))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = ps.gated_norm(**t, post="rms", pre="layer", cu_rows=cu)
+        assert torch.equal(y, want[0]) and torch.equal(h, want[1])
