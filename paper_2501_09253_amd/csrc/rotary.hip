@@ -43,45 +43,135 @@ __device__ __forceinline__ void rotary_angles(const RotaryArgs& a, int64_t t0, i
     }
 }
 
-// One value pair a thread, whatever the strides
-template <typename T, bool HALF>
+// n / d for n * d < 2^32, by the rounded-up reciprocal
+struct Divisor {
+    uint32_t d, m;
+    explicit Divisor(uint32_t d_) : d(d_), m(d_ > 1 ? (uint32_t)(((1ull << 32) + d_ - 1) / d_) : 0) {}
+    __device__ __forceinline__ int operator()(int n) const { return d > 1 ? (int)__umulhi((uint32_t)n, m) : n; }
+};
+
+template <int BYTES> struct Piece;
+template <> struct Piece<16> { typedef u32x4 type; };
+template <> struct Piece<8> { typedef q8_u32x2 type; };
+template <> struct Piece<4> { typedef uint32_t type; };
+template <> struct Piece<2> { typedef uint16_t type; };
+
+// An item is VP pairs of a head, two pieces of VP values each (HALF: p and P + p, NEXT: one behind the other), or two pieces of what is copied.  A block's items are
+// numbered line by line (token, head); a thread asks for its first IT items before the angles are formed, so the two ways to memory overlap.
+template <typename T, bool HALF, int VP, int IT>
 __global__ void __launch_bounds__(256)
-rotary_pairs_kernel(RotaryArgs a) {
+rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
     extern __shared__ float2 s_turn[];
+    typedef typename Piece<VP * sizeof(T)>::type Raw;
     const int64_t t0 = block_of_lines() * a.TB;
     if (t0 >= a.tokens) return;
-    const int nt = (int)min((int64_t)a.TB, a.tokens - t0);
+    const int nt = (int)min((int64_t)a.TB, a.tokens - t0), total = nt * (int)(heads.d * items.d), turned = a.P / VP;
+    const T* in;
+    T* out;
+    int t, ia, ib;
+    bool second;
+    auto place = [&](int i) {
+        const int line = items(i), c = i - line * (int)items.d;
+        t = heads(line);
+        const int h = line - t * (int)heads.d, hk = h - a.heads;
+        if (hk < 0) {
+            in = (const T*)a.q + (t0 + t) * a.qs[0] + h * a.qs[1];
+            out = (T*)a.q_out + (t0 + t) * a.qo[0] + h * a.qo[1];
+        } else {
+            in = (const T*)a.k + (t0 + t) * a.ks[0] + hk * a.ks[1];
+            out = (T*)a.k_out + (t0 + t) * a.ko[0] + hk * a.ko[1];
+        }
+        if (c < turned) {
+            ia = HALF ? c * VP : 2 * c * VP;
+            ib = HALF ? a.P + c * VP : ia + VP;
+            second = true;
+            t = t * a.P + c * VP;               // of the first pair's angle
+        } else {
+            ia = 2 * a.P + 2 * (c - turned) * VP;
+            ib = ia + VP;
+            second = ib < a.D;
+            t = -1;
+        }
+    };
+    Raw ra[IT], rb[IT];
+    auto load = [&](int i, Raw& x, Raw& y) {
+        place(i);
+        x = *reinterpret_cast<const Raw*>(in + ia);
+        if (second) y = *reinterpret_cast<const Raw*>(in + ib);
+    };
+    auto finish = [&](int i, Raw& x, Raw& y) {
+        place(i);
+        if (t >= 0) {
+            T vx[VP], vy[VP];
+            __builtin_memcpy(vx, &x, sizeof x);
+            __builtin_memcpy(vy, &y, sizeof y);
+            const float2* cs = s_turn + t;
+#pragma unroll
+            for (int e = 0; e < VP; ++e) {
+                T *pa = HALF || e < VP / 2 ? vx : vy, *pb = pa;     // where pair e lies in the two pieces
+                int ja = HALF ? e : 2 * e % VP, jb = ja + 1;
+                if (HALF || VP == 1) { pa = vx; pb = vy; ja = jb = e; }
+                const float u = load1(pa + ja), v = load1(pb + jb), c = cs[e].x, s = cs[e].y;
+                store1(pa + ja, u * c - v * s);
+                store1(pb + jb, u * s + v * c);
+            }
+            __builtin_memcpy(&x, vx, sizeof x);
+            __builtin_memcpy(&y, vy, sizeof y);
+        }
+        *reinterpret_cast<Raw*>(out + ia) = x;
+        if (second) *reinterpret_cast<Raw*>(out + ib) = y;
+    };
+#pragma unroll
+    for (int j = 0; j < IT; ++j)
+        if (threadIdx.x + 256 * j < total) load(threadIdx.x + 256 * j, ra[j], rb[j]);
     rotary_angles(a, t0, nt, s_turn);
     __syncthreads();
-    const int rest = a.keep ? 0 : a.D - 2 * a.P, items = a.P + rest, H = a.heads + a.kv_heads;
-    for (int i = threadIdx.x; i < nt * H * items; i += 256) {
-        const int line = i / items, p = i - line * items, t = line / H, h = line - t * H;
-        const bool isq = h < a.heads;
-        const int hh = isq ? h : h - a.heads;
-        const T* in = isq ? (const T*)a.q + (t0 + t) * a.qs[0] + hh * a.qs[1] : (const T*)a.k + (t0 + t) * a.ks[0] + hh * a.ks[1];
-        T* out = isq ? (T*)a.q_out + (t0 + t) * a.qo[0] + hh * a.qo[1] : (T*)a.k_out + (t0 + t) * a.ko[0] + hh * a.ko[1];
-        if (p >= a.P) {
-            out[a.P + p] = in[a.P + p];
-            continue;
-        }
-        const int ia = HALF ? p : 2 * p, ib = HALF ? a.P + p : 2 * p + 1;
-        const float2 cs = s_turn[t * a.P + p];
-        const float x = load1(in + ia), y = load1(in + ib);
-        store1(out + ia, x * cs.x - y * cs.y);
-        store1(out + ib, x * cs.y + y * cs.x);
+#pragma unroll
+    for (int j = 0; j < IT; ++j)
+        if (threadIdx.x + 256 * j < total) finish(threadIdx.x + 256 * j, ra[j], rb[j]);
+    for (int i = threadIdx.x + 256 * IT; i < total; i += 256) {
+        load(i, ra[0], rb[0]);
+        finish(i, ra[0], rb[0]);
     }
 }
 
-template <typename T>
-static int launch_rotary(const RotaryArgs& in, int layout, hipStream_t st) {
+template <typename T, int VP>
+static int launch_rotary_as(const RotaryArgs& in, int layout, hipStream_t st) {
+    constexpr int IT = 4;
     RotaryArgs a = in;
-    const int H = a.heads + a.kv_heads;
-    a.TB = (int)std::max<int64_t>(1, std::min<int64_t>(2048 / std::max(1, H * a.D / 2), 4096 / a.P));
+    const int H = a.heads + a.kv_heads, rest = a.keep ? 0 : a.D - 2 * a.P, items = a.P / VP + (int)cdiv(rest, 2 * VP);
+    // IT items a thread, but 512 blocks where the tokens give them; angles of a block: up to 32 KB
+    a.TB = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 * IT / (H * items), cdiv(a.tokens, 512)), 4096 / a.P));
     const dim3 grid = block_lines(cdiv(a.tokens, a.TB));
     const size_t lds = (size_t)a.TB * a.P * sizeof(float2);
-    if (layout == PSERVE_PAIR_HALF) rotary_pairs_kernel<T, true><<<grid, 256, lds, st>>>(a);
-    else rotary_pairs_kernel<T, false><<<grid, 256, lds, st>>>(a);
-    return check_launch("rotary_pairs_kernel");
+    if (layout == PSERVE_PAIR_HALF) rotary_kernel<T, true, VP, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
+    else rotary_kernel<T, false, VP, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
+    return check_launch("rotary_kernel");
+}
+
+// Pieces as wide as the head's layout, the strides and the addresses allow
+template <typename T>
+static int launch_rotary(const RotaryArgs& a, int layout, hipStream_t st) {
+    auto fits = [&](int vp) {
+        const int64_t b = vp * (int64_t)sizeof(T);
+        const int rest = a.keep ? 0 : a.D - 2 * a.P;
+        bool ok = a.P % vp == 0 && rest % vp == 0;
+        auto one = [&](const void* p, const int64_t* s, int n) {
+            ok = ok && !((uintptr_t)p & (b - 1)) && (a.tokens == 1 || s[0] * (int64_t)sizeof(T) % b == 0) && (n == 1 || s[1] * (int64_t)sizeof(T) % b == 0);
+        };
+        one(a.q, a.qs, a.heads);
+        one(a.q_out, a.qo, a.heads);
+        if (a.kv_heads) {
+            one(a.k, a.ks, a.kv_heads);
+            one(a.k_out, a.ko, a.kv_heads);
+        }
+        return ok;
+    };
+    if constexpr (sizeof(T) == 2)
+        if (fits(8)) return launch_rotary_as<T, 8>(a, layout, st);
+    if (fits(4)) return launch_rotary_as<T, 4>(a, layout, st);
+    if (fits(2)) return launch_rotary_as<T, 2>(a, layout, st);
+    return launch_rotary_as<T, 1>(a, layout, st);
 }
 
 // ---- positions of a plan's tokens
