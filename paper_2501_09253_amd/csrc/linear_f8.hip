@@ -225,10 +225,257 @@ static int launch_few(const LinearF8Args& a, hipStream_t st) {
     return check_launch("linear_f8_few_kernel");
 }
 
+// ---- many tiles: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, two stages of a block (128 of K) in LDS.
+// A lane's operand of the 32 x 32 x 64 instruction is two 16-byte chunks of a row, chunk 4 ks + fh and 4 ks + 2 + fh of the block's eight (any
+// order of K within a block does, the same for both operands).  The first operand's rows become the accumulators' rows, so the channels go
+// first, in the order that leaves a lane with eight consecutive channels of one row of x.
+__device__ __forceinline__ int lf_kperm(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+
+template <int WGM, int WGN, int TM, int TN>
+struct LFCfg {
+    static constexpr int NW = WGM * WGN, WM = 32 * TM, WN = 32 * TN, BM = WGM * WM, BN = WGN * WN;
+    static constexpr int STAGE = (BM + BN) * 128;           // bytes
+    static constexpr int LDS = 2 * STAGE;
+    static_assert(STAGE >= NW * 4096, "the output staging (4 KB a wavefront) reuses a stage");
+};
+
+template <typename T, bool RES, bool VEC, int WGM, int WGN, int TM, int TN>
+__global__ void __launch_bounds__(64 * WGM * WGN, 2)
+linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
+    using Cfg = LFCfg<WGM, WGN, TM, TN>;
+    constexpr int NW = Cfg::NW, WM = Cfg::WM, WN = Cfg::WN, BM = Cfg::BM, BN = Cfg::BN;
+    constexpr int RP = 8 * NW, A_LD = BM / RP, B_LD = BN / RP, LD = A_LD + B_LD, STAGE_V = Cfg::STAGE / 16;
+    constexpr int GM = 8;                                   // row tiles of a group, see below
+    extern __shared__ __attribute__((aligned(16))) uint8_t lf_smem[];
+    u32x4* ring = reinterpret_cast<u32x4*>(lf_smem);        // [2][rows of x, rows of w][8 chunks], chunk ^ ((row >> 1) & 7)
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave % WGM, wn = wave / WGM, fr = lane & 31, fh = lane >> 5;
+    const int n_tiles = total / m_tiles, KT = a.Kp / 128;
+
+    // Tiles are numbered in groups of GM row tiles, rows fastest; XCD x (block id mod 8) takes the x-th eighth of the numbers, so
+    // the blocks of an XCD run on neighbouring tiles and share the panels in its L2.
+    const int xcd = blockIdx.x & 7, t_end = (int)((int64_t)total * (xcd + 1) / 8), t_step = gridDim.x >> 3;
+    int t = (int)((int64_t)total * xcd / 8) + (blockIdx.x >> 3);
+    if (t >= t_end) return;
+
+    const int lc = lane & 7, lr = 8 * wave + (lane >> 3), gc = lc ^ ((lr >> 1) & 7);
+    int a_off[A_LD], b_off[B_LD];                           // byte offsets from the tile's first row
+    const uint8_t *a_base, *b_base;
+    const uint8_t *sa[TM], *sb[TN];                         // scales of the lane's rows
+    int64_t m0 = 0;
+    int n0 = 0;
+    auto decode = [&](int tt) {
+        const int grp = tt / (GM * n_tiles), r = tt - grp * (GM * n_tiles), gm = min(GM, m_tiles - grp * GM), nt = r / gm;
+        m0 = (int64_t)(grp * GM + r - nt * gm) * BM;
+        n0 = nt * BN;
+    };
+    const int rowA = wm * WM + fr, rowB = wn * WN + lf_kperm(fr);
+    auto setup = [&]() {
+        a_base = a.x8 + m0 * a.Kp;
+        b_base = a.w8 + (int64_t)n0 * a.Kp;
+        const int last = (int)min((int64_t)BM, a.rows - m0) - 1, lastB = a.Np - 1 - n0;
+#pragma unroll
+        for (int l = 0; l < A_LD; ++l) a_off[l] = min(lr + l * RP, last) * a.Kp + gc * 16;
+#pragma unroll
+        for (int l = 0; l < B_LD; ++l) b_off[l] = min(lr + l * RP, lastB) * a.Kp + gc * 16;
+    };
+    auto scale_rows = [&]() {
+        const int last = (int)min((int64_t)BM, a.rows - m0) - 1, lastB = a.Np - 1 - n0;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sa[i] = a.sx + (m0 + min(rowA + 32 * i, last)) * a.Sp;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sb[j] = a.sw + (int64_t)(n0 + min(rowB + 32 * j, lastB)) * a.Sp;
+    };
+    auto load_stage = [&](int kt, int stage) {
+        u32x4* dst = ring + stage * STAGE_V + wave * 64;
+        const uint8_t *ap = a_base + (int64_t)kt * 128, *bp = b_base + (int64_t)kt * 128;
+#pragma unroll
+        for (int l = 0; l < A_LD; ++l) __builtin_amdgcn_global_load_lds((const void*)(ap + a_off[l]), (lds_void*)(dst + l * (64 * NW)), 16, 0, 0);
+#pragma unroll
+        for (int l = 0; l < B_LD; ++l) __builtin_amdgcn_global_load_lds((const void*)(bp + b_off[l]), (lds_void*)(dst + BM * 8 + l * (64 * NW)), 16, 0, 0);
+    };
+    const u32x4 *pA = ring + rowA * 8, *pB = ring + BM * 8 + rowB * 8;
+    const int swA = (rowA >> 1) & 7, swB = (rowB >> 1) & 7;
+    i32x8 fa[TM], fb[TN];
+    auto fragment = [&](const u32x4* row, int ks, int sw) {
+        const u32x4 lo = row[(4 * ks + fh) ^ sw], hi = row[(4 * ks + 2 + fh) ^ sw];
+        return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
+
+    decode(t);
+    setup();
+    load_stage(0, 0);
+#pragma unroll 1
+    for (;;) {
+        scale_rows();
+        f32x16 acc[TM][TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        int xa[TM], xb[TN];                                 // scale bytes of four blocks
+#pragma unroll 1
+        for (int kt = 0; kt < KT; ++kt) {
+            const int cur = kt & 1;
+            if ((kt & 3) == 0) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) xa[i] = *reinterpret_cast<const int*>(sa[i] + kt);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) xb[j] = *reinterpret_cast<const int*>(sb[j] + kt);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");     // the stage has landed; the other one is read
+            if (kt + 1 < KT) load_stage(kt + 1, cur ^ 1);
+            const u32x4 *ra = pA + cur * STAGE_V, *rb = pB + cur * STAGE_V;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[i] = fragment(ra + i * 256, ks, swA);
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb[j] = fragment(rb + j * 256, ks, swB);
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) {
+                        if constexpr (sizeof(T) == 2) {
+                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, 0, xb[j], 0, xa[i]);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f8_as_bf16(fb[j], q, xb[j] & 255), f8_as_bf16(fa[i], q, xa[i] & 255), acc[i][j], 0, 0, 0);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < TM; ++i) xa[i] = (int)((uint32_t)xa[i] >> 8);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) xb[j] = (int)((uint32_t)xb[j] >> 8);
+        }
+        // ---- output in pieces of 32 rows x 128 bytes, through the second stage
+        const int64_t r0 = m0 + wm * WM;
+        const int c0 = n0 + wn * WN;
+        constexpr int CV = 16 / sizeof(T), PC = 8 * CV;     // values of a 16-byte chunk, columns of a piece
+        constexpr int PJ = PC / 32, NP = TN / PJ;           // accumulator tiles of a piece, pieces of 32 rows
+        const int nt = t + t_step;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // every wavefront has read its last fragments
+        if (nt < t_end) {                                   // the first step of the next tile comes in beside the end of this one
+            decode(nt);
+            setup();
+            load_stage(0, 0);
+        }
+        u32x4* ep = ring + STAGE_V + wave * 256;            // [32 rows][8 chunks], chunk ^ ((row >> 1) & 7)
+        const int er = lane >> 3, ec = lane & 7, sw = (fr >> 1) & 7;
+        // chunk of the lane's 16-byte word q of a piece: words 2 jj + c (bf16), 2 c + h (fp32)
+        auto chunk = [&](int q) { return (sizeof(T) == 2 ? 2 * q + fh : 4 * (q >> 1) + 2 * fh + (q & 1)) ^ sw; };
+        // value `lane % PC` of row r of a piece
+        constexpr int RI = 64 / PC;                         // rows an instruction covers where the rows are off the 16-byte grid
+        auto cell = [&](int r) -> T* { return reinterpret_cast<T*>(ep + r * 8 + (((lane % PC) / CV) ^ ((r >> 1) & 7))) + lane % CV; };
+#pragma unroll
+        for (int p = 0; p < TM * NP; ++p) {
+            const int i = p / NP, jp = p % NP, pcol = c0 + PC * jp;
+            if (pcol >= a.N) continue;
+            const bool in = pcol + lane % PC < a.N;
+            u32x4 rres[4];
+            if constexpr (RES) {                            // the residual as the accumulators lie, through the staging
+                if constexpr (VEC) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int rr = 8 * k + er, n = pcol + CV * ec;
+                        const int64_t row = min(r0 + 32 * i + rr, a.rows - 1);
+                        ep[rr * 8 + (ec ^ ((rr >> 1) & 7))] = *reinterpret_cast<const u32x4*>((const T*)a.res + row * a.N + (n < a.N ? n : 0));
+                    }
+                } else {
+#pragma unroll 8
+                    for (int r = lane / PC; r < 32; r += RI) {
+                        const int64_t row = r0 + 32 * i + r;
+                        *cell(r) = in && row < a.rows ? ((const T*)a.res)[row * a.N + pcol + lane % PC] : T(0);
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) rres[q] = ep[fr * 8 + chunk(q)];
+                __builtin_amdgcn_wave_barrier();
+            }
+#pragma unroll
+            for (int jj = 0; jj < PJ; ++jj)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int n = pcol + 32 * jj + 16 * c + 8 * fh;
+                    float v[8], b[8];
+                    if (a.b && n < a.Np) load8(a.b + n, b);
+                    else
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) b[e] = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] = acc[i][jp * PJ + jj][8 * c + e] + b[e];
+                        if constexpr (RES && sizeof(T) == 2) {
+                            const uint32_t r = rres[2 * jj + c][e / 2];
+                            v[e] += e & 1 ? __uint_as_float(r & 0xffff0000u) : __uint_as_float(r << 16);
+                        } else if constexpr (RES) {
+                            v[e] += __uint_as_float(rres[2 * c + e / 4][e % 4]);
+                        }
+                    }
+                    if constexpr (sizeof(T) == 2) {
+                        ep[fr * 8 + chunk(2 * jj + c)] = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            ep[fr * 8 + chunk(2 * c + h)] = u32x4{__float_as_uint(v[4 * h]), __float_as_uint(v[4 * h + 1]), __float_as_uint(v[4 * h + 2]), __float_as_uint(v[4 * h + 3])};
+                    }
+                }
+            __builtin_amdgcn_wave_barrier();
+            if constexpr (VEC) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int rr = 8 * k + er, n = pcol + CV * ec;
+                    const int64_t row = r0 + 32 * i + rr;
+                    const u32x4 o = ep[rr * 8 + (ec ^ ((rr >> 1) & 7))];
+                    // (past the L2, which holds the panels)
+                    if (row < a.rows && n < a.N) __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>((T*)a.y + row * a.N + n));
+                }
+            } else {
+#pragma unroll 8
+                for (int r = lane / PC; r < 32; r += RI) {
+                    const int64_t row = r0 + 32 * i + r;
+                    if (in && row < a.rows) ((T*)a.y)[row * a.N + pcol + lane % PC] = *cell(r);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+        if (nt >= t_end) break;
+        t = nt;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the staging is done with
+    }
+}
+
+template <typename T, bool RES, bool VEC, int WGM, int WGN, int TM, int TN>
+static int launch_tile_as(const LinearF8Args& a, hipStream_t st) {
+    using Cfg = LFCfg<WGM, WGN, TM, TN>;
+    PS_SET_LDS_ONCE((linear_f8_tile_kernel<T, RES, VEC, WGM, WGN, TM, TN>), Cfg::LDS);
+    const int64_t mt = cdiv(a.rows, Cfg::BM), total = mt * cdiv(a.N, Cfg::BN);
+    const unsigned grid = (unsigned)(8 * cdiv(std::min<int64_t>(total, Cfg::LDS > 80 * 1024 ? 256 : 512), 8));
+    linear_f8_tile_kernel<T, RES, VEC, WGM, WGN, TM, TN><<<grid, 64 * Cfg::NW, Cfg::LDS, st>>>(a, (int)mt, (int)total);
+    return check_launch("linear_f8_tile_kernel");
+}
+template <typename T, bool RES, bool VEC>
+static int launch_tile_vec(const LinearF8Args& a, hipStream_t st) {
+    if (cdiv(a.rows, 256) * cdiv(a.N, 256) >= 256) return launch_tile_as<T, RES, VEC, 4, 2, 2, 4>(a, st);
+    return launch_tile_as<T, RES, VEC, 2, 2, 2, 2>(a, st);
+}
+template <typename T>
+static int launch_tile(const LinearF8Args& a, hipStream_t st) {
+    const bool vec = a.N % (16 / sizeof(T)) == 0 && !(((uintptr_t)a.y | (uintptr_t)a.res) & 15);
+    if (a.res) return vec ? launch_tile_vec<T, true, true>(a, st) : launch_tile_vec<T, true, false>(a, st);
+    return vec ? launch_tile_vec<T, false, true>(a, st) : launch_tile_vec<T, false, false>(a, st);
+}
+
 template <typename T>
 static int product(const LinearF8Args& a, hipStream_t st) {
     if (a.rows <= 32) return launch_few<T, 1, 1>(a, st);
-    return launch_few<T, 2, 2>(a, st);
+    if (cdiv(a.rows, 128) * cdiv(a.N, 128) <= 64) return launch_few<T, 2, 2>(a, st);
+    return launch_tile<T>(a, st);
 }
 
 static int rows_ok(const char* who, int64_t rows, int32_t K) {
