@@ -235,7 +235,8 @@ template <int WGM, int WGN, int TM, int TN>
 struct LFCfg {
     static constexpr int NW = WGM * WGN, WM = 32 * TM, WN = 32 * TN, BM = WGM * WM, BN = WGN * WN;
     static constexpr int STAGE = (BM + BN) * 128;           // bytes
-    static constexpr int LDS = 2 * STAGE;
+    static constexpr int LDS = 2 * STAGE + 2 * 4 * (BM + BN);       // two stages; scales of four blocks, of this group and the next
+    static_assert(64 * NW == BM + BN, "a thread loads the scales of a row");
     static_assert(STAGE >= NW * 4096, "the output staging (4 KB a wavefront) reuses a stage");
 };
 
@@ -261,7 +262,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
     const int lc = lane & 7, lr = 8 * wave + (lane >> 3), gc = lc ^ ((lr >> 1) & 7);
     int a_off[A_LD], b_off[B_LD];                           // byte offsets from the tile's first row
     const uint8_t *a_base, *b_base;
-    const uint8_t *sa[TM], *sb[TN];                         // scales of the lane's rows
+    const uint8_t* s_base;                                  // scales of the thread's row
     int64_t m0 = 0;
     int n0 = 0;
     auto decode = [&](int tt) {
@@ -278,13 +279,11 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
         for (int l = 0; l < A_LD; ++l) a_off[l] = min(lr + l * RP, last) * a.Kp + gc * 16;
 #pragma unroll
         for (int l = 0; l < B_LD; ++l) b_off[l] = min(lr + l * RP, lastB) * a.Kp + gc * 16;
+        s_base = tid < BM ? a.sx + (m0 + min(tid, last)) * a.Sp : a.sw + (int64_t)(n0 + min(tid - BM, lastB)) * a.Sp;
     };
-    auto scale_rows = [&]() {
-        const int last = (int)min((int64_t)BM, a.rows - m0) - 1, lastB = a.Np - 1 - n0;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) sa[i] = a.sx + (m0 + min(rowA + 32 * i, last)) * a.Sp;
-#pragma unroll
-        for (int j = 0; j < TN; ++j) sb[j] = a.sw + (int64_t)(n0 + min(rowB + 32 * j, lastB)) * a.Sp;
+    uint32_t* s_scale = reinterpret_cast<uint32_t*>(lf_smem + 2 * Cfg::STAGE);      // [2][rows of x, rows of w] words of four blocks
+    auto load_scales = [&](int group) {
+        __builtin_amdgcn_global_load_lds((const void*)(s_base + 4 * group), (lds_void*)(s_scale + (group & 1) * (BM + BN) + wave * 64), 4, 0, 0);
     };
     auto load_stage = [&](int kt, int stage) {
         u32x4* dst = ring + stage * STAGE_V + wave * 64;
@@ -296,18 +295,48 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
     };
     const u32x4 *pA = ring + rowA * 8, *pB = ring + BM * 8 + rowB * 8;
     const int swA = (rowA >> 1) & 7, swB = (rowB >> 1) & 7;
-    i32x8 fa[TM], fb[TN];
+    // One load instruction a call, so that the refill of a stage is spread over the matrix instructions behind the barrier that frees it
+    auto load_one = [&](int kt, int stage, int l) {
+        u32x4* dst = ring + stage * STAGE_V + wave * 64;
+        if (l < A_LD) __builtin_amdgcn_global_load_lds((const void*)(a_base + (int64_t)kt * 128 + a_off[l < A_LD ? l : 0]), (lds_void*)(dst + l * (64 * NW)), 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((const void*)(b_base + (int64_t)kt * 128 + b_off[l >= A_LD ? l - A_LD : 0]),
+                                              (lds_void*)(dst + BM * 8 + (l - A_LD) * (64 * NW)), 16, 0, 0);
+    };
+    i32x8 fa[2][TM], fb[TN];
     auto fragment = [&](const u32x4* row, int ks, int sw) {
         const u32x4 lo = row[(4 * ks + fh) ^ sw], hi = row[(4 * ks + 2 + fh) ^ sw];
         return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
+    auto read_a = [&](int stage, int ks, int i) { fa[ks][i] = fragment(pA + stage * STAGE_V + i * 256, ks, swA); };
+    auto read_b = [&](int stage, int ks, int j) { fb[j] = fragment(pB + stage * STAGE_V + j * 256, ks, swB); };
+    int xa[TM], xb[TN], xa_next[TM], xb_next[TN];           // scale bytes of four blocks, and of the next four
+    auto mma = [&](int ks, int i, int j, f32x16& c) {
+        if constexpr (sizeof(T) == 2) {
+            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[ks][i], c, 0, 0, 0, xb[j], 0, xa[i]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f8_as_bf16(fb[j], q, xb[j] & 255), f8_as_bf16(fa[ks][i], q, xa[i] & 255), c, 0, 0, 0);
+        }
+        asm volatile("" : "+v"(c));                         // (it stays here: else the compiler sinks it past the branches around the loads)
+    };
+    constexpr int NM = TM * TN;                             // matrix instructions of half a block
+    constexpr int LPS = (LD + 2 * NM - TM - 1) / (2 * NM - TM);     // loads behind one of them
+
+    auto read_scales = [&](int group, int (&pa)[TM], int (&pb)[TN]) {
+        const uint32_t* p = s_scale + (group & 1) * (BM + BN);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) pa[i] = (int)p[rowA + 32 * i];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) pb[j] = (int)p[BM + rowB + 32 * j];
     };
 
     decode(t);
     setup();
     load_stage(0, 0);
+    load_scales(0);
+    if (KT > 1) load_stage(1, 1);
 #pragma unroll 1
     for (;;) {
-        scale_rows();
         f32x16 acc[TM][TN];
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -315,42 +344,53 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-        int xa[TM], xb[TN];                                 // scale bytes of four blocks
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");           // the first two blocks have landed
+#pragma unroll
+        for (int i = 0; i < TM; ++i) read_a(0, 0, i);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) read_b(0, 0, j);
+        read_scales(0, xa, xb);
 #pragma unroll 1
         for (int kt = 0; kt < KT; ++kt) {
-            const int cur = kt & 1;
-            if ((kt & 3) == 0) {
+            const int cur = kt & 1, nxt = cur ^ 1;
+            const bool refill = kt + 2 < KT, late = kt > 0 && kt + 1 < KT;
+            const bool turn = (kt & 3) == 3;
+            if ((kt & 3) == 0 && kt + 4 < KT) load_scales(kt / 4 + 1);
+            if (turn) read_scales(kt / 4 + 1, xa_next, xb_next);        // (where there is a next group, in three steps' time it has landed)
+            // first half: the second half's operands come in, a channel tile's as soon as its last instruction is out
 #pragma unroll
-                for (int i = 0; i < TM; ++i) xa[i] = *reinterpret_cast<const int*>(sa[i] + kt);
+            for (int q = 0; q < NM; ++q) {
+                const int j = q / TM, i = q % TM, sl = NM - TM + q;
+                mma(0, i, j, acc[i][j]);
+                if (q < TM) read_a(cur, 1, q);
+                if (i == TM - 1) read_b(cur, 1, j);
+                if (late) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j) xb[j] = *reinterpret_cast<const int*>(sb[j] + kt);
+                    for (int l = 0; l < LD; ++l) if (l / LPS == sl) load_one(kt + 1, nxt, l);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");     // the stage has landed; the other one is read
-            if (kt + 1 < KT) load_stage(kt + 1, cur ^ 1);
-            const u32x4 *ra = pA + cur * STAGE_V, *rb = pB + cur * STAGE_V;
+            // second half: behind its first instructions every operand of the stage has been read and the next stage has landed (what is read
+            // behind the last step is not used)
 #pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
+            for (int q = 0; q < NM; ++q) {
+                const int j = q / TM, i = q % TM;
+                mma(1, i, j, acc[i][j]);
+                if (q == TM - 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+                if (q >= TM - 1) {
+                    if (q < 2 * TM - 1) read_a(nxt, 0, q - (TM - 1));
+                    if (i == TM - 1) read_b(nxt, 0, j);
+                    if (refill && q >= TM) {
 #pragma unroll
-                for (int i = 0; i < TM; ++i) fa[i] = fragment(ra + i * 256, ks, swA);
-#pragma unroll
-                for (int j = 0; j < TN; ++j) fb[j] = fragment(rb + j * 256, ks, swB);
-#pragma unroll
-                for (int j = 0; j < TN; ++j)
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) {
-                        if constexpr (sizeof(T) == 2) {
-                            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, 0, xb[j], 0, xa[i]);
-                        } else {
-#pragma unroll
-                            for (int q = 0; q < 4; ++q)
-                                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f8_as_bf16(fb[j], q, xb[j] & 255), f8_as_bf16(fa[i], q, xa[i] & 255), acc[i][j], 0, 0, 0);
-                        }
+                        for (int l = 0; l < LD; ++l) if (l / LPS == q - TM) load_one(kt + 2, cur, l);
                     }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int i = 0; i < TM; ++i) xa[i] = (int)((uint32_t)xa[i] >> 8);
+            for (int i = 0; i < TM; ++i) xa[i] = turn ? xa_next[i] : (int)((uint32_t)xa[i] >> 8);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) xb[j] = (int)((uint32_t)xb[j] >> 8);
+            for (int j = 0; j < TN; ++j) xb[j] = turn ? xb_next[j] : (int)((uint32_t)xb[j] >> 8);
         }
         // ---- output in pieces of 32 rows x 128 bytes, through the second stage
         const int64_t r0 = m0 + wm * WM;
@@ -363,6 +403,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
             decode(nt);
             setup();
             load_stage(0, 0);
+            load_scales(0);
         }
         u32x4* ep = ring + STAGE_V + wave * 256;            // [32 rows][8 chunks], chunk ^ ((row >> 1) & 7)
         const int er = lane >> 3, ec = lane & 7, sw = (fr >> 1) & 7;
@@ -447,6 +488,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
         if (nt >= t_end) break;
         t = nt;
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the staging is done with
+        if (KT > 1) load_stage(1, 1);
     }
 }
 
