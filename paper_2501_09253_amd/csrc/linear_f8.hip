@@ -225,33 +225,43 @@ static int launch_few(const LinearF8Args& a, hipStream_t st) {
     return check_launch("linear_f8_few_kernel");
 }
 
-// ---- many tiles: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, two stages of a block (128 of K) in LDS.
-// A lane's operand of the 32 x 32 x 64 instruction is two 16-byte chunks of a row, chunk 4 ks + fh and 4 ks + 2 + fh of the block's eight (any
-// order of K within a block does, the same for both operands).  The first operand's rows become the accumulators' rows, so the channels go
+// ---- many tiles: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, a ring of NS stages of HB half blocks (64 of K) in LDS.
+// A lane's operand of the 32 x 32 x 64 instruction is two 16-byte chunks of a row, chunks fh and 2 + fh of the half block's four (any order of K
+// within a block does, the same for both operands).  The first operand's rows become the accumulators' rows, so the channels go
 // first, in the order that leaves a lane with eight consecutive channels of one row of x.
 __device__ __forceinline__ int lf_kperm(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
-template <int WGM, int WGN, int TM, int TN>
+// 16 bytes at any element's address
+template <typename T> struct LFAny;
+template <> struct LFAny<uint16_t> { typedef u32x4 __attribute__((aligned(2))) type; };
+template <> struct LFAny<float> { typedef u32x4 __attribute__((aligned(4))) type; };
+
+template <int WGM, int WGN, int TM, int TN, int HB, int NS>
 struct LFCfg {
     static constexpr int NW = WGM * WGN, WM = 32 * TM, WN = 32 * TN, BM = WGM * WM, BN = WGN * WN;
-    static constexpr int STAGE = (BM + BN) * 128;           // bytes
-    static constexpr int LDS = 2 * STAGE + 2 * 4 * (BM + BN);       // two stages; scales of four blocks, of this group and the next
-    static_assert(64 * NW == BM + BN, "a thread loads the scales of a row");
-    static_assert(STAGE >= NW * 4096, "the output staging (4 KB a wavefront) reuses a stage");
+    static constexpr int STAGE = (BM + BN) * 64 * HB;       // bytes
+    static constexpr int LDS = NS * STAGE + 2 * 4 * (BM + BN) + 2 * 4 * BN;      // stages; scales of four blocks, of this group and the next; biases, of this tile and the next
+    static constexpr int PRE = (NS * STAGE - 4096 * NW) / STAGE;    // stages beside the output staging (4 KB a wavefront at the ring's end)
+    static_assert(PRE >= 1, "ring");
+    static_assert(BM % (16 / HB * NW) == 0 && BN % (16 / HB * NW) == 0 && (BM + BN) % 64 == 0, "loads of a stage");
 };
 
-template <typename T, bool RES, bool VEC, int WGM, int WGN, int TM, int TN>
+template <typename T, bool RES, int WGM, int WGN, int TM, int TN, int HB, int NS>
 __global__ void __launch_bounds__(64 * WGM * WGN, 2)
 linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
-    using Cfg = LFCfg<WGM, WGN, TM, TN>;
+    using Cfg = LFCfg<WGM, WGN, TM, TN, HB, NS>;
     constexpr int NW = Cfg::NW, WM = Cfg::WM, WN = Cfg::WN, BM = Cfg::BM, BN = Cfg::BN;
-    constexpr int RP = 8 * NW, A_LD = BM / RP, B_LD = BN / RP, LD = A_LD + B_LD, STAGE_V = Cfg::STAGE / 16;
+    constexpr int CH = 4 * HB, RP = 64 / CH * NW, A_LD = BM / RP, B_LD = BN / RP, LD = A_LD + B_LD, STAGE_V = Cfg::STAGE / 16;
+    constexpr int S_LD = (BM + BN + 64 * NW - 1) / (64 * NW);
+    constexpr bool ALONE = Cfg::LDS > 80 * 1024;            // a block a CU
     constexpr int GM = 8;                                   // row tiles of a group, see below
     extern __shared__ __attribute__((aligned(16))) uint8_t lf_smem[];
-    u32x4* ring = reinterpret_cast<u32x4*>(lf_smem);        // [2][rows of x, rows of w][8 chunks], chunk ^ ((row >> 1) & 7)
+    u32x4* ring = reinterpret_cast<u32x4*>(lf_smem);        // [NS][rows of x, rows of w][CH chunks], swizzled: sixteen rows, all banks
+    uint32_t* s_scale = reinterpret_cast<uint32_t*>(lf_smem + NS * Cfg::STAGE);      // [2][rows of x, rows of w] words of four blocks
+    float* s_bias = reinterpret_cast<float*>(s_scale + 2 * (BM + BN));               // [2][channels]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % WGM, wn = wave / WGM, fr = lane & 31, fh = lane >> 5;
-    const int n_tiles = total / m_tiles, KT = a.Kp / 128;
+    const int n_tiles = total / m_tiles, KT = a.Kp / 128, steps = KT * 2 / HB;
 
     // Tiles are numbered in groups of GM row tiles, rows fastest; XCD x (block id mod 8) takes the x-th eighth of the numbers, so
     // the blocks of an XCD run on neighbouring tiles and share the panels in its L2.
@@ -259,10 +269,10 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
     int t = (int)((int64_t)total * xcd / 8) + (blockIdx.x >> 3);
     if (t >= t_end) return;
 
-    const int lc = lane & 7, lr = 8 * wave + (lane >> 3), gc = lc ^ ((lr >> 1) & 7);
+    auto swizzle = [](int row) { return HB == 1 ? (row >> 2) & 3 : (row >> 1) & 7; };
+    const int lr = 64 / CH * wave + lane / CH, gc = lane % CH ^ swizzle(lr);
     int a_off[A_LD], b_off[B_LD];                           // byte offsets from the tile's first row
-    const uint8_t *a_base, *b_base;
-    const uint8_t* s_base;                                  // scales of the thread's row
+    const uint8_t *a_base, *b_base, *s_base[S_LD];          // (s: scales of the thread's rows)
     int64_t m0 = 0;
     int n0 = 0;
     auto decode = [&](int tt) {
@@ -270,7 +280,6 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
         m0 = (int64_t)(grp * GM + r - nt * gm) * BM;
         n0 = nt * BN;
     };
-    const int rowA = wm * WM + fr, rowB = wn * WN + lf_kperm(fr);
     auto setup = [&]() {
         a_base = a.x8 + m0 * a.Kp;
         b_base = a.w8 + (int64_t)n0 * a.Kp;
@@ -279,49 +288,52 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
         for (int l = 0; l < A_LD; ++l) a_off[l] = min(lr + l * RP, last) * a.Kp + gc * 16;
 #pragma unroll
         for (int l = 0; l < B_LD; ++l) b_off[l] = min(lr + l * RP, lastB) * a.Kp + gc * 16;
-        s_base = tid < BM ? a.sx + (m0 + min(tid, last)) * a.Sp : a.sw + (int64_t)(n0 + min(tid - BM, lastB)) * a.Sp;
+#pragma unroll
+        for (int l = 0; l < S_LD; ++l) {
+            const int r = tid + l * 64 * NW;
+            s_base[l] = r < BM ? a.sx + (m0 + min(r, last)) * a.Sp : a.sw + (int64_t)(n0 + min(r - BM, lastB)) * a.Sp;
+        }
     };
-    uint32_t* s_scale = reinterpret_cast<uint32_t*>(lf_smem + 2 * Cfg::STAGE);      // [2][rows of x, rows of w] words of four blocks
+    int odd = 0;                                            // half of the biases
+    auto load_bias = [&](int half) {
+#pragma unroll
+        for (int c = 0; c < BN; c += 64 * NW)
+            if (a.b && c + 64 * wave < BN)
+                __builtin_amdgcn_global_load_lds((const void*)(a.b + min(n0 + c + tid, a.Np - 1)), (lds_void*)(s_bias + half * BN + c + 64 * wave), 4, 0, 0);
+    };
     auto load_scales = [&](int group) {
-        __builtin_amdgcn_global_load_lds((const void*)(s_base + 4 * group), (lds_void*)(s_scale + (group & 1) * (BM + BN) + wave * 64), 4, 0, 0);
-    };
-    auto load_stage = [&](int kt, int stage) {
-        u32x4* dst = ring + stage * STAGE_V + wave * 64;
-        const uint8_t *ap = a_base + (int64_t)kt * 128, *bp = b_base + (int64_t)kt * 128;
 #pragma unroll
-        for (int l = 0; l < A_LD; ++l) __builtin_amdgcn_global_load_lds((const void*)(ap + a_off[l]), (lds_void*)(dst + l * (64 * NW)), 16, 0, 0);
+        for (int l = 0; l < S_LD; ++l)
+            if (64 * (wave + l * NW) < BM + BN)
+                __builtin_amdgcn_global_load_lds((const void*)(s_base[l] + 4 * group), (lds_void*)(s_scale + (group & 1) * (BM + BN) + 64 * (wave + l * NW)), 4, 0, 0);
+    };
+    // step h of 64 HB of K into stage st.  One load instruction a call, so that a refill is spread over the matrix instructions behind the barrier that frees
+    // its stage
+    auto load_one = [&](int h, int st, int l) {
+        u32x4* dst = ring + st * STAGE_V + wave * 64;
+        if (l < A_LD) __builtin_amdgcn_global_load_lds((const void*)(a_base + (int64_t)h * (64 * HB) + a_off[l < A_LD ? l : 0]), (lds_void*)(dst + l * (64 * NW)), 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((const void*)(b_base + (int64_t)h * (64 * HB) + b_off[l >= A_LD ? l - A_LD : 0]),
+                                              (lds_void*)(dst + BM * CH + (l - A_LD) * (64 * NW)), 16, 0, 0);
+    };
+    auto load_stage = [&](int h, int st) {
 #pragma unroll
-        for (int l = 0; l < B_LD; ++l) __builtin_amdgcn_global_load_lds((const void*)(bp + b_off[l]), (lds_void*)(dst + BM * 8 + l * (64 * NW)), 16, 0, 0);
+        for (int l = 0; l < LD; ++l) load_one(h, st, l);
     };
-    const u32x4 *pA = ring + rowA * 8, *pB = ring + BM * 8 + rowB * 8;
-    const int swA = (rowA >> 1) & 7, swB = (rowB >> 1) & 7;
-    // One load instruction a call, so that the refill of a stage is spread over the matrix instructions behind the barrier that frees it
-    auto load_one = [&](int kt, int stage, int l) {
-        u32x4* dst = ring + stage * STAGE_V + wave * 64;
-        if (l < A_LD) __builtin_amdgcn_global_load_lds((const void*)(a_base + (int64_t)kt * 128 + a_off[l < A_LD ? l : 0]), (lds_void*)(dst + l * (64 * NW)), 16, 0, 0);
-        else __builtin_amdgcn_global_load_lds((const void*)(b_base + (int64_t)kt * 128 + b_off[l >= A_LD ? l - A_LD : 0]),
-                                              (lds_void*)(dst + BM * 8 + (l - A_LD) * (64 * NW)), 16, 0, 0);
-    };
+    const int rowA = wm * WM + fr, rowB = wn * WN + lf_kperm(fr);
+    const u32x4 *pA[2 * HB], *pB[2 * HB];                   // the lane's chunks of a stage's first row tiles
+#pragma unroll
+    for (int c = 0; c < 2 * HB; ++c) {
+        pA[c] = ring + rowA * CH + ((2 * c + fh) ^ swizzle(rowA));
+        pB[c] = ring + (BM + rowB) * CH + ((2 * c + fh) ^ swizzle(rowB));
+    }
     i32x8 fa[2][TM], fb[TN];
-    auto fragment = [&](const u32x4* row, int ks, int sw) {
-        const u32x4 lo = row[(4 * ks + fh) ^ sw], hi = row[(4 * ks + 2 + fh) ^ sw];
+    auto fragment = [&](const u32x4* p, const u32x4* q, int at) {
+        const u32x4 lo = p[at], hi = q[at];
         return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
     };
-    auto read_a = [&](int stage, int ks, int i) { fa[ks][i] = fragment(pA + stage * STAGE_V + i * 256, ks, swA); };
-    auto read_b = [&](int stage, int ks, int j) { fb[j] = fragment(pB + stage * STAGE_V + j * 256, ks, swB); };
+    auto read_a = [&](int set, int st, int half, int i) { fa[set][i] = fragment(pA[2 * half], pA[2 * half + 1], st * STAGE_V + i * 32 * CH); };
+    auto read_b = [&](int st, int half, int j) { fb[j] = fragment(pB[2 * half], pB[2 * half + 1], st * STAGE_V + j * 32 * CH); };
     int xa[TM], xb[TN], xa_next[TM], xb_next[TN];           // scale bytes of four blocks, and of the next four
-    auto mma = [&](int ks, int i, int j, f32x16& c) {
-        if constexpr (sizeof(T) == 2) {
-            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[ks][i], c, 0, 0, 0, xb[j], 0, xa[i]);
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f8_as_bf16(fb[j], q, xb[j] & 255), f8_as_bf16(fa[ks][i], q, xa[i] & 255), c, 0, 0, 0);
-        }
-        asm volatile("" : "+v"(c));                         // (it stays here: else the compiler sinks it past the branches around the loads)
-    };
-    constexpr int NM = TM * TN;                             // matrix instructions of half a block
-    constexpr int LPS = (LD + 2 * NM - TM - 1) / (2 * NM - TM);     // loads behind one of them
-
     auto read_scales = [&](int group, int (&pa)[TM], int (&pb)[TN]) {
         const uint32_t* p = s_scale + (group & 1) * (BM + BN);
 #pragma unroll
@@ -329,12 +341,34 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
 #pragma unroll
         for (int j = 0; j < TN; ++j) pb[j] = (int)p[BM + rowB + 32 * j];
     };
+    auto mma = [&](int set, int i, int j, f32x16& c) {
+        if constexpr (sizeof(T) == 2) {
+            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[set][i], c, 0, 0, 0, xb[j], 0, xa[i]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f8_as_bf16(fb[j], q, xb[j] & 255), f8_as_bf16(fa[set][i], q, xa[i] & 255), c, 0, 0, 0);
+        }
+        asm volatile("" : "+v"(c));                         // (it stays here: else the compiler sinks it past the branches around the loads)
+    };
+    constexpr int NM = TM * TN;                             // matrix instructions of half a block
+    constexpr int SLOTS = HB == 1 ? NM - TM : 2 * NM - TM, LPS = (LD + SLOTS - 1) / SLOTS;      // of them with loads behind, loads behind one
 
+    // Blocks in step, one a CU, all write their outputs at the same time, with the matrix cores idle, and multiply at the same time, with memory idle.  Where
+    // the tiles do not come out even, the blocks that have one less therefore begin later, by about the time that an output takes (12,544 x 1536 x 6144 with
+    // a residual 155 -> 149 us, x 4608 99 -> 91).
+    const int share = t_end - (int)((int64_t)total * xcd / 8);          // tiles of the XCD
+    if (ALONE && share > t_step && (int)(blockIdx.x >> 3) >= share % t_step && share % t_step != 0)
+        for (int d = min(16, KT * 4 / 3); d > 0; --d) __builtin_amdgcn_s_sleep(16);      // 1024 cycles
     decode(t);
     setup();
     load_stage(0, 0);
     load_scales(0);
-    if (KT > 1) load_stage(1, 1);
+    load_bias(0);
+    if (!a.b)
+        for (int c = tid; c < 2 * BN; c += 64 * NW) s_bias[c] = 0.f;
+#pragma unroll
+    for (int st = 1; st < NS; ++st)
+        if (st < steps) load_stage(st, st);
 #pragma unroll 1
     for (;;) {
         f32x16 acc[TM][TN];
@@ -344,118 +378,139 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
             for (int j = 0; j < TN; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");           // the first two blocks have landed
+        if (steps >= NS) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 1) * LD) : "memory");       // the first step has landed
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-        for (int i = 0; i < TM; ++i) read_a(0, 0, i);
+        for (int i = 0; i < TM; ++i) read_a(0, 0, 0, i);
 #pragma unroll
         for (int j = 0; j < TN; ++j) read_b(0, 0, j);
         read_scales(0, xa, xb);
+        int cur = 0;                                        // stage of this step
 #pragma unroll 1
         for (int kt = 0; kt < KT; ++kt) {
-            const int cur = kt & 1, nxt = cur ^ 1;
-            const bool refill = kt + 2 < KT, late = kt > 0 && kt + 1 < KT;
             const bool turn = (kt & 3) == 3;
-            if ((kt & 3) == 0 && kt + 4 < KT) load_scales(kt / 4 + 1);
-            if (turn) read_scales(kt / 4 + 1, xa_next, xb_next);        // (where there is a next group, in three steps' time it has landed)
-            // first half: the second half's operands come in, a channel tile's as soon as its last instruction is out
 #pragma unroll
-            for (int q = 0; q < NM; ++q) {
-                const int j = q / TM, i = q % TM, sl = NM - TM + q;
-                mma(0, i, j, acc[i][j]);
-                if (q < TM) read_a(cur, 1, q);
-                if (i == TM - 1) read_b(cur, 1, j);
-                if (late) {
+            for (int ks = 0; ks < 2; ++ks) {
+                // The step's last half: behind its first instructions every operand of the stage is read and the next step has landed (behind that are
+                // the loads of those after it, where there are any; scales' loads among them only make the wait longer).  The stage is refilled behind
+                // the instructions that follow, up to the next step's last half.  What is read behind the last step is not used
+                const bool last = HB == 1 || ks == 1;
+                const int h = HB == 1 ? 2 * kt + ks : kt, nxt = cur == NS - 1 ? 0 : cur + 1, prv = cur == 0 ? NS - 1 : cur - 1;
+                const bool refill = h + NS < steps, late = h > 0 && h - 1 + NS < steps;
 #pragma unroll
-                    for (int l = 0; l < LD; ++l) if (l / LPS == sl) load_one(kt + 1, nxt, l);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            // second half: behind its first instructions every operand of the stage has been read and the next stage has landed (what is read
-            // behind the last step is not used)
+                for (int q = 0; q < NM; ++q) {
+                    const int j = q / TM, i = q % TM;
+                    mma(ks, i, j, acc[i][j]);
+                    if (last) {
+                        if (q == TM - 1) {
+                            if (NS > 2 && h + NS <= steps) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NS - 2) * LD) : "memory");
+                            else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+                        }
+                        if (q >= TM - 1) {
+                            if (q < 2 * TM - 1) read_a(ks ^ 1, nxt, 0, q - (TM - 1));
+                            if (i == TM - 1) read_b(nxt, 0, j);
+                            if (refill && q >= TM) {
 #pragma unroll
-            for (int q = 0; q < NM; ++q) {
-                const int j = q / TM, i = q % TM;
-                mma(1, i, j, acc[i][j]);
-                if (q == TM - 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-                if (q >= TM - 1) {
-                    if (q < 2 * TM - 1) read_a(nxt, 0, q - (TM - 1));
-                    if (i == TM - 1) read_b(nxt, 0, j);
-                    if (refill && q >= TM) {
+                                for (int l = 0; l < LD; ++l) if (l / LPS == q - TM) load_one(h + NS, cur, l);
+                            }
+                        }
+                    } else {
+                        if (q < TM) read_a(1, cur, HB - 1, q);
+                        if (i == TM - 1) read_b(cur, HB - 1, j);
+                        if (late) {
 #pragma unroll
-                        for (int l = 0; l < LD; ++l) if (l / LPS == q - TM) load_one(kt + 2, cur, l);
+                            for (int l = 0; l < LD; ++l) if (l / LPS == NM - TM + q) load_one(h - 1 + NS, prv, l);
+                        }
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if (last) cur = nxt;
             }
+            if ((kt & 3) == 0 && kt + 4 < KT) load_scales(kt / 4 + 1);
+            if ((kt & 3) == 2) read_scales(kt / 4 + 1, xa_next, xb_next);       // (where there is a next group, two blocks later it has landed)
 #pragma unroll
             for (int i = 0; i < TM; ++i) xa[i] = turn ? xa_next[i] : (int)((uint32_t)xa[i] >> 8);
 #pragma unroll
             for (int j = 0; j < TN; ++j) xb[j] = turn ? xb_next[j] : (int)((uint32_t)xb[j] >> 8);
         }
-        // ---- output in pieces of 32 rows x 128 bytes, through the second stage
+        // ---- output in pieces of 32 rows x 128 bytes, through the end of the ring
         const int64_t r0 = m0 + wm * WM;
         const int c0 = n0 + wn * WN;
         constexpr int CV = 16 / sizeof(T), PC = 8 * CV;     // values of a 16-byte chunk, columns of a piece
-        constexpr int PJ = PC / 32, NP = TN / PJ;           // accumulator tiles of a piece, pieces of 32 rows
-        const int nt = t + t_step;
+        constexpr int PJ = PC / 32, NP = TN / PJ, PS = TM * NP, RQ = RES ? (PS < 4 ? PS : 4) : 1;      // accumulator tiles of a piece; pieces of 32 rows, of all; residuals under way
+        const int nt = t + t_step, er = lane >> 3, ec = lane & 7;
+        // whole lines go past the L2, which holds the panels; where rows begin inside a line, its parts meet there
+        const bool lines = a.N % (8 * CV) == 0 && !((uintptr_t)a.y & 127);
+        typedef typename LFAny<T>::type Any;
+        u32x4 rres[RQ][4];
+        // the residual of piece p, eight whole lines an instruction
+        auto res_load = [&](int p) {
+            const int n = c0 + PC * (p % NP) + CV * ec;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t row = r0 + 32 * (p / NP) + 8 * k + er;
+                const T* rp = (const T*)a.res + row * a.N + n;
+                u32x4 v = {0, 0, 0, 0};
+                if (row < a.rows) {
+                    if (n + CV <= a.N) v = *reinterpret_cast<const Any*>(rp);
+                    else if (n < a.N) {
+                        T e[CV];
+#pragma unroll
+                        for (int c = 0; c < CV; ++c) e[c] = n + c < a.N ? rp[c] : T(0);
+                        __builtin_memcpy(&v, e, sizeof v);
+                    }
+                }
+                rres[p % RQ][k] = v;
+            }
+        };
+        if constexpr (RES) {
+#pragma unroll
+            for (int p = 0; p < RQ; ++p) res_load(p);
+        }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // every wavefront has read its last fragments
-        if (nt < t_end) {                                   // the first step of the next tile comes in beside the end of this one
+        if (nt < t_end) {                                   // the first steps of the next tile come in beside the end of this one
             decode(nt);
             setup();
             load_stage(0, 0);
             load_scales(0);
+            load_bias(odd ^ 1);
+#pragma unroll
+            for (int st = 1; st < Cfg::PRE; ++st)
+                if (st < steps) load_stage(st, st);
         }
-        u32x4* ep = ring + STAGE_V + wave * 256;            // [32 rows][8 chunks], chunk ^ ((row >> 1) & 7)
-        const int er = lane >> 3, ec = lane & 7, sw = (fr >> 1) & 7;
+        const float* bias = s_bias + odd * BN + wn * WN + 8 * fh;
+        u32x4* ep = ring + NS * STAGE_V - NW * 256 + wave * 256;        // [32 rows][8 chunks], chunk ^ ((row >> 1) & 7)
+        const int sw = (fr >> 1) & 7;
         // chunk of the lane's 16-byte word q of a piece: words 2 jj + c (bf16), 2 c + h (fp32)
         auto chunk = [&](int q) { return (sizeof(T) == 2 ? 2 * q + fh : 4 * (q >> 1) + 2 * fh + (q & 1)) ^ sw; };
-        // value `lane % PC` of row r of a piece
-        constexpr int RI = 64 / PC;                         // rows an instruction covers where the rows are off the 16-byte grid
-        auto cell = [&](int r) -> T* { return reinterpret_cast<T*>(ep + r * 8 + (((lane % PC) / CV) ^ ((r >> 1) & 7))) + lane % CV; };
 #pragma unroll
-        for (int p = 0; p < TM * NP; ++p) {
+        for (int p = 0; p < PS; ++p) {
             const int i = p / NP, jp = p % NP, pcol = c0 + PC * jp;
             if (pcol >= a.N) continue;
-            const bool in = pcol + lane % PC < a.N;
-            u32x4 rres[4];
+            u32x4 beside[4];
             if constexpr (RES) {                            // the residual as the accumulators lie, through the staging
-                if constexpr (VEC) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int rr = 8 * k + er, n = pcol + CV * ec;
-                        const int64_t row = min(r0 + 32 * i + rr, a.rows - 1);
-                        ep[rr * 8 + (ec ^ ((rr >> 1) & 7))] = *reinterpret_cast<const u32x4*>((const T*)a.res + row * a.N + (n < a.N ? n : 0));
-                    }
-                } else {
-#pragma unroll 8
-                    for (int r = lane / PC; r < 32; r += RI) {
-                        const int64_t row = r0 + 32 * i + r;
-                        *cell(r) = in && row < a.rows ? ((const T*)a.res)[row * a.N + pcol + lane % PC] : T(0);
-                    }
-                }
+                for (int k = 0; k < 4; ++k) ep[(8 * k + er) * 8 + (ec ^ (((8 * k + er) >> 1) & 7))] = rres[p % RQ][k];
+                if (p + RQ < PS) res_load(p + RQ);
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int q = 0; q < 4; ++q) rres[q] = ep[fr * 8 + chunk(q)];
+                for (int q = 0; q < 4; ++q) beside[q] = ep[fr * 8 + chunk(q)];
                 __builtin_amdgcn_wave_barrier();
             }
 #pragma unroll
             for (int jj = 0; jj < PJ; ++jj)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    const int n = pcol + 32 * jj + 16 * c + 8 * fh;
                     float v[8], b[8];
-                    if (a.b && n < a.Np) load8(a.b + n, b);
-                    else
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) b[e] = 0.f;
+                    load8(bias + PC * jp + 32 * jj + 16 * c, b);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         v[e] = acc[i][jp * PJ + jj][8 * c + e] + b[e];
                         if constexpr (RES && sizeof(T) == 2) {
-                            const uint32_t r = rres[2 * jj + c][e / 2];
+                            const uint32_t r = beside[2 * jj + c][e / 2];
                             v[e] += e & 1 ? __uint_as_float(r & 0xffff0000u) : __uint_as_float(r << 16);
                         } else if constexpr (RES) {
-                            v[e] += __uint_as_float(rres[2 * c + e / 4][e % 4]);
+                            v[e] += __uint_as_float(beside[2 * c + e / 4][e % 4]);
                         }
                     }
                     if constexpr (sizeof(T) == 2) {
@@ -467,56 +522,67 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
                     }
                 }
             __builtin_amdgcn_wave_barrier();
-            if constexpr (VEC) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int rr = 8 * k + er, n = pcol + CV * ec;
-                    const int64_t row = r0 + 32 * i + rr;
-                    const u32x4 o = ep[rr * 8 + (ec ^ ((rr >> 1) & 7))];
-                    // (past the L2, which holds the panels)
-                    if (row < a.rows && n < a.N) __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>((T*)a.y + row * a.N + n));
-                }
-            } else {
-#pragma unroll 8
-                for (int r = lane / PC; r < 32; r += RI) {
-                    const int64_t row = r0 + 32 * i + r;
-                    if (in && row < a.rows) ((T*)a.y)[row * a.N + pcol + lane % PC] = *cell(r);
+            for (int k = 0; k < 4; ++k) {
+                const int rr = 8 * k + er, n = pcol + CV * ec;
+                const int64_t row = r0 + 32 * i + rr;
+                const u32x4 o = ep[rr * 8 + (ec ^ ((rr >> 1) & 7))];
+                T* yp = (T*)a.y + row * a.N + n;
+                if (row < a.rows && n + CV <= a.N) {
+                    if (lines) __builtin_nontemporal_store(o, reinterpret_cast<Any*>(yp));
+                    else *reinterpret_cast<Any*>(yp) = o;
+                } else if (row < a.rows) {
+                    T e[CV];
+                    __builtin_memcpy(e, &o, sizeof o);
+#pragma unroll
+                    for (int c = 0; c < CV; ++c)
+                        if (n + c < a.N) yp[c] = e[c];
                 }
             }
             __builtin_amdgcn_wave_barrier();
         }
         if (nt >= t_end) break;
         t = nt;
+        odd ^= 1;
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the staging is done with
-        if (KT > 1) load_stage(1, 1);
+#pragma unroll
+        for (int st = Cfg::PRE; st < NS; ++st)
+            if (st < steps) load_stage(st, st);
     }
 }
 
-template <typename T, bool RES, bool VEC, int WGM, int WGN, int TM, int TN>
+template <typename T, bool RES, int WGM, int WGN, int TM, int TN, int HB, int NS>
 static int launch_tile_as(const LinearF8Args& a, hipStream_t st) {
-    using Cfg = LFCfg<WGM, WGN, TM, TN>;
-    PS_SET_LDS_ONCE((linear_f8_tile_kernel<T, RES, VEC, WGM, WGN, TM, TN>), Cfg::LDS);
+    using Cfg = LFCfg<WGM, WGN, TM, TN, HB, NS>;
+    PS_SET_LDS_ONCE((linear_f8_tile_kernel<T, RES, WGM, WGN, TM, TN, HB, NS>), Cfg::LDS);
     const int64_t mt = cdiv(a.rows, Cfg::BM), total = mt * cdiv(a.N, Cfg::BN);
     const unsigned grid = (unsigned)(8 * cdiv(std::min<int64_t>(total, Cfg::LDS > 80 * 1024 ? 256 : 512), 8));
-    linear_f8_tile_kernel<T, RES, VEC, WGM, WGN, TM, TN><<<grid, 64 * Cfg::NW, Cfg::LDS, st>>>(a, (int)mt, (int)total);
+    linear_f8_tile_kernel<T, RES, WGM, WGN, TM, TN, HB, NS><<<grid, 64 * Cfg::NW, Cfg::LDS, st>>>(a, (int)mt, (int)total);
     return check_launch("linear_f8_tile_kernel");
 }
-template <typename T, bool RES, bool VEC>
-static int launch_tile_vec(const LinearF8Args& a, hipStream_t st) {
-    if (cdiv(a.rows, 256) * cdiv(a.N, 256) >= 256) return launch_tile_as<T, RES, VEC, 4, 2, 2, 4>(a, st);
-    return launch_tile_as<T, RES, VEC, 2, 2, 2, 2>(a, st);
+// Of the tiles the one with the least time by its rounds (256 blocks at a time of the largest tile, 512 of the others), us a round: so much for each
+// block of K and so much for its beginning and end, fitted to 4096 .. 16384 rows (256 x 256 / 128 x 128 / 64 x 128 us, bf16): 12,544 x 1536 x 6144 with
+// a residual 158 / 164 / 197, 12,544 x 6144 x 1536 with one 164 / 144 / 177, 2048 x 4096 x 4096 46 / 36 / 45, 3000 x 3000 x 3000 37 / 43 / 41,
+// 2048 x 2048 x 2048 29 / 17 / 14, 100 x 2048 x 8192 25 / 13 / 9, 6000 x 1000 x 3000 with a residual 53 / 40 / 43; fp32: 8000 x 500 x 1500 with one 64 / 37 / 36 (the
+// largest tile's operands spill there, and it is left out), 500 x 3000 x 2000 68 / 26 / 19
+template <typename T, bool RES>
+static int launch_tile_res(const LinearF8Args& a, hipStream_t st) {
+    constexpr bool HALF = sizeof(T) == 2;
+    const double KT = a.Kp / 128;
+    auto cost = [&](int bm, int bn, int at_once, double step, double ends) { return (double)cdiv(cdiv(a.rows, bm) * cdiv(a.N, bn), at_once) * (step * KT + ends); };
+    const double small = HALF ? cost(64, 128, 512, 0.64, RES ? 4.5 : 4.0) : cost(64, 128, 512, 1.05, 7.5);
+    const double mid = HALF ? cost(128, 128, 512, 1.06, RES ? 6.0 : 5.0) : cost(128, 128, 512, 1.85, 13.0);
+    if constexpr (HALF)
+        if (cost(256, 256, 256, 1.5, RES ? 14.0 : 11.0) <= std::min(mid, small)) return launch_tile_as<T, RES, 4, 2, 2, 4, 1, 4>(a, st);
+    if (mid <= small) return launch_tile_as<T, RES, 2, 2, 2, 2, 2, 2>(a, st);
+    return launch_tile_as<T, RES, 2, 2, 1, 2, 2, 3>(a, st);
 }
 template <typename T>
-static int launch_tile(const LinearF8Args& a, hipStream_t st) {
-    const bool vec = a.N % (16 / sizeof(T)) == 0 && !(((uintptr_t)a.y | (uintptr_t)a.res) & 15);
-    if (a.res) return vec ? launch_tile_vec<T, true, true>(a, st) : launch_tile_vec<T, true, false>(a, st);
-    return vec ? launch_tile_vec<T, false, true>(a, st) : launch_tile_vec<T, false, false>(a, st);
-}
+static int launch_tile(const LinearF8Args& a, hipStream_t st) { return a.res ? launch_tile_res<T, true>(a, st) : launch_tile_res<T, false>(a, st); }
 
 template <typename T>
 static int product(const LinearF8Args& a, hipStream_t st) {
     if (a.rows <= 32) return launch_few<T, 1, 1>(a, st);
-    if (cdiv(a.rows, 128) * cdiv(a.N, 128) <= 64) return launch_few<T, 2, 2>(a, st);
     return launch_tile<T>(a, st);
 }
 

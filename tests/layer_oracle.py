@@ -129,26 +129,26 @@ def f8_held(x):
     return code.reshape(rows, Kp).to(torch.uint8), (e + 127).view(rows, -1).to(torch.uint8), held.reshape(rows, Kp)[:, :K].contiguous()
 
 
-def linear_f8(x, w, b, res, dtype):
+def linear_f8(x, w, b, res, dtype, device="cpu"):
     """(y, bound, size) of the layer: bound of every element's error, rounding included; size: magnitudes of the products, summed.
     bf16: of eight products of neighbouring K each loses less than 2^-13 of the largest, with numbers below the format's normal ones counting as the
     smallest of those.  Sums add (K / 16 + 32) times up to 2 U (the instruction cuts off) of the magnitudes summed."""
-    hx, hw = f8_held(x)[2], f8_held(w.t().contiguous())[2]
+    hx, hw = f8_held(x)[2].to(device), f8_held(w.t().contiguous())[2].to(device)
     K = hx.shape[1]
     main, size = hx @ hw.t(), hx.abs() @ hw.abs().t()
     bound = (K / 16 + 32) * 2 * U * size
     if dtype == torch.bfloat16:
         def largest(h, src):
-            scale = f8_held(src)[1].double() - 127
+            scale = f8_held(src)[1].double().to(device) - 127
             low = (2.0 ** (scale - 6)).repeat_interleave(128, 1)
-            v = torch.zeros((h.shape[0], low.shape[1]), dtype=torch.float64)
+            v = torch.zeros((h.shape[0], low.shape[1]), dtype=torch.float64, device=device)
             v[:, :K] = h.abs()
             return torch.maximum(v, low).view(h.shape[0], -1, 8).amax(-1)
         bound = bound + 8 * 2.0 ** -13 * (largest(hx, x) @ largest(hw, w.t().contiguous()).t())
     want = main.clone()
     for t in (b, res):
         if t is not None:
-            want = want + t.double().cpu()
-            size = size + t.double().cpu().abs()
+            want = want + t.double().to(device)
+            size = size + t.double().to(device).abs()
     bound = bound + 2 * U * size + HALF[dtype] * want.abs() + 1e-37
     return want, bound, size

@@ -88,6 +88,24 @@ def test_against_64_bits(rows, K, N, dtype):
     check(layer.forward(held, res=res.cuda()), x, w, b, res)
 
 
+@pytest.mark.parametrize("rows,K,N", [(3000, 500, 3000), (3001, 130, 2999), (8000, 500, 4001), (9600, 1300, 4000), (16384, 300, 1000), (1, 700, 100000), (70000, 64, 96)])
+def test_large_layers(rows, K, N):
+    """Large tiles, several to a block, with and without edges; the reference's products on the GPU in 64 bits."""
+    x, w = make(1, (rows, K), torch.bfloat16) * torch.logspace(-3, 3, rows)[:, None].to(torch.bfloat16), make(2, (K, N), torch.bfloat16, K ** -0.5)
+    b, res = make(3, (N,), torch.bfloat16), make(4, (rows, N), torch.bfloat16)
+    want, tol, _ = lo.linear_f8(x, w, b, res, torch.bfloat16, "cuda")
+    layer = ps.LinearF8(w.cuda(), b.cuda(), ps.BF16)
+    got = layer.forward(x.cuda(), res=res.cuda())
+    assert torch.all((got.double() - want).abs() <= tol)
+    rows8 = ps.RowsF8(rows, K).write(x.cuda())
+    again = torch.full((rows, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    for _ in range(3):                                                  # the same sums in the same order, whatever the blocks' pace
+        layer.forward(rows8, res=res.cuda(), y=again)
+        assert torch.equal(again, got)
+    want, tol, _ = lo.linear_f8(x, w, b, None, torch.bfloat16, "cuda")
+    assert torch.all((layer.forward(rows8).double() - want).abs() <= tol)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [1, 40, 200])
 def test_one_key_is_seen(rows, dtype):
