@@ -125,71 +125,125 @@ static int launch_rows_write(const void* x, int64_t ldx, int64_t rows, int32_t K
     return check_launch("f8_rows_write_kernel");
 }
 
-// ---- the product: 16 MT rows x 16 NT channels, eight wavefronts that share K and read their operands from memory (a lane 32 bytes of a
-// row's block), the next block's in flight; the sums meet in LDS, in a fixed order
-template <typename T, int MT, int NT>
-__global__ void __launch_bounds__(512)
-linear_f8_few_kernel(LinearF8Args a, int m_tiles) {
-    constexpr int BM = 16 * MT, BN = 16 * NT, RS = BN + 4, WV = 8;      // RS: values of a row in LDS
+// 16 bytes at any element's address
+template <typename T> struct LFAny;
+template <> struct LFAny<uint16_t> { typedef u32x4 __attribute__((aligned(2))) type; };
+template <> struct LFAny<float> { typedef u32x4 __attribute__((aligned(4))) type; };
+
+// ---- few rows: 16 MT rows x 16 NT channels, WV wavefronts that share K and read their operands from memory (a lane 32 values of a row's
+// block, 16 g4 .. + 15 and 64 + 16 g4 .. + 15), the next block's in flight; the sums meet in LDS, in a fixed order.  FROM_X: rows of x are rounded on the way
+// in, by every block for itself (a row's block of 128 is four lanes).
+
+// v of the lanes with the same number mod 16: their largest, in all of them
+__device__ __forceinline__ uint32_t f8_column_max(uint32_t m) {
+    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+    return max(m, (uint32_t)__shfl_xor((int)m, 32));
+}
+template <typename T, int MT, int NT, int WV, bool FROM_X>
+__global__ void __launch_bounds__(64 * WV)
+linear_f8_few_kernel(LinearF8Args a) {
+    constexpr int BM = 16 * MT, BN = 16 * NT, RS = BN + 4;              // RS: values of a row in LDS
     __shared__ __attribute__((aligned(16))) float s_sum[WV][BM * RS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4;
-    const int64_t m0 = (int64_t)(blockIdx.x % m_tiles) * BM;
-    const int n0 = (int)(blockIdx.x / m_tiles) * BN;
+    const int n0 = blockIdx.x * BN;
     const int KT = a.Kp / 128;                                          // blocks, dealt to the wavefronts in shares
     const int per = (KT + WV - 1) / WV, k0 = min(KT, wave * per), k1 = min(KT, k0 + per);
-    const uint8_t *wp[NT], *xp[MT], *wsp[NT], *xsp[MT];
+    const uint8_t *wp[NT], *wsp[NT], *xp[MT], *xsp[MT];
+    const T* xv[MT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-        const int64_t n = min(n0 + 16 * j + col, a.Np - 1);
-        wp[j] = a.w8 + n * a.Kp + 32 * g4;
-        wsp[j] = a.sw + n * a.Sp;
+        wp[j] = a.w8 + (int64_t)(n0 + 16 * j + col) * a.Kp + 16 * g4;  // (there are N rounded up to 256)
+        wsp[j] = a.sw + (int64_t)(n0 + 16 * j + col) * a.Sp;
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t r = min(m0 + 16 * i + col, a.rows - 1);
-        xp[i] = a.x8 + r * a.Kp + 32 * g4;
-        xsp[i] = a.sx + r * a.Sp;
+        const int64_t r = min((int64_t)(16 * i + col), a.rows - 1);
+        if constexpr (FROM_X) {
+            xv[i] = (const T*)a.x + r * a.ldx;
+        } else {
+            xp[i] = a.x8 + r * a.Kp + 16 * g4;
+            xsp[i] = a.sx + r * a.Sp;
+        }
     }
+    typedef typename LFAny<T>::type Any;
     f32x4 acc[MT][NT];
-    i32x8 w[2][NT], x[2][MT];
-    int ws[2][NT], xs[2][MT];
+    i32x8 w[2][NT], x[FROM_X ? 1 : 2][MT];
+    Raw8<T> raw[FROM_X ? 2 : 1][MT][4];
+    int ws[2][NT], xs[FROM_X ? 1 : 2][MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto operand = [&](const uint8_t* p) {
+        const u32x4 lo = *reinterpret_cast<const u32x4*>(p), hi = *reinterpret_cast<const u32x4*>(p + 64);
+        return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+    };
     auto load = [&](int set, int k) {
-        k = min(k, KT - 1);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            w[set][j] = *reinterpret_cast<const i32x8*>(wp[j] + (int64_t)k * 128);
+            w[set][j] = operand(wp[j] + (int64_t)k * 128);
             ws[set][j] = wsp[j][k];
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            x[set][i] = *reinterpret_cast<const i32x8*>(xp[i] + (int64_t)k * 128);
-            xs[set][i] = xsp[i][k];
+            if constexpr (FROM_X) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int at = 128 * k + 64 * (c >> 1) + 16 * g4 + 8 * (c & 1);
+                    Raw8<T>& r = raw[set][i][c];
+                    if (at + 8 <= a.K) {
+#pragma unroll
+                        for (int h = 0; h < (int)sizeof(T) / 2; ++h) r.w[h] = *reinterpret_cast<const Any*>(xv[i] + at + h * (16 / sizeof(T)));
+                    } else {
+                        T v[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = at + e < a.K ? xv[i][at + e] : T(0);
+                        __builtin_memcpy(&r, v, sizeof r);
+                    }
+                }
+            } else {
+                x[set][i] = operand(xp[i] + (int64_t)k * 128);
+                xs[set][i] = xsp[i][k];
+            }
         }
     };
     auto mma = [&](int set) {
+        const int from = FROM_X ? 0 : set;
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = 0; i < MT; ++i) {
+            if constexpr (FROM_X) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) m = largest8(m, raw[set][i][c]);
+                const F8Scale z(f8_column_max(m));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float v[8];
+                    values8(raw[set][i][c], v);
+                    const q8_u32x2 p = z.pack8(v);
+                    x[0][i][2 * c] = (int)p[0];
+                    x[0][i][2 * c + 1] = (int)p[1];
+                }
+                xs[0][i] = (int)z.byte;
+            }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 if constexpr (sizeof(T) == 2) {
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[set][j], x[set][i], acc[i][j], 0, 0, 0, ws[set][j], 0, xs[set][i]);
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[set][j], x[from][i], acc[i][j], 0, 0, 0, ws[set][j], 0, xs[from][i]);
                 } else {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_as_bf16(w[set][j], q, ws[set][j]), f8_as_bf16(x[set][i], q, xs[set][i]), acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f8_as_bf16(w[set][j], q, ws[set][j]), f8_as_bf16(x[from][i], q, xs[from][i]), acc[i][j], 0, 0, 0);
                 }
             }
+        }
     };
     if (k0 < k1) load(0, k0);
     for (int k = k0; k < k1; k += 2) {
-        load(1, k + 1);
+        if (k + 1 < k1) load(1, k + 1);
         mma(0);
         if (k + 1 >= k1) break;
-        load(0, k + 2);
+        if (k + 2 < k1) load(0, k + 2);
         mma(1);
     }
     // ---- the wavefronts' sums meet: the lane has row `col` of a tile and channels 4 g4 .. + 3
@@ -200,14 +254,13 @@ linear_f8_few_kernel(LinearF8Args a, int m_tiles) {
     __syncthreads();
     for (int idx = tid; idx < BM * BN / 4; idx += 64 * WV) {
         const int r = idx / (BN / 4), c = idx % (BN / 4) * 4, n = n0 + c;
-        const int64_t row = m0 + r;
-        if (row >= a.rows || n >= a.N) continue;
+        if (r >= a.rows || n >= a.N) continue;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < WV; ++i) s += *reinterpret_cast<const f32x4*>(&s_sum[i][r * RS + c]);
         const f32x4 b = a.b ? *reinterpret_cast<const f32x4*>(a.b + n) : f32x4{0.f, 0.f, 0.f, 0.f};
-        T* yp = (T*)a.y + row * a.N + n;
-        const T* rp = (const T*)a.res + row * a.N + n;
+        T* yp = (T*)a.y + (int64_t)r * a.N + n;
+        const T* rp = (const T*)a.res + (int64_t)r * a.N + n;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (n + e >= a.N) break;
@@ -218,11 +271,25 @@ linear_f8_few_kernel(LinearF8Args a, int m_tiles) {
     }
 }
 
-template <typename T, int MT, int NT>
-static int launch_few(const LinearF8Args& a, hipStream_t st) {
-    const int64_t mt = cdiv(a.rows, 16 * MT);
-    linear_f8_few_kernel<T, MT, NT><<<(unsigned)(mt * cdiv(a.N, 16 * NT)), 512, 0, st>>>(a, (int)mt);
+template <typename T, int MT, int NT, int WV, bool FROM_X>
+static int launch_few_as(const LinearF8Args& a, hipStream_t st) {
+    linear_f8_few_kernel<T, MT, NT, WV, FROM_X><<<(unsigned)cdiv(a.N, 16 * NT), 64 * WV, 0, st>>>(a);
     return check_launch("linear_f8_few_kernel");
+}
+constexpr int LF_FEW = 32;                      // rows
+// us in a captured stream, a launch of 2.4 for the rows of x included: 12 x 4096 x 4096 bf16 9.7 rounded in here, 9.9 in a launch of its own (which costs the host another
+// launch, too); 16 x 8192 x 8192 34 and 23, 32 x 4096 x 4096 14.6 and 13.4, 12 x 4096 x 4096 fp32 13.1 and 10.1: every block reads all of x
+template <typename T>
+static bool few_from_x(const LinearF8Args& a) { return sizeof(T) == 2 && a.rows <= 16 && a.N < 6144; }
+// 32 channels a block where that still makes 192 blocks (16 x 8192 x 8192 25.5 -> 19.8, 12 x 1536 x 6144 5.5 -> 4.9, but 12 x 4096 x 4096 7.5 -> 10.0).  Four
+// row tiles are slower than tiles in LDS (33 x 4096 x 4096 17.4 and 14.5)
+template <typename T>
+static int launch_few(const LinearF8Args& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2)
+        if (a.x) return a.Kp >= 2048 ? launch_few_as<T, 1, 1, 16, true>(a, st) : launch_few_as<T, 1, 1, 8, true>(a, st);
+    if (a.N >= 6144) return a.rows <= 16 ? launch_few_as<T, 1, 2, 8, false>(a, st) : launch_few_as<T, 2, 2, 8, false>(a, st);
+    if (a.rows <= 16) return a.Kp >= 2048 ? launch_few_as<T, 1, 1, 16, false>(a, st) : launch_few_as<T, 1, 1, 8, false>(a, st);
+    return a.Kp >= 2048 ? launch_few_as<T, 2, 1, 16, false>(a, st) : launch_few_as<T, 2, 1, 8, false>(a, st);
 }
 
 // ---- many tiles: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, a ring of NS stages of HB half blocks (64 of K) in LDS.
@@ -230,11 +297,6 @@ static int launch_few(const LinearF8Args& a, hipStream_t st) {
 // within a block does, the same for both operands).  The first operand's rows become the accumulators' rows, so the channels go
 // first, in the order that leaves a lane with eight consecutive channels of one row of x.
 __device__ __forceinline__ int lf_kperm(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
-
-// 16 bytes at any element's address
-template <typename T> struct LFAny;
-template <> struct LFAny<uint16_t> { typedef u32x4 __attribute__((aligned(2))) type; };
-template <> struct LFAny<float> { typedef u32x4 __attribute__((aligned(4))) type; };
 
 template <int WGM, int WGN, int TM, int TN, int HB, int NS>
 struct LFCfg {
@@ -581,9 +643,13 @@ template <typename T>
 static int launch_tile(const LinearF8Args& a, hipStream_t st) { return a.res ? launch_tile_res<T, true>(a, st) : launch_tile_res<T, false>(a, st); }
 
 template <typename T>
-static int product(const LinearF8Args& a, hipStream_t st) {
-    if (a.rows <= 32) return launch_few<T, 1, 1>(a, st);
-    return launch_tile<T>(a, st);
+static int forward(LinearF8Args a, hipStream_t st) {
+    const bool few = a.rows <= LF_FEW;
+    if (a.x && !(few && few_from_x<T>(a))) {
+        PS_TRY(launch_rows_write<T>(a.x, a.ldx, a.rows, a.K, a.x8, a.sx, st));
+        a.x = nullptr;
+    }
+    return few ? launch_few<T>(a, st) : launch_tile<T>(a, st);
 }
 
 static int rows_ok(const char* who, int64_t rows, int32_t K) {
@@ -603,11 +669,7 @@ static int run_product(const char* who, const pserve_linear_f8_t* op, LinearF8Ar
     a.res = residual; a.y = y;
     a.w8 = op->w; a.sw = op->scale; a.b = op->b;
     a.K = op->K; a.N = op->N; a.Kp = op->Kp; a.Np = op->Np; a.Sp = op->Sp;
-    if (a.x) {
-        if (op->dtype == PSERVE_BF16) PS_TRY(launch_rows_write<uint16_t>(a.x, a.ldx, a.rows, a.K, a.x8, a.sx, st));
-        else PS_TRY(launch_rows_write<float>(a.x, a.ldx, a.rows, a.K, a.x8, a.sx, st));
-    }
-    return op->dtype == PSERVE_BF16 ? product<uint16_t>(a, st) : product<float>(a, st);
+    return op->dtype == PSERVE_BF16 ? forward<uint16_t>(a, st) : forward<float>(a, st);
 }
 
 }  // namespace pserve

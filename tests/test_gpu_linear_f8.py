@@ -71,7 +71,7 @@ def test_rows_that_are_not_finite_and_rows_apart(dtype):
 
 
 SHAPES = [(1, 64, 64), (1, 1, 1), (3, 77, 5), (12, 256, 512), (16, 4100, 130), (17, 128, 255), (33, 640, 1280), (64, 1000, 77), (130, 320, 264),
-          (257, 129, 1000), (300, 2048, 640), (128, 128, 128), (129, 8200, 40), (700, 1536, 768), (1100, 384, 1152), (2, 16384, 33), (15, 513, 16),
+          (257, 129, 1000), (300, 2048, 640), (128, 128, 128), (129, 8200, 40), (700, 1536, 768), (1100, 384, 1152), (2, 16384, 33), (15, 513, 16), (20, 2300, 100), (31, 300, 6200), (16, 2049, 6145), (17, 5000, 50),
           (1300, 1100, 1030), (1281, 100, 1001), (5000, 700, 3400), (4200, 136, 4099)]
 
 
