@@ -54,6 +54,23 @@ struct F8Scale {
 
 __device__ __forceinline__ float f8_scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// 16 bytes at any element's address
+template <typename T> struct AnyPiece;
+template <> struct AnyPiece<uint16_t> { typedef u32x4 __attribute__((aligned(2))) type; };
+template <> struct AnyPiece<float> { typedef u32x4 __attribute__((aligned(4))) type; };
+
+// A store, past the caches where `past` says so.  (The empty statements keep the compiler from making one store of the two.)
+template <typename P>
+__device__ __forceinline__ void store_piece(P* p, const u32x4& v, bool past) {
+    if (past) {
+        asm volatile("");
+        __builtin_nontemporal_store(v, p);
+        asm volatile("");
+    } else {
+        *p = v;
+    }
+}
+
 // the largest |v| of eight values as a bit pattern (infinities and NaN come out on top)
 __device__ __forceinline__ uint32_t f8_largest(const float (&v)[8]) {
     uint32_t m = 0;

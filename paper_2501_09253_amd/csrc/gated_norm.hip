@@ -20,81 +20,111 @@ struct NormArgs {
     int64_t rows, xs, fs, ys, hs, gate_s, scale_s, shift_s;
     float skip, branch, post_eps, pre_eps;
     int32_t C, n, post, pre;
+    int32_t stream;                             // outputs past the caches
 };
 
-// The request of a row and the index of its vectors: the last s with cu[s] <= row, 64 places of the range looked at in one go.
-// Where the starts do not ascend, any one; false: none, or one whose vectors are not there.
+// The request of a row and the index of its vectors: the last s with cu[s] <= row.  Where the starts do not ascend, any one; false: none, or one whose
+// vectors are not there.  WAVE: the row is a wavefront's, which looks at 64 places in one go; else a lane's own search
+template <bool WAVE>
 __device__ __forceinline__ bool norm_request(const NormArgs& a, int64_t row, int& s) {
     s = 0;
     if (a.cu) {
         const int lane = threadIdx.x & 63;
-        int lo = 0, len = a.n;
-        for (;;) {
-            const int step = (len + 63) / 64;
-            const bool le = lane * step < len && a.cu[lo + lane * step] <= row;
-            const uint64_t past = ~__ballot(le);
-            const int count = past ? __ffsll((unsigned long long)past) - 1 : 64;
-            if (count == 0) return false;
-            lo += (count - 1) * step;
-            len = min(step, len - (count - 1) * step);
-            if (step == 1) break;
+        if (WAVE && a.n < 64) {
+            const uint64_t past = ~__ballot(lane <= a.n && a.cu[min(lane, a.n)] <= row);
+            s = __ffsll((unsigned long long)past) - 2;          // (bit 63 is one of them, or n = 63 and the row is behind the last request)
+            if (past == 0 || s < 0 || s >= a.n) return false;
+        } else if (WAVE) {
+            int lo = 0, len = a.n;
+            for (;;) {
+                const int step = (len + 63) / 64;
+                const bool le = lane * step < len && a.cu[lo + lane * step] <= row;
+                const uint64_t past = ~__ballot(le);
+                const int count = past ? __ffsll((unsigned long long)past) - 1 : 64;
+                if (count == 0) return false;
+                lo += (count - 1) * step;
+                len = min(step, len - (count - 1) * step);
+                if (step == 1) break;
+            }
+            s = lo;
+            if (row >= a.cu[s + 1]) return false;
+        } else {
+            int lo = 0, hi = a.n;                               // cu[lo] <= row < cu[hi], where the ends hold
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.cu[mid] <= row) lo = mid;
+                else hi = mid;
+            }
+            s = lo;
+            if (row < a.cu[s] || row >= a.cu[s + 1]) return false;
         }
-        s = lo;
-        if (row >= a.cu[s + 1]) return false;
     }
     if (a.which) {
         s = a.which[s];
         if (s < 0 || s >= a.n) return false;
     }
-    s = __builtin_amdgcn_readfirstlane(s);
+    if (WAVE) s = __builtin_amdgcn_readfirstlane(s);
     return true;
 }
 
-// The sum over the TPR threads of a row, in all of them, in a fixed order
+// The sum over the threads of a row, in all of them, in a fixed order: TPR neighbouring lanes, or (TPR = 0) a block
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* s_part) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    if (TPR == 256) {
+    for (int d = 1; d < (TPR ? TPR : 64); d <<= 1) v += __shfl_xor(v, d);
+    if (TPR == 0) {
         __syncthreads();                        // (the sum before has been read)
         if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = (s_part[0] + s_part[1]) + (s_part[2] + s_part[3]);
+        v = s_part[0];
+        for (int i = 1; i < (int)blockDim.x / 64; ++i) v += s_part[i];
     }
     return v;
 }
 
-template <typename T, int TPR, int CH, bool VEC>
-__global__ void __launch_bounds__(256)
+// TPR threads a row (0: a block), CH chunks of eight values a thread; EVEN: whole chunks
+template <typename T, int TPR, int CH, bool EVEN>
+__global__ void __launch_bounds__(TPR ? 256 : CH == 1 ? 512 : 1024)
 gated_norm_kernel(NormArgs a) {
-    __shared__ float s_part[4];
-    const int t = threadIdx.x % TPR;
-    const int64_t row = block_of_lines() * (256 / TPR) + threadIdx.x / TPR;
+    __shared__ float s_part[16];
+    const int span = TPR ? TPR : blockDim.x, t = TPR ? (int)threadIdx.x % TPR : (int)threadIdx.x;
+    const int64_t row = TPR ? block_of_lines() * (256 / TPR) + threadIdx.x / TPR : block_of_lines();
     if (row >= a.rows) return;
-    int s;
-    if (!norm_request(a, row, s)) return;
     const int C = a.C;
-    auto get = [&](const T* p, int c, float (&v)[8]) {
-        if (VEC) {
-            if (8 * c < C) load8(p + 8 * c, v);
-            else
+    typedef typename AnyPiece<T>::type Any;
+    constexpr int W = sizeof(T) / 2, CV = 16 / sizeof(T);   // 16-byte words of a chunk, values of a word
+    auto fetch = [&](const T* p, int c, Raw8<T>& r) {
+        if (EVEN ? 8 * c < C : 8 * c + 8 <= C) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 0.f;
+            for (int h = 0; h < W; ++h) r.w[h] = *reinterpret_cast<const Any*>(p + 8 * c + h * CV);
         } else {
+            T v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 8 * c + e < C ? load1(p + 8 * c + e) : 0.f;
+            for (int e = 0; e < 8; ++e) v[e] = !EVEN && 8 * c + e < C ? p[8 * c + e] : T(0);
+            __builtin_memcpy(&r, v, sizeof r);
         }
+    };
+    auto get = [&](const T* p, int c, float (&v)[8]) {
+        Raw8<T> r;
+        fetch(p, c, r);
+        values8(r, v);
     };
     auto put = [&](T* p, int c, const float (&v)[8]) {
-        if (VEC) {
-            if (8 * c < C) store8(p + 8 * c, v);
-        } else {
+        T o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) store1(o + e, v[e]);
+        if (EVEN ? 8 * c < C : 8 * c + 8 <= C) {
+            Raw8<T> r;
+            __builtin_memcpy(&r, o, sizeof r);
+#pragma unroll
+            for (int h = 0; h < W; ++h) store_piece(reinterpret_cast<Any*>(p + 8 * c + h * CV), r.w[h], a.stream);
+        } else if (!EVEN) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (8 * c + e < C) store1(p + 8 * c + e, v[e]);
+                if (8 * c + e < C) p[8 * c + e] = o[e];
         }
     };
-    auto in_row = [&](int c, int e) { return VEC ? 8 * c < C : 8 * c + e < C; };
+    auto in_row = [&](int c, int e) { return EVEN ? 8 * c < C : 8 * c + e < C; };
     const float by = 1.f / (float)C;
     // what N multiplies by, after taking the mean off in place
     auto normed = [&](float (&v)[CH][8], int kind, float eps) -> float {
@@ -108,7 +138,7 @@ gated_norm_kernel(NormArgs a) {
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = in_row(t + i * TPR, e) ? v[i][e] - mean : 0.f;
+                for (int e = 0; e < 8; ++e) v[i][e] = in_row(t + i * span, e) ? v[i][e] - mean : 0.f;
         }
         float sq = 0.f;
 #pragma unroll
@@ -117,20 +147,38 @@ gated_norm_kernel(NormArgs a) {
             for (int e = 0; e < 8; ++e) sq = fmaf(v[i][e], v[i][e], sq);
         return 1.f / sqrtf(row_sum<TPR>(sq, s_part) * by + eps);
     };
+    // The row comes in beside the search for its request, and with it known the vectors beside the sums
     float v[CH][8], w[8];
-    const T* xr = (const T*)a.x + row * a.xs;
-    if (a.f) {
-        const T* fr = (const T*)a.f + row * a.fs;
+    Raw8<T> xw[CH], fw[CH];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) get(fr, t + i * TPR, v[i]);
+    for (int i = 0; i < CH; ++i) fetch((const T*)a.x + row * a.xs, t + i * span, xw[i]);
+    if (a.f)
+#pragma unroll
+        for (int i = 0; i < CH; ++i) fetch((const T*)a.f + row * a.fs, t + i * span, fw[i]);
+    int s;
+    if (!norm_request<(TPR == 0 || TPR == 64)>(a, row, s)) return;
+    Raw8<T> gw[2][CH];
+    const T *first[2] = {(const T*)a.post_gain, a.gate ? (const T*)a.gate + s * a.gate_s : nullptr};
+    const T *second[2] = {a.scale ? (const T*)a.scale + s * a.scale_s : nullptr, a.shift ? (const T*)a.shift + s * a.shift_s : nullptr};
+    auto ahead = [&](const T* const (&from)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (from[k])
+#pragma unroll
+                for (int i = 0; i < CH; ++i) fetch(from[k], t + i * span, gw[k][i]);
+    };
+    if (a.f) {
+        ahead(first);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) values8(fw[i], v[i]);
         const float r = a.post != PSERVE_NORM_NONE ? normed(v, a.post, a.post_eps) : 1.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int c = t + i * TPR;
+            const int c = t + i * span;
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] *= r;
             if (a.post_gain) {
-                get((const T*)a.post_gain, c, w);
+                values8(gw[0][i], w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[i][e] *= w[e];
             }
@@ -140,31 +188,32 @@ gated_norm_kernel(NormArgs a) {
                 for (int e = 0; e < 8; ++e) v[i][e] += w[e];
             }
             if (a.gate) {
-                get((const T*)a.gate + s * a.gate_s, c, w);
+                values8(gw[1][i], w);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[i][e] *= w[e];
             }
-            get(xr, c, w);
+            values8(xw[i], w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] = in_row(c, e) ? fmaf(a.branch, v[i][e], a.skip * w[e]) : 0.f;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            get(xr, t + i * TPR, v[i]);
+            values8(xw[i], v[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] *= a.skip;
         }
     }
     if (a.y)
 #pragma unroll
-        for (int i = 0; i < CH; ++i) put((T*)a.y + row * a.ys, t + i * TPR, v[i]);
+        for (int i = 0; i < CH; ++i) put((T*)a.y + row * a.ys, t + i * span, v[i]);
     if (!a.h && !a.v8) return;
+    ahead(second);
     const float r = a.pre != PSERVE_NORM_NONE ? normed(v, a.pre, a.pre_eps) : 1.f;
     const int Kp = f8_width(C), Sp = f8_scales(C);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = t + i * TPR;
+        const int c = t + i * span;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[i][e] *= r;
         if (a.pre_gain) {
@@ -178,12 +227,12 @@ gated_norm_kernel(NormArgs a) {
             for (int e = 0; e < 8; ++e) v[i][e] += w[e];
         }
         if (a.scale) {
-            get((const T*)a.scale + s * a.scale_s, c, w);
+            values8(gw[0][i], w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] *= 1.f + w[e];
         }
         if (a.shift) {
-            get((const T*)a.shift + s * a.shift_s, c, w);
+            values8(gw[1][i], w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] += w[e];
         }
@@ -200,19 +249,27 @@ gated_norm_kernel(NormArgs a) {
     }
 }
 
-template <typename T, bool VEC>
-static int launch_norm(const NormArgs& a, hipStream_t st) {
-    const int chunks = (int)cdiv(a.C, 8);
-    const dim3 waves = block_lines(cdiv(a.rows, 4)), rows = block_lines(a.rows);
-    if (chunks <= 64) gated_norm_kernel<T, 64, 1, VEC><<<waves, 256, 0, st>>>(a);
-    else if (chunks <= 128) gated_norm_kernel<T, 64, 2, VEC><<<waves, 256, 0, st>>>(a);
-    else if (chunks <= 256) gated_norm_kernel<T, 256, 1, VEC><<<rows, 256, 0, st>>>(a);
-    else if (chunks <= 512) gated_norm_kernel<T, 256, 2, VEC><<<rows, 256, 0, st>>>(a);
-    else if (chunks <= 1024) gated_norm_kernel<T, 256, 4, VEC><<<rows, 256, 0, st>>>(a);
-    else gated_norm_kernel<T, 256, 8, VEC><<<rows, 256, 0, st>>>(a);
+template <typename T, int TPR, int CH, bool EVEN>
+static int launch_norm_as(const NormArgs& a, hipStream_t st) {
+    const int block = TPR ? 256 : (int)cdiv(cdiv(a.C, 8), 64 * CH) * 64;
+    gated_norm_kernel<T, TPR, CH, EVEN><<<block_lines(TPR ? cdiv(a.rows, 256 / (TPR ? TPR : 1)) : a.rows), block, 0, st>>>(a);
     return check_launch("gated_norm_kernel");
 }
-
+// A row is a wavefront's, or a part of one, where its chunks of eight are that many lanes, and a block's else.  Outputs that do not fit the caches beside the
+// inputs go past them (12,544 x 1536, bf16, y and h: 39 -> 32 us, 4.9 TB/s; 300,000 x 64 41 -> 32); 8-bit rows do not: the product reads
+// them next; nor does fp32, where a store instruction leaves every other 16 bytes (6000 x 3000 66 us and 83).
+template <typename T, bool EVEN>
+static int launch_norm(const NormArgs& a, hipStream_t st) {
+    const int chunks = (int)cdiv(a.C, 8);
+    if (chunks <= 8 && !a.v8) return launch_norm_as<T, 8, 1, EVEN>(a, st);          // (8-bit rows have sixteen chunks at least)
+    if (chunks <= 16) return launch_norm_as<T, 16, 1, EVEN>(a, st);
+    if (chunks <= 32) return launch_norm_as<T, 32, 1, EVEN>(a, st);
+    if (chunks <= 64) return launch_norm_as<T, 64, 1, EVEN>(a, st);
+    // (60,000 x 640, bf16: 91 us by blocks of 128, 75 by wavefronts; 1694 x 1000, fp32: 9.7 and 10.4)
+    if (chunks <= 128 && a.rows >= 8192) return launch_norm_as<T, 64, 2, EVEN>(a, st);
+    if (chunks <= 512) return launch_norm_as<T, 0, 1, EVEN>(a, st);
+    return launch_norm_as<T, 0, 2, EVEN>(a, st);
+}
 }  // namespace pserve
 
 extern "C" {
@@ -239,12 +296,10 @@ int pserve_gated_norm(const pserve_gated_norm_desc* d, const pserve_gated_norm_b
                                                                    {b->gate, d->gate_stride, false}, {b->scale, d->scale_stride, false}, {b->shift, d->shift_stride, false},
                                                                    {b->post_gain, d->C, false}, {b->post_bias, d->C, false}, {b->pre_gain, d->C, false}, {b->pre_bias, d->C, false}};
     const int64_t es = (int64_t)dtype_size(d->dtype);
-    bool vec = d->C % 8 == 0;
     for (const auto& r : rowed) {
         if (!r.p) continue;
         PS_REQUIRE(!((uintptr_t)r.p & (es - 1)), "%s: a buffer is not aligned to its type", who);
         PS_REQUIRE(r.stride >= 0 && r.stride < (1ll << 31) && (!r.row || d->rows == 1 || r.stride >= d->C), "%s: a stride of %lld elements (C = %d)", who, (long long)r.stride, d->C);
-        vec = vec && !((uintptr_t)r.p & 15) && r.stride * es % 16 == 0;
     }
     PS_REQUIRE(!((uintptr_t)b->rows8 & 15), "%s: rows8 is not 16-byte aligned", who);
     NormArgs a{};
@@ -258,10 +313,11 @@ int pserve_gated_norm(const pserve_gated_norm_desc* d, const pserve_gated_norm_b
     a.rows = d->rows; a.xs = d->x_stride; a.fs = d->f_stride; a.ys = d->y_stride; a.hs = d->h_stride;
     a.gate_s = d->gate_stride; a.scale_s = d->scale_stride; a.shift_s = d->shift_stride;
     a.skip = d->skip_scale; a.branch = d->branch_scale; a.post_eps = d->post_eps; a.pre_eps = d->pre_eps;
+    a.stream = es == 2 && d->rows * d->C * es * ((b->y ? 1 : 0) + (b->h ? 1 : 0)) > (4 << 20);
     a.C = d->C; a.n = d->n; a.post = d->post_norm; a.pre = d->pre_norm;
     hipStream_t st = (hipStream_t)stream;
-    if (d->dtype == PSERVE_BF16) return vec ? launch_norm<uint16_t, true>(a, st) : launch_norm<uint16_t, false>(a, st);
-    return vec ? launch_norm<float, true>(a, st) : launch_norm<float, false>(a, st);
+    if (d->dtype == PSERVE_BF16) return d->C % 8 == 0 ? launch_norm<uint16_t, true>(a, st) : launch_norm<uint16_t, false>(a, st);
+    return d->C % 8 == 0 ? launch_norm<float, true>(a, st) : launch_norm<float, false>(a, st);
 }
 
 }  // extern "C"

@@ -125,11 +125,6 @@ static int launch_rows_write(const void* x, int64_t ldx, int64_t rows, int32_t K
     return check_launch("f8_rows_write_kernel");
 }
 
-// 16 bytes at any element's address
-template <typename T> struct LFAny;
-template <> struct LFAny<uint16_t> { typedef u32x4 __attribute__((aligned(2))) type; };
-template <> struct LFAny<float> { typedef u32x4 __attribute__((aligned(4))) type; };
-
 // ---- few rows: 16 MT rows x 16 NT channels, WV wavefronts that share K and read their operands from memory (a lane 32 values of a row's
 // block, 16 g4 .. + 15 and 64 + 16 g4 .. + 15), the next block's in flight; the sums meet in LDS, in a fixed order.  FROM_X: rows of x are rounded on the way
 // in, by every block for itself (a row's block of 128 is four lanes).
@@ -165,7 +160,7 @@ linear_f8_few_kernel(LinearF8Args a) {
             xsp[i] = a.sx + r * a.Sp;
         }
     }
-    typedef typename LFAny<T>::type Any;
+    typedef typename AnyPiece<T>::type Any;
     f32x4 acc[MT][NT];
     i32x8 w[2][NT], x[FROM_X ? 1 : 2][MT];
     Raw8<T> raw[FROM_X ? 2 : 1][MT][4];
@@ -503,7 +498,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
         const int nt = t + t_step, er = lane >> 3, ec = lane & 7;
         // whole lines go past the L2, which holds the panels; where rows begin inside a line, its parts meet there
         const bool lines = a.N % (8 * CV) == 0 && !((uintptr_t)a.y & 127);
-        typedef typename LFAny<T>::type Any;
+        typedef typename AnyPiece<T>::type Any;
         u32x4 rres[RQ][4];
         // the residual of piece p, eight whole lines an instruction
         auto res_load = [&](int p) {
@@ -591,8 +586,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
                 const u32x4 o = ep[rr * 8 + (ec ^ ((rr >> 1) & 7))];
                 T* yp = (T*)a.y + row * a.N + n;
                 if (row < a.rows && n + CV <= a.N) {
-                    if (lines) __builtin_nontemporal_store(o, reinterpret_cast<Any*>(yp));
-                    else *reinterpret_cast<Any*>(yp) = o;
+                    store_piece(reinterpret_cast<Any*>(yp), o, lines);
                 } else if (row < a.rows) {
                     T e[CV];
                     __builtin_memcpy(e, &o, sizeof o);

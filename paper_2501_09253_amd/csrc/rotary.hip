@@ -6,7 +6,7 @@
 // heads are: a block computes those of its tokens once, into LDS, then walks its tokens' heads in 16-byte pieces.
 // An angle is taken in revolutions, in 64 bits (positions reach 2^24, and 32 bits leave a position of 2^17 with an angle off by 2^-7); the
 // fraction of a revolution is rounded to fp32, at most 2^-26 off: 2^-23.3 radians.
-#include "quant8.h"
+#include "f8.h"
 
 using namespace pserve;
 
@@ -50,30 +50,27 @@ struct Divisor {
     __device__ __forceinline__ int operator()(int n) const { return d > 1 ? (int)__umulhi((uint32_t)n, m) : n; }
 };
 
-template <int BYTES> struct Piece;
-template <> struct Piece<16> { typedef u32x4 type; };
-template <> struct Piece<8> { typedef q8_u32x2 type; };
-template <> struct Piece<4> { typedef uint32_t type; };
-template <> struct Piece<2> { typedef uint16_t type; };
-
-// An item is VP pairs of a head, two pieces of VP values each (HALF: p and P + p, NEXT: one behind the other), or two pieces of what is copied.  A block's items are
-// numbered line by line (token, head); a thread asks for its first IT items before the angles are formed, so the two ways to memory overlap.
-template <typename T, bool HALF, int VP, int IT>
+// An item is two pieces of 16 bytes of a head, at any element's address, V values each.  HALF: the values of V pairs, from p and P + p on, then pieces of what
+// is copied.  NEXT: pieces hold whole pairs, turned or copied; an item's two are half of the head apart, so that neighbouring lanes have neighbouring pieces.
+// A block's items are numbered line by line (token, head); a thread asks for its first IT items before the angles are formed, so the two ways to
+// memory overlap.
+template <typename T, bool HALF, int IT>
 __global__ void __launch_bounds__(256)
 rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
     extern __shared__ float2 s_turn[];
-    typedef typename Piece<VP * sizeof(T)>::type Raw;
+    constexpr int V = 16 / sizeof(T);
+    typedef typename AnyPiece<T>::type Any;
     const int64_t t0 = block_of_lines() * a.TB;
     if (t0 >= a.tokens) return;
-    const int nt = (int)min((int64_t)a.TB, a.tokens - t0), total = nt * (int)(heads.d * items.d), turned = a.P / VP;
+    const int nt = (int)min((int64_t)a.TB, a.tokens - t0), total = nt * (int)(heads.d * items.d);
+    const int turned = HALF ? (a.P + V - 1) / V : 0, last = a.keep ? 2 * a.P : a.D, begin = HALF ? 2 * a.P : 0;     // copied (NEXT: all) values: begin .. last - 1
+    const int apart = (int)items.d - turned;                    // between the pieces of an item of those
     const T* in;
     T* out;
-    int t, ia, ib;
-    bool second;
+    int cs, at[2], len[2];                                      // the token's angles; where the pieces are, and how many values
+    bool pairs;                                                 // (HALF) an item of pairs
     auto place = [&](int i) {
-        const int line = items(i), c = i - line * (int)items.d;
-        t = heads(line);
-        const int h = line - t * (int)heads.d, hk = h - a.heads;
+        const int line = items(i), c = i - line * (int)items.d, t = heads(line), h = line - t * (int)heads.d, hk = h - a.heads;
         if (hk < 0) {
             in = (const T*)a.q + (t0 + t) * a.qs[0] + h * a.qs[1];
             out = (T*)a.q_out + (t0 + t) * a.qo[0] + h * a.qo[1];
@@ -81,97 +78,102 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
             in = (const T*)a.k + (t0 + t) * a.ks[0] + hk * a.ks[1];
             out = (T*)a.k_out + (t0 + t) * a.ko[0] + hk * a.ko[1];
         }
-        if (c < turned) {
-            ia = HALF ? c * VP : 2 * c * VP;
-            ib = HALF ? a.P + c * VP : ia + VP;
-            second = true;
-            t = t * a.P + c * VP;               // of the first pair's angle
+        cs = t * a.P;
+        pairs = HALF && c < turned;
+        if (pairs) {
+            at[0] = c * V;
+            at[1] = a.P + c * V;
+            len[0] = len[1] = min(V, a.P - c * V);
         } else {
-            ia = 2 * a.P + 2 * (c - turned) * VP;
-            ib = ia + VP;
-            second = ib < a.D;
-            t = -1;
-        }
-    };
-    Raw ra[IT], rb[IT];
-    auto load = [&](int i, Raw& x, Raw& y) {
-        place(i);
-        x = *reinterpret_cast<const Raw*>(in + ia);
-        if (second) y = *reinterpret_cast<const Raw*>(in + ib);
-    };
-    auto finish = [&](int i, Raw& x, Raw& y) {
-        place(i);
-        if (t >= 0) {
-            T vx[VP], vy[VP];
-            __builtin_memcpy(vx, &x, sizeof x);
-            __builtin_memcpy(vy, &y, sizeof y);
-            const float2* cs = s_turn + t;
 #pragma unroll
-            for (int e = 0; e < VP; ++e) {
-                T *pa = HALF || e < VP / 2 ? vx : vy, *pb = pa;     // where pair e lies in the two pieces
-                int ja = HALF ? e : 2 * e % VP, jb = ja + 1;
-                if (HALF || VP == 1) { pa = vx; pb = vy; ja = jb = e; }
-                const float u = load1(pa + ja), v = load1(pb + jb), c = cs[e].x, s = cs[e].y;
-                store1(pa + ja, u * c - v * s);
-                store1(pb + jb, u * s + v * c);
+            for (int k = 0; k < 2; ++k) {
+                at[k] = begin + (c - turned + k * apart) * V;
+                len[k] = max(0, min(V, last - at[k]));
             }
-            __builtin_memcpy(&x, vx, sizeof x);
-            __builtin_memcpy(&y, vy, sizeof y);
         }
-        *reinterpret_cast<Raw*>(out + ia) = x;
-        if (second) *reinterpret_cast<Raw*>(out + ib) = y;
     };
+    auto load = [&](int i, u32x4 (&x)[2]) {
+        place(i);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (len[k] == V) x[k] = *reinterpret_cast<const Any*>(in + at[k]);
+            else {
+                T v[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = e < len[k] ? in[at[k] + e] : T(0);
+                __builtin_memcpy(&x[k], v, sizeof v);
+            }
+        }
+    };
+    auto finish = [&](int i, u32x4 (&x)[2]) {
+        place(i);
+        T v[2][V];
+        __builtin_memcpy(v, x, sizeof v);
+        if constexpr (HALF) {
+            if (pairs)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float2 t = s_turn[cs + min(at[0] + e, a.P - 1)];
+                    const float p = load1(&v[0][e]), q = load1(&v[1][e]);
+                    store1(&v[0][e], p * t.x - q * t.y);
+                    store1(&v[1][e], p * t.y + q * t.x);
+                }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    const int pair = (at[k] + e) >> 1;
+                    const float2 t = s_turn[cs + min(pair, a.P - 1)];
+                    const float p = load1(&v[k][e]), q = load1(&v[k][e + 1]);
+                    T o[2];
+                    store1(o, p * t.x - q * t.y);
+                    store1(o + 1, p * t.y + q * t.x);
+                    v[k][e] = pair < a.P ? o[0] : v[k][e];
+                    v[k][e + 1] = pair < a.P ? o[1] : v[k][e + 1];
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (len[k] == V) {
+                u32x4 o;
+                __builtin_memcpy(&o, v[k], sizeof o);
+                *reinterpret_cast<Any*>(out + at[k]) = o;
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (e < len[k]) out[at[k] + e] = v[k][e];
+            }
+        }
+    };
+    u32x4 held[IT][2];
 #pragma unroll
     for (int j = 0; j < IT; ++j)
-        if (threadIdx.x + 256 * j < total) load(threadIdx.x + 256 * j, ra[j], rb[j]);
+        if (threadIdx.x + 256 * j < total) load(threadIdx.x + 256 * j, held[j]);
     rotary_angles(a, t0, nt, s_turn);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < IT; ++j)
-        if (threadIdx.x + 256 * j < total) finish(threadIdx.x + 256 * j, ra[j], rb[j]);
+        if (threadIdx.x + 256 * j < total) finish(threadIdx.x + 256 * j, held[j]);
     for (int i = threadIdx.x + 256 * IT; i < total; i += 256) {
-        load(i, ra[0], rb[0]);
-        finish(i, ra[0], rb[0]);
+        load(i, held[0]);
+        finish(i, held[0]);
     }
 }
 
-template <typename T, int VP>
-static int launch_rotary_as(const RotaryArgs& in, int layout, hipStream_t st) {
-    constexpr int IT = 4;
+template <typename T>
+static int launch_rotary(const RotaryArgs& in, int layout, hipStream_t st) {
+    constexpr int IT = 4, V = 16 / sizeof(T);
     RotaryArgs a = in;
-    const int H = a.heads + a.kv_heads, rest = a.keep ? 0 : a.D - 2 * a.P, items = a.P / VP + (int)cdiv(rest, 2 * VP);
+    const bool half = layout == PSERVE_PAIR_HALF;
+    const int H = a.heads + a.kv_heads, rest = (a.keep ? 2 * a.P : a.D) - (half ? 2 * a.P : 0), items = (half ? (int)cdiv(a.P, V) : 0) + (int)cdiv(rest, 2 * V);
     // IT items a thread, but 512 blocks where the tokens give them; angles of a block: up to 32 KB
     a.TB = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 * IT / (H * items), cdiv(a.tokens, 512)), 4096 / a.P));
     const dim3 grid = block_lines(cdiv(a.tokens, a.TB));
     const size_t lds = (size_t)a.TB * a.P * sizeof(float2);
-    if (layout == PSERVE_PAIR_HALF) rotary_kernel<T, true, VP, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
-    else rotary_kernel<T, false, VP, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
+    if (half) rotary_kernel<T, true, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
+    else rotary_kernel<T, false, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
     return check_launch("rotary_kernel");
-}
-
-// Pieces as wide as the head's layout, the strides and the addresses allow
-template <typename T>
-static int launch_rotary(const RotaryArgs& a, int layout, hipStream_t st) {
-    auto fits = [&](int vp) {
-        const int64_t b = vp * (int64_t)sizeof(T);
-        const int rest = a.keep ? 0 : a.D - 2 * a.P;
-        bool ok = a.P % vp == 0 && rest % vp == 0;
-        auto one = [&](const void* p, const int64_t* s, int n) {
-            ok = ok && !((uintptr_t)p & (b - 1)) && (a.tokens == 1 || s[0] * (int64_t)sizeof(T) % b == 0) && (n == 1 || s[1] * (int64_t)sizeof(T) % b == 0);
-        };
-        one(a.q, a.qs, a.heads);
-        one(a.q_out, a.qo, a.heads);
-        if (a.kv_heads) {
-            one(a.k, a.ks, a.kv_heads);
-            one(a.k_out, a.ko, a.kv_heads);
-        }
-        return ok;
-    };
-    if constexpr (sizeof(T) == 2)
-        if (fits(8)) return launch_rotary_as<T, 8>(a, layout, st);
-    if (fits(4)) return launch_rotary_as<T, 4>(a, layout, st);
-    if (fits(2)) return launch_rotary_as<T, 2>(a, layout, st);
-    return launch_rotary_as<T, 1>(a, layout, st);
 }
 
 // ---- positions of a plan's tokens
