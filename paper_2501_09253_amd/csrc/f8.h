@@ -50,9 +50,43 @@ struct F8Scale {
         }
         return o;
     }
+    __device__ __forceinline__ void pack(const float (&v)[8], uint8_t* o) const { *reinterpret_cast<q8_u32x2*>(o) = pack8(v); }
+    __device__ __forceinline__ void pack(const float (&v)[4], uint8_t* o) const {
+        const float w[8] = {v[0], v[1], v[2], v[3], 0.f, 0.f, 0.f, 0.f};
+        *reinterpret_cast<uint32_t*>(o) = pack8(w)[0];
+    }
 };
 
 __device__ __forceinline__ float f8_scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Over neighbouring lanes (8, 16, 32 or 64), in all of them, by operands that come from other lanes: within sixteen as in lanes_max, then
+// lane ^ 16 and lane ^ 32 by swapping rows of sixteen and halves (both results together are the lane's own and the other value)
+__device__ __forceinline__ uint32_t max_16_apart(uint32_t m) {
+    const auto r = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    return max(r[0], r[1]);
+}
+__device__ __forceinline__ uint32_t max_32_apart(uint32_t m) {
+    const auto r = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return max(r[0], r[1]);
+}
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+#define PS_LANE(ctrl) v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), ctrl, 0xf, 0xf, true))
+    PS_LANE(0xb1);
+    PS_LANE(0x4e);
+    PS_LANE(0x141);
+    if (L >= 16) PS_LANE(0x140);
+#undef PS_LANE
+    if (L >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (L == 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return v;
+}
 
 // 16 bytes at any element's address
 template <typename T> struct AnyPiece;
@@ -71,11 +105,12 @@ __device__ __forceinline__ void store_piece(P* p, const u32x4& v, bool past) {
     }
 }
 
-// the largest |v| of eight values as a bit pattern (infinities and NaN come out on top)
-__device__ __forceinline__ uint32_t f8_largest(const float (&v)[8]) {
+// the largest |v| of N values as a bit pattern (infinities and NaN come out on top)
+template <int N>
+__device__ __forceinline__ uint32_t f8_largest(const float (&v)[N]) {
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+    for (int i = 0; i < N; ++i) m = max(m, abs_bits(v[i]));
     return m;
 }
 

@@ -20,7 +20,6 @@ struct NormArgs {
     int64_t rows, xs, fs, ys, hs, gate_s, scale_s, shift_s;
     float skip, branch, post_eps, pre_eps;
     int32_t C, n, post, pre;
-    int32_t stream;                             // outputs past the caches
 };
 
 // The request of a row and the index of its vectors: the last s with cu[s] <= row.  Where the starts do not ascend, any one; false: none, or one whose
@@ -70,8 +69,7 @@ __device__ __forceinline__ bool norm_request(const NormArgs& a, int64_t row, int
 // The sum over the threads of a row, in all of them, in a fixed order: TPR neighbouring lanes, or (TPR = 0) a block
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* s_part) {
-#pragma unroll
-    for (int d = 1; d < (TPR ? TPR : 64); d <<= 1) v += __shfl_xor(v, d);
+    v = lanes_sum<TPR ? TPR : 64>(v);
     if (TPR == 0) {
         __syncthreads();                        // (the sum before has been read)
         if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = v;
@@ -82,74 +80,78 @@ __device__ __forceinline__ float row_sum(float v, float* s_part) {
     return v;
 }
 
-// TPR threads a row (0: a block), CH chunks of eight values a thread; EVEN: whole chunks
+// TPR threads a row (0: a block), CH chunks of 16 bytes a thread; EVEN: whole chunks
 template <typename T, int TPR, int CH, bool EVEN>
-__global__ void __launch_bounds__(TPR ? 256 : CH == 1 ? 512 : 1024)
+__global__ void __launch_bounds__(TPR ? 256 : 1024)
 gated_norm_kernel(NormArgs a) {
     __shared__ float s_part[16];
     const int span = TPR ? TPR : blockDim.x, t = TPR ? (int)threadIdx.x % TPR : (int)threadIdx.x;
     const int64_t row = TPR ? block_of_lines() * (256 / TPR) + threadIdx.x / TPR : block_of_lines();
     if (row >= a.rows) return;
     const int C = a.C;
+    constexpr int V = 16 / sizeof(T);           // values of a chunk
     typedef typename AnyPiece<T>::type Any;
-    constexpr int W = sizeof(T) / 2, CV = 16 / sizeof(T);   // 16-byte words of a chunk, values of a word
-    auto fetch = [&](const T* p, int c, Raw8<T>& r) {
-        if (EVEN ? 8 * c < C : 8 * c + 8 <= C) {
-#pragma unroll
-            for (int h = 0; h < W; ++h) r.w[h] = *reinterpret_cast<const Any*>(p + 8 * c + h * CV);
+    auto fetch = [&](const T* p, int c, u32x4& r) {
+        if (EVEN ? V * c < C : V * c + V <= C) {
+            r = *reinterpret_cast<const Any*>(p + V * c);
         } else {
-            T v[8];
+            T v[V];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = !EVEN && 8 * c + e < C ? p[8 * c + e] : T(0);
+            for (int e = 0; e < V; ++e) v[e] = !EVEN && V * c + e < C ? p[V * c + e] : T(0);
             __builtin_memcpy(&r, v, sizeof r);
         }
     };
-    auto get = [&](const T* p, int c, float (&v)[8]) {
-        Raw8<T> r;
-        fetch(p, c, r);
-        values8(r, v);
+    auto values = [&](const u32x4& r, float (&v)[V]) {
+        T x[V];
+        __builtin_memcpy(x, &r, sizeof r);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = load1(x + e);
     };
-    auto put = [&](T* p, int c, const float (&v)[8]) {
-        T o[8];
+    auto get = [&](const T* p, int c, float (&v)[V]) {
+        u32x4 r;
+        fetch(p, c, r);
+        values(r, v);
+    };
+    auto put = [&](T* p, int c, const float (&v)[V]) {
+        T o[V];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) store1(o + e, v[e]);
-        if (EVEN ? 8 * c < C : 8 * c + 8 <= C) {
-            Raw8<T> r;
+        for (int e = 0; e < V; ++e) store1(o + e, v[e]);
+        if (EVEN ? V * c < C : V * c + V <= C) {
+            u32x4 r;
             __builtin_memcpy(&r, o, sizeof r);
-#pragma unroll
-            for (int h = 0; h < W; ++h) store_piece(reinterpret_cast<Any*>(p + 8 * c + h * CV), r.w[h], a.stream);
+            __builtin_nontemporal_store(r, reinterpret_cast<Any*>(p + V * c));
         } else if (!EVEN) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (8 * c + e < C) p[8 * c + e] = o[e];
+            for (int e = 0; e < V; ++e)
+                if (V * c + e < C) p[V * c + e] = o[e];
         }
     };
-    auto in_row = [&](int c, int e) { return EVEN ? 8 * c < C : 8 * c + e < C; };
+    auto in_row = [&](int c, int e) { return EVEN ? V * c < C : V * c + e < C; };
     const float by = 1.f / (float)C;
     // what N multiplies by, after taking the mean off in place
-    auto normed = [&](float (&v)[CH][8], int kind, float eps) -> float {
+    auto normed = [&](float (&v)[CH][V], int kind, float eps) -> float {
         if (kind == PSERVE_NORM_LAYER) {
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[i][e];
+                for (int e = 0; e < V; ++e) sum += v[i][e];
             const float mean = row_sum<TPR>(sum, s_part) * by;
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = in_row(t + i * span, e) ? v[i][e] - mean : 0.f;
+                for (int e = 0; e < V; ++e) v[i][e] = in_row(t + i * span, e) ? v[i][e] - mean : 0.f;
         }
         float sq = 0.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(v[i][e], v[i][e], sq);
+            for (int e = 0; e < V; ++e) sq = fmaf(v[i][e], v[i][e], sq);
         return 1.f / sqrtf(row_sum<TPR>(sq, s_part) * by + eps);
     };
     // The row comes in beside the search for its request, and with it known the vectors beside the sums
-    float v[CH][8], w[8];
-    Raw8<T> xw[CH], fw[CH];
+    float v[CH][V], w[V];
+    u32x4 xw[CH], fw[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) fetch((const T*)a.x + row * a.xs, t + i * span, xw[i]);
     if (a.f)
@@ -157,7 +159,7 @@ gated_norm_kernel(NormArgs a) {
         for (int i = 0; i < CH; ++i) fetch((const T*)a.f + row * a.fs, t + i * span, fw[i]);
     int s;
     if (!norm_request<(TPR == 0 || TPR == 64)>(a, row, s)) return;
-    Raw8<T> gw[2][CH];
+    u32x4 gw[2][CH];
     const T *first[2] = {(const T*)a.post_gain, a.gate ? (const T*)a.gate + s * a.gate_s : nullptr};
     const T *second[2] = {a.scale ? (const T*)a.scale + s * a.scale_s : nullptr, a.shift ? (const T*)a.shift + s * a.shift_s : nullptr};
     auto ahead = [&](const T* const (&from)[2]) {
@@ -170,38 +172,38 @@ gated_norm_kernel(NormArgs a) {
     if (a.f) {
         ahead(first);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) values8(fw[i], v[i]);
+        for (int i = 0; i < CH; ++i) values(fw[i], v[i]);
         const float r = a.post != PSERVE_NORM_NONE ? normed(v, a.post, a.post_eps) : 1.f;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int c = t + i * span;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] *= r;
+            for (int e = 0; e < V; ++e) v[i][e] *= r;
             if (a.post_gain) {
-                values8(gw[0][i], w);
+                values(gw[0][i], w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] *= w[e];
+                for (int e = 0; e < V; ++e) v[i][e] *= w[e];
             }
             if (a.post_bias) {
                 get((const T*)a.post_bias, c, w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] += w[e];
+                for (int e = 0; e < V; ++e) v[i][e] += w[e];
             }
             if (a.gate) {
-                values8(gw[1][i], w);
+                values(gw[1][i], w);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] *= w[e];
+                for (int e = 0; e < V; ++e) v[i][e] *= w[e];
             }
-            values8(xw[i], w);
+            values(xw[i], w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = in_row(c, e) ? fmaf(a.branch, v[i][e], a.skip * w[e]) : 0.f;
+            for (int e = 0; e < V; ++e) v[i][e] = in_row(c, e) ? fmaf(a.branch, v[i][e], a.skip * w[e]) : 0.f;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            values8(xw[i], v[i]);
+            values(xw[i], v[i]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] *= a.skip;
+            for (int e = 0; e < V; ++e) v[i][e] *= a.skip;
         }
     }
     if (a.y)
@@ -215,34 +217,36 @@ gated_norm_kernel(NormArgs a) {
     for (int i = 0; i < CH; ++i) {
         const int c = t + i * span;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] *= r;
+        for (int e = 0; e < V; ++e) v[i][e] *= r;
         if (a.pre_gain) {
             get((const T*)a.pre_gain, c, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] *= w[e];
+            for (int e = 0; e < V; ++e) v[i][e] *= w[e];
         }
         if (a.pre_bias) {
             get((const T*)a.pre_bias, c, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] += w[e];
+            for (int e = 0; e < V; ++e) v[i][e] += w[e];
         }
         if (a.scale) {
-            values8(gw[0][i], w);
+            values(gw[0][i], w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] *= 1.f + w[e];
+            for (int e = 0; e < V; ++e) v[i][e] *= 1.f + w[e];
         }
         if (a.shift) {
-            values8(gw[1][i], w);
+            values(gw[1][i], w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] += w[e];
+            for (int e = 0; e < V; ++e) v[i][e] += w[e];
         }
         if (a.h) put((T*)a.h + row * a.hs, c, v[i]);
-        if (a.v8 && 8 * c < Kp) {               // (sixteen lanes in step)
+        if (a.v8 && V * c < Kp) {               // (the lanes of a block of 128 in step)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = in_row(c, e) ? v[i][e] : 0.f;
-            const F8Scale z(lanes_max<16>(f8_largest(v[i])));
-            *reinterpret_cast<q8_u32x2*>(a.v8 + row * Kp + 8 * c) = z.pack8(v[i]);
-            if (c % 16 == 0) a.s8[row * Sp + c / 16] = (uint8_t)z.byte;
+            for (int e = 0; e < V; ++e) v[i][e] = in_row(c, e) ? v[i][e] : 0.f;
+            constexpr int LANES = 128 / V;
+            uint32_t m = lanes_max<16>(f8_largest(v[i]));
+            if (LANES == 32) m = max_16_apart(m);
+            F8Scale(m).pack(v[i], a.v8 + row * Kp + V * c);
+            if (c % LANES == 0) a.s8[row * Sp + c / LANES] = (uint8_t)F8Scale(m).byte;
             if (c == 0)
                 for (int b = Kp / 128; b < Sp; ++b) a.s8[row * Sp + b] = 127;
         }
@@ -251,25 +255,27 @@ gated_norm_kernel(NormArgs a) {
 
 template <typename T, int TPR, int CH, bool EVEN>
 static int launch_norm_as(const NormArgs& a, hipStream_t st) {
-    const int block = TPR ? 256 : (int)cdiv(cdiv(a.C, 8), 64 * CH) * 64;
+    const int block = TPR ? 256 : (int)cdiv(cdiv(a.C, 16 / sizeof(T)), 64 * CH) * 64;
     gated_norm_kernel<T, TPR, CH, EVEN><<<block_lines(TPR ? cdiv(a.rows, 256 / (TPR ? TPR : 1)) : a.rows), block, 0, st>>>(a);
     return check_launch("gated_norm_kernel");
 }
-// A row is a wavefront's, or a part of one, where its chunks of eight are that many lanes, and a block's else.  Outputs that do not fit the caches beside the
-// inputs go past them (12,544 x 1536, bf16, y and h: 39 -> 32 us, 4.9 TB/s; 300,000 x 64 41 -> 32); 8-bit rows do not: the product reads
-// them next; nor does fp32, where a store instruction leaves every other 16 bytes (6000 x 3000 66 us and 83).
+// A row is a wavefront's, or a part of one, where its 16-byte chunks are that many lanes, and a block's else.  Outputs go past the caches (12,544 x 1536,
+// bf16, y and h: 39 -> 32 us, 4.9 TB/s; 300,000 x 64 41 -> 32); 8-bit rows do not: the product reads them next.
 template <typename T, bool EVEN>
 static int launch_norm(const NormArgs& a, hipStream_t st) {
-    const int chunks = (int)cdiv(a.C, 8);
-    if (chunks <= 8 && !a.v8) return launch_norm_as<T, 8, 1, EVEN>(a, st);          // (8-bit rows have sixteen chunks at least)
-    if (chunks <= 16) return launch_norm_as<T, 16, 1, EVEN>(a, st);
+    const int chunks = (int)cdiv(a.C, 16 / sizeof(T)), least = a.v8 ? F8_BLOCK * (int)sizeof(T) / 16 : 1;           // (8-bit rows have whole blocks)
+    if (chunks <= 8 && least <= 8) return launch_norm_as<T, 8, 1, EVEN>(a, st);
+    if (chunks <= 16 && least <= 16) return launch_norm_as<T, 16, 1, EVEN>(a, st);
     if (chunks <= 32) return launch_norm_as<T, 32, 1, EVEN>(a, st);
     if (chunks <= 64) return launch_norm_as<T, 64, 1, EVEN>(a, st);
-    // (60,000 x 640, bf16: 91 us by blocks of 128, 75 by wavefronts; 1694 x 1000, fp32: 9.7 and 10.4)
+    // (60,000 x 640, bf16: 91 us by blocks of 128, 75 by wavefronts; 500 x 640 the other way round)
     if (chunks <= 128 && a.rows >= 8192) return launch_norm_as<T, 64, 2, EVEN>(a, st);
     if (chunks <= 512) return launch_norm_as<T, 0, 1, EVEN>(a, st);
-    return launch_norm_as<T, 0, 2, EVEN>(a, st);
+    if (sizeof(T) == 2 || chunks <= 2048) return launch_norm_as<T, 0, 2, EVEN>(a, st);
+    if constexpr (sizeof(T) == 4) return launch_norm_as<T, 0, 4, EVEN>(a, st);
+    return PSERVE_OK;
 }
+
 }  // namespace pserve
 
 extern "C" {
@@ -313,11 +319,10 @@ int pserve_gated_norm(const pserve_gated_norm_desc* d, const pserve_gated_norm_b
     a.rows = d->rows; a.xs = d->x_stride; a.fs = d->f_stride; a.ys = d->y_stride; a.hs = d->h_stride;
     a.gate_s = d->gate_stride; a.scale_s = d->scale_stride; a.shift_s = d->shift_stride;
     a.skip = d->skip_scale; a.branch = d->branch_scale; a.post_eps = d->post_eps; a.pre_eps = d->pre_eps;
-    a.stream = es == 2 && d->rows * d->C * es * ((b->y ? 1 : 0) + (b->h ? 1 : 0)) > (4 << 20);
     a.C = d->C; a.n = d->n; a.post = d->post_norm; a.pre = d->pre_norm;
     hipStream_t st = (hipStream_t)stream;
     if (d->dtype == PSERVE_BF16) return d->C % 8 == 0 ? launch_norm<uint16_t, true>(a, st) : launch_norm<uint16_t, false>(a, st);
-    return d->C % 8 == 0 ? launch_norm<float, true>(a, st) : launch_norm<float, false>(a, st);
+    return d->C % 4 == 0 ? launch_norm<float, true>(a, st) : launch_norm<float, false>(a, st);
 }
 
 }  // extern "C"

@@ -129,11 +129,6 @@ static int launch_rows_write(const void* x, int64_t ldx, int64_t rows, int32_t K
 // block, 16 g4 .. + 15 and 64 + 16 g4 .. + 15), the next block's in flight; the sums meet in LDS, in a fixed order.  FROM_X: rows of x are rounded on the way
 // in, by every block for itself (a row's block of 128 is four lanes).
 
-// v of the lanes with the same number mod 16: their largest, in all of them
-__device__ __forceinline__ uint32_t f8_column_max(uint32_t m) {
-    m = max(m, (uint32_t)__shfl_xor((int)m, 16));
-    return max(m, (uint32_t)__shfl_xor((int)m, 32));
-}
 template <typename T, int MT, int NT, int WV, bool FROM_X>
 __global__ void __launch_bounds__(64 * WV)
 linear_f8_few_kernel(LinearF8Args a) {
@@ -210,7 +205,7 @@ linear_f8_few_kernel(LinearF8Args a) {
                 uint32_t m = 0;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) m = largest8(m, raw[set][i][c]);
-                const F8Scale z(f8_column_max(m));
+                const F8Scale z(max_32_apart(max_16_apart(m)));      // (of the lanes with the same number mod 16)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     float v[8];
