@@ -28,6 +28,7 @@ struct RotaryArgs {
     const int32_t* axis;
     int64_t tokens, qs[2], ks[2], qo[2], ko[2];
     int32_t heads, kv_heads, D, P, axes, TB;    // TB: tokens of a block
+    int32_t lines;                              // store instructions write whole runs of 128 bytes
     int32_t keep;                               // in place: what is not turned stays
 };
 
@@ -50,15 +51,15 @@ struct Divisor {
     __device__ __forceinline__ int operator()(int n) const { return d > 1 ? (int)__umulhi((uint32_t)n, m) : n; }
 };
 
-// An item is two pieces of 16 bytes of a head, at any element's address, V values each.  HALF: the values of V pairs, from p and P + p on, then pieces of what
-// is copied.  NEXT: pieces hold whole pairs, turned or copied; an item's two are half of the head apart, so that neighbouring lanes have neighbouring pieces.
+// An item is K pieces of 16 bytes of a head, at any element's address, V values each.  HALF: two, the values of V pairs, from p and P + p on, then pieces of
+// what is copied, half of that apart.  NEXT: one, of whole pairs, turned or copied.
 // A block's items are numbered line by line (token, head); a thread asks for its first IT items before the angles are formed, so the two ways to
 // memory overlap.
 template <typename T, bool HALF, int IT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 6)
 rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
     extern __shared__ float2 s_turn[];
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T), K = HALF ? 2 : 1;
     typedef typename AnyPiece<T>::type Any;
     const int64_t t0 = block_of_lines() * a.TB;
     if (t0 >= a.tokens) return;
@@ -67,7 +68,7 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
     const int apart = (int)items.d - turned;                    // between the pieces of an item of those
     const T* in;
     T* out;
-    int cs, at[2], len[2];                                      // the token's angles; where the pieces are, and how many values
+    int cs, at[K], len[K];                                      // the token's angles; where the pieces are, and how many values
     bool pairs;                                                 // (HALF) an item of pairs
     auto place = [&](int i) {
         const int line = items(i), c = i - line * (int)items.d, t = heads(line), h = line - t * (int)heads.d, hk = h - a.heads;
@@ -82,20 +83,20 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
         pairs = HALF && c < turned;
         if (pairs) {
             at[0] = c * V;
-            at[1] = a.P + c * V;
-            len[0] = len[1] = min(V, a.P - c * V);
+            at[K - 1] = a.P + c * V;
+            len[0] = len[K - 1] = min(V, a.P - c * V);
         } else {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < K; ++k) {
                 at[k] = begin + (c - turned + k * apart) * V;
                 len[k] = max(0, min(V, last - at[k]));
             }
         }
     };
-    auto load = [&](int i, u32x4 (&x)[2]) {
+    auto load = [&](int i, u32x4 (&x)[K]) {
         place(i);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < K; ++k) {
             if (len[k] == V) x[k] = *reinterpret_cast<const Any*>(in + at[k]);
             else {
                 T v[V];
@@ -105,22 +106,22 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
             }
         }
     };
-    auto finish = [&](int i, u32x4 (&x)[2]) {
+    auto finish = [&](int i, u32x4 (&x)[K]) {
         place(i);
-        T v[2][V];
+        T v[K][V];
         __builtin_memcpy(v, x, sizeof v);
         if constexpr (HALF) {
             if (pairs)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const float2 t = s_turn[cs + min(at[0] + e, a.P - 1)];
-                    const float p = load1(&v[0][e]), q = load1(&v[1][e]);
+                    const float p = load1(&v[0][e]), q = load1(&v[K - 1][e]);
                     store1(&v[0][e], p * t.x - q * t.y);
-                    store1(&v[1][e], p * t.y + q * t.x);
+                    store1(&v[K - 1][e], p * t.y + q * t.x);
                 }
         } else {
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int k = 0; k < K; ++k)
 #pragma unroll
                 for (int e = 0; e < V; e += 2) {
                     const int pair = (at[k] + e) >> 1;
@@ -134,11 +135,11 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
                 }
         }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < K; ++k) {
             if (len[k] == V) {
                 u32x4 o;
                 __builtin_memcpy(&o, v[k], sizeof o);
-                *reinterpret_cast<Any*>(out + at[k]) = o;
+                store_piece(reinterpret_cast<Any*>(out + at[k]), o, a.lines);
             } else {
 #pragma unroll
                 for (int e = 0; e < V; ++e)
@@ -146,7 +147,7 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
             }
         }
     };
-    u32x4 held[IT][2];
+    u32x4 held[IT][K];
 #pragma unroll
     for (int j = 0; j < IT; ++j)
         if (threadIdx.x + 256 * j < total) load(threadIdx.x + 256 * j, held[j]);
@@ -163,16 +164,22 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
 
 template <typename T>
 static int launch_rotary(const RotaryArgs& in, int layout, hipStream_t st) {
-    constexpr int IT = 4, V = 16 / sizeof(T);
+    constexpr int V = 16 / sizeof(T);
     RotaryArgs a = in;
     const bool half = layout == PSERVE_PAIR_HALF;
-    const int H = a.heads + a.kv_heads, rest = (a.keep ? 2 * a.P : a.D) - (half ? 2 * a.P : 0), items = (half ? (int)cdiv(a.P, V) : 0) + (int)cdiv(rest, 2 * V);
-    // IT items a thread, but 512 blocks where the tokens give them; angles of a block: up to 32 KB
-    a.TB = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 * IT / (H * items), cdiv(a.tokens, 512)), 4096 / a.P));
+    const int H = a.heads + a.kv_heads, rest = (a.keep ? 2 * a.P : a.D) - (half ? 2 * a.P : 0), items = half ? (int)cdiv(a.P, V) + (int)cdiv(rest, 2 * V) : (int)cdiv(rest, V);
+    const int each = half ? 4 : 8;              // items of a thread
+    // that many, but 512 blocks where the tokens give them; angles of a block: up to 32 KB
+    a.TB = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(256 * each / (H * items), cdiv(a.tokens, 512)), 4096 / a.P));
+    // Runs of 128 bytes go past the caches (12,544 tokens x 48 heads of 64, neighbours paired, bf16: 44 -> 35 us; runs of 64, 131,072 x 20 heads of 64, would take 150 for 143)
+    auto line = [&](const void* p, const int64_t* s, int n) {
+        return !((uintptr_t)p & 63) && (a.tokens == 1 || s[0] * (int64_t)sizeof(T) % 64 == 0) && (n == 1 || s[1] * (int64_t)sizeof(T) % 64 == 0);
+    };
+    a.lines = (half ? a.P : a.D) * (int)sizeof(T) % 128 == 0 && line(a.q_out, a.qo, a.heads) && (!a.kv_heads || line(a.k_out, a.ko, a.kv_heads));
     const dim3 grid = block_lines(cdiv(a.tokens, a.TB));
     const size_t lds = (size_t)a.TB * a.P * sizeof(float2);
-    if (half) rotary_kernel<T, true, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
-    else rotary_kernel<T, false, IT><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
+    if (half) rotary_kernel<T, true, 4><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
+    else rotary_kernel<T, false, 8><<<grid, 256, lds, st>>>(a, Divisor(items), Divisor(H));
     return check_launch("rotary_kernel");
 }
 
