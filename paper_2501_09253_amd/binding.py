@@ -607,8 +607,9 @@ def _workspace(need: int, workspace, device, who: str):
 def _apart(who: str, out, *inputs):
     """`out` shares no byte with an input (dense or strided: the extents are compared)."""
     def extent(t):
-        last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
-        return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+        values = t.numel() if t.is_contiguous() else 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+        at = t.data_ptr()
+        return at, at + values * t.element_size()
     if out.numel() == 0:
         return
     o0, o1 = extent(out)
@@ -875,24 +876,34 @@ class Rotary:
         who = "Rotary.forward"
         _here(who, q, k, pos, q_out, k_out)
         dtype = _dtype_code(who, q)
-        if q.dim() != 3 or q.shape[1] == 0 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[1] == 0 or k.shape[2] != q.shape[2] or k.dtype != q.dtype)):
+        shape = q.shape
+        if len(shape) != 3 or shape[1] == 0:
             raise PserveError(EINVAL, f"{who}: q [T, heads, D], k [T, kv_heads, D] of one dtype")
-        _ints(who, pos, torch.float32, (q.shape[0], self.axes), "pos")
-        _need(k is not None or k_out is None, f"{who}: k_out without k")
+        T, H, D = shape
+        _ints(who, pos, torch.float32, (T, self.axes), "pos")
+        sq = q.stride()
+        Hk, sk = 0, (0, 0, 1)
+        if k is not None:
+            if k.dim() != 3 or k.shape[0] != T or k.shape[1] == 0 or k.shape[2] != D or k.dtype != q.dtype:
+                raise PserveError(EINVAL, f"{who}: q [T, heads, D], k [T, kv_heads, D] of one dtype")
+            Hk, sk = k.shape[1], k.stride()
+        elif k_out is not None:
+            raise PserveError(EINVAL, f"{who}: k_out without k")
+        if D > 1 and (sq[2] != 1 or sk[2] != 1):
+            raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out, sqo = torch.empty_like(q, memory_format=torch.contiguous_format), (H * D, D)
         else:
             self._given(who, q_out, q, pos, k, k_out)
+            sqo = q_out.stride()
+        sko = (0, 0)
         if k is not None:
             if k_out is None:
-                k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+                k_out, sko = torch.empty_like(k, memory_format=torch.contiguous_format), (Hk * D, D)
             else:
                 self._given(who, k_out, k, pos, q, None)
-        for t in (q, k):
-            if t is not None and t.stride(2) != 1 and t.shape[2] > 1:
-                raise PserveError(EINVAL, f"{who}: the values of a head must be consecutive")
-        d = _rotary_desc(q.shape[1], 0 if k is None else k.shape[1], q.shape[2], dtype, q.shape[0], q.stride(), (0, 0) if k is None else k.stride(),
-                         q_out.stride(), (0, 0) if k is None else k_out.stride())
+                sko = k_out.stride()
+        d = _rotary_desc(H, Hk, D, dtype, T, sq, sk, sqo, sko)
         if k is None:
             _check(lib().pserve_rotary_forward(self._h, d, pos.data_ptr(), q.data_ptr(), None, q_out.data_ptr(), None, _stream()))
         else:
@@ -1056,7 +1067,8 @@ def gated_norm(x, f=None, *, post: Optional[str] = None, post_gain=None, post_bi
     dtype = _dtype_code(who, x)
     if x.dim() != 2:
         raise PserveError(EINVAL, f"{who}: x must be [rows, C]")
-    rows, Cc = x.shape
+    shape, dt = x.shape, x.dtype
+    rows, Cc = shape
     if post not in NORM or pre not in NORM:
         raise PserveError(EINVAL, f"{who}: unknown norm")
     n = 1
@@ -1067,51 +1079,63 @@ def gated_norm(x, f=None, *, post: Optional[str] = None, post_gain=None, post_bi
         n, cu_p, which_p = plan.n, plan.table_device_ptr("cu_seqlens"), plan.table_device_ptr("perm")
     else:
         if cu_rows is not None:
-            _need(cu_rows.dim() == 1 and cu_rows.shape[0] >= 2, f"{who}: cu_rows must be int32 [n + 1], n > 0")
-            _ints(who, cu_rows, torch.int32, cu_rows.shape, "cu_rows")
+            if cu_rows.dim() != 1 or cu_rows.shape[0] < 2 or cu_rows.dtype != torch.int32 or not cu_rows.is_contiguous():
+                raise PserveError(EINVAL, f"{who}: cu_rows must be contiguous int32 [n + 1], n > 0")
             n, cu_p = cu_rows.shape[0] - 1, cu_rows.data_ptr()
         if which is not None:
             _ints(who, which, torch.int32, (n,), "which")
             which_p = which.data_ptr()
-    ends = f is not None
     begins = rows8 is not None or h is not None or pre is not None or pre_gain is not None or pre_bias is not None or scale is not None or shift is not None
-    for t in (post_gain, post_bias, pre_gain, pre_bias):
-        if t is not None and (t.shape != (Cc,) or t.dtype != x.dtype or not t.is_contiguous()):
-            raise PserveError(EINVAL, f"{who}: gains and biases must be contiguous [{Cc}] of x's dtype")
-    for t in (gate, scale, shift):
-        if t is not None and (t.shape != (n, Cc) or t.dtype != x.dtype or (t.stride(1) != 1 and Cc > 1)):
+    buffers = _GatedNormBuffers()
+    buffers.cu_rows, buffers.which = cu_p, which_p
+    # vectors of C values; of the requests; rows
+    for name, t in (("post_gain", post_gain), ("post_bias", post_bias), ("pre_gain", pre_gain), ("pre_bias", pre_bias)):
+        if t is not None:
+            if t.shape != shape[1:] or t.dtype != dt or not t.is_contiguous():
+                raise PserveError(EINVAL, f"{who}: gains and biases must be contiguous [{Cc}] of x's dtype")
+            setattr(buffers, name, t.data_ptr())
+    strides = []
+    for name, t in (("gate", gate), ("scale", scale), ("shift", shift)):
+        if t is None:
+            strides.append(0)
+            continue
+        st = t.stride()
+        if t.dim() != 2 or t.shape[0] != n or t.shape[1] != Cc or t.dtype != dt or (st[1] != 1 and Cc > 1):
             raise PserveError(EINVAL, f"{who}: gate, scale and shift must be [{n}, {Cc}] of x's dtype, the values of a request consecutive")
+        strides.append(st[0] if n > 1 else Cc)
+        setattr(buffers, name, t.data_ptr())
+    spaced = []
+    for name, t, new in (("x", x, False), ("f", f, False), ("y", y, f is not None), ("h", h, begins and rows8 is None)):
+        if t is None:
+            spaced.append(Cc if new else 0)
+            continue
+        st = t.stride()
+        if t.shape != shape or t.dtype != dt or (st[1] != 1 and Cc > 1) or (rows > 1 and st[0] < Cc):
+            raise PserveError(EINVAL, f"{who}: x, f, y and h must be [{rows}, {Cc}] of one dtype, the values of a row consecutive, rows apart")
+        spaced.append(st[0] if rows > 1 else Cc)
+        setattr(buffers, name, t.data_ptr())
     if rows8 is not None:
         _need(h is None, f"{who}: h and rows8 at once")
         _need((rows8.rows, rows8.K) == (rows, Cc), f"{who}: rows8 must have {rows} rows of {Cc} values")
-    for t in (x, f, y, h):
-        if t is not None and (t.shape != (rows, Cc) or t.dtype != x.dtype or (t.stride(1) != 1 and Cc > 1) or (rows > 1 and t.stride(0) < Cc)):
-            raise PserveError(EINVAL, f"{who}: x, f, y and h must be [{rows}, {Cc}] of one dtype, the values of a row consecutive, rows apart")
-    vectors = (post_gain, post_bias, gate, pre_gain, pre_bias, scale, shift, cu_rows, which)
-    for out, other in ((y, h), (h, y)):
-        if out is not None:
-            for t in (x, f):
-                if t is not None and not (t.data_ptr() == out.data_ptr() and (t.stride(0) == out.stride(0) or rows <= 1)):
-                    _apart(who, out, t)
-            _apart(who, out, other, *vectors)
-    if rows8 is not None:
-        _apart(who, rows8.buffer, x, f, y, *vectors)
-    if y is None and ends:
-        y = torch.empty((rows, Cc), dtype=x.dtype, device=x.device)
+    if y is not None or h is not None or rows8 is not None:
+        vectors = (post_gain, post_bias, gate, pre_gain, pre_bias, scale, shift, cu_rows, which)
+        for out, other in ((y, h), (h, y)):
+            if out is not None:
+                for t in (x, f):
+                    if t is not None and not (t.data_ptr() == out.data_ptr() and (t.stride(0) == out.stride(0) or rows <= 1)):
+                        _apart(who, out, t)
+                _apart(who, out, other, *vectors)
+        if rows8 is not None:
+            _apart(who, rows8.buffer, x, f, y, *vectors)
+            buffers.rows8 = rows8.buffer.data_ptr()
+    if y is None and f is not None:
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        buffers.y = y.data_ptr()
     if h is None and begins and rows8 is None:
-        h = torch.empty((rows, Cc), dtype=x.dtype, device=x.device)
-
-    def stride(t):
-        return 0 if t is None else Cc if t.shape[0] <= 1 else t.stride(0)
-
-    def ptr(t):
-        return None if t is None else t.data_ptr()
-
-    d = _gated_norm_desc(Cc, dtype, n, NORM[post], NORM[pre], float(post_eps), float(pre_eps), float(skip_scale), float(branch_scale), rows,
-                         stride(x), stride(f), stride(y), stride(h), stride(gate), stride(scale), stride(shift))
-    b = _GatedNormBuffers(ptr(x), ptr(f), ptr(post_gain), ptr(post_bias), ptr(gate), ptr(pre_gain), ptr(pre_bias), ptr(scale), ptr(shift),
-                          cu_p, which_p, ptr(y), ptr(h), None if rows8 is None else rows8.buffer.data_ptr())
-    _check(lib().pserve_gated_norm(d, C.byref(b), _stream()))
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
+        buffers.h = h.data_ptr()
+    d = _gated_norm_desc(Cc, dtype, n, NORM[post], NORM[pre], float(post_eps), float(pre_eps), float(skip_scale), float(branch_scale), rows, *spaced, *strides)
+    _check(lib().pserve_gated_norm(d, C.byref(buffers), _stream()))
     return y, h
 
 
