@@ -93,7 +93,19 @@ template <typename T> struct AnyPiece;
 template <> struct AnyPiece<uint16_t> { typedef u32x4 __attribute__((aligned(2))) type; };
 template <> struct AnyPiece<float> { typedef u32x4 __attribute__((aligned(4))) type; };
 
-// A store, past the caches where `past` says so.  (The empty statements keep the compiler from making one store of the two.)
+// A load or store, past the caches where `past` says so.  (The empty statements keep the compiler from making one store of the two.)
+template <typename P>
+__device__ __forceinline__ u32x4 load_piece(const P* p, bool past) {
+    u32x4 v;
+    if (past) {
+        asm volatile("");
+        v = __builtin_nontemporal_load(p);
+        asm volatile("");
+    } else {
+        v = *p;
+    }
+    return v;
+}
 template <typename P>
 __device__ __forceinline__ void store_piece(P* p, const u32x4& v, bool past) {
     if (past) {

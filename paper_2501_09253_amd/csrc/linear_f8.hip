@@ -306,7 +306,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
     constexpr int CH = 4 * HB, RP = 64 / CH * NW, A_LD = BM / RP, B_LD = BN / RP, LD = A_LD + B_LD, STAGE_V = Cfg::STAGE / 16;
     constexpr int S_LD = (BM + BN + 64 * NW - 1) / (64 * NW);
     constexpr bool ALONE = Cfg::LDS > 80 * 1024;            // a block a CU
-    constexpr int GM = 8;                                   // row tiles of a group, see below
+    constexpr int GM = 4;                                   // row tiles of a group, see below
     extern __shared__ __attribute__((aligned(16))) uint8_t lf_smem[];
     u32x4* ring = reinterpret_cast<u32x4*>(lf_smem);        // [NS][rows of x, rows of w][CH chunks], swizzled: sixteen rows, all banks
     uint32_t* s_scale = reinterpret_cast<uint32_t*>(lf_smem + NS * Cfg::STAGE);      // [2][rows of x, rows of w] words of four blocks
@@ -504,7 +504,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
                 const T* rp = (const T*)a.res + row * a.N + n;
                 u32x4 v = {0, 0, 0, 0};
                 if (row < a.rows) {
-                    if (n + CV <= a.N) v = *reinterpret_cast<const Any*>(rp);
+                    if (n + CV <= a.N) v = load_piece(reinterpret_cast<const Any*>(rp), lines);
                     else if (n < a.N) {
                         T e[CV];
 #pragma unroll
@@ -611,16 +611,20 @@ static int launch_tile_as(const LinearF8Args& a, hipStream_t st) {
     linear_f8_tile_kernel<T, RES, WGM, WGN, TM, TN, HB, NS><<<grid, 64 * Cfg::NW, Cfg::LDS, st>>>(a, (int)mt, (int)total);
     return check_launch("linear_f8_tile_kernel");
 }
-// Of the tiles the one with the least time by its rounds (256 blocks at a time of the largest tile, 512 of the others), us a round: so much for each
-// block of K and so much for its beginning and end, fitted to 4096 .. 16384 rows (256 x 256 / 128 x 128 / 64 x 128 us, bf16): 12,544 x 1536 x 6144 with
-// a residual 158 / 164 / 197, 12,544 x 6144 x 1536 with one 164 / 144 / 177, 2048 x 4096 x 4096 46 / 36 / 45, 3000 x 3000 x 3000 37 / 43 / 41,
-// 2048 x 2048 x 2048 29 / 17 / 14, 100 x 2048 x 8192 25 / 13 / 9, 6000 x 1000 x 3000 with a residual 53 / 40 / 43; fp32: 8000 x 500 x 1500 with one 64 / 37 / 36 (the
-// largest tile's operands spill there, and it is left out), 500 x 3000 x 2000 68 / 26 / 19
+// Of the tiles the one with the least time by its rounds (256 blocks at a time of the largest tile, 512 of the others, of which the last round's are alone
+// on their CUs), us a round: so much for each block of K and so much for its beginning and end, fitted to (256 x 256 / 128 x 128 / 64 x 128 us, bf16) 12,544 x 1536 x 6144
+// with a residual 158 / 164 / 197, 12,544 x 6144 x 1536 with one 164 / 144 / 177, 2048 x 4096 x 4096 46 / 36 / 45, 3000 x 3000 x 3000 37 / 43 / 41, 2048 x 2048 x 2048
+// 29 / 17 / 14, 100 x 2048 x 8192 25 / 13 / 9, 6000 x 1000 x 3000 with a residual 53 / 40 / 43; fp32: 8000 x 500 x 1500 with one 64 / 37 / 36 (the largest
+// tile's operands spill there, and it is left out), 500 x 3000 x 2000 68 / 26 / 19
 template <typename T, bool RES>
 static int launch_tile_res(const LinearF8Args& a, hipStream_t st) {
     constexpr bool HALF = sizeof(T) == 2;
     const double KT = a.Kp / 128;
-    auto cost = [&](int bm, int bn, int at_once, double step, double ends) { return (double)cdiv(cdiv(a.rows, bm) * cdiv(a.N, bn), at_once) * (step * KT + ends); };
+    auto cost = [&](int bm, int bn, int at_once, double step, double ends) {
+        const int64_t tiles = cdiv(a.rows, bm) * cdiv(a.N, bn), rest = tiles % at_once;
+        const double last = rest == 0 ? 0.0 : at_once == 256 ? 1.0 : 0.55 + 0.45 * (double)rest / at_once;
+        return ((double)(tiles / at_once) + last) * (step * KT + ends);
+    };
     const double small = HALF ? cost(64, 128, 512, 0.64, RES ? 4.5 : 4.0) : cost(64, 128, 512, 1.05, 7.5);
     const double mid = HALF ? cost(128, 128, 512, 1.06, RES ? 6.0 : 5.0) : cost(128, 128, 512, 1.85, 13.0);
     if constexpr (HALF)
