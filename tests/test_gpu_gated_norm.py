@@ -88,10 +88,12 @@ def test_parts_left_out(left_out, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("counts", [[1], [0, 3, 0, 5, 1, 0], [1] * 70, [0] * 40 + [7] + [0] * 30 + [2], [3, 0] * 100, [1] * 5000])
-def test_requests(counts, dtype):
+@pytest.mark.parametrize("counts,C", [([1], 96), ([0, 3, 0, 5, 1, 0], 96), ([1] * 70, 96), ([0] * 40 + [7] + [0] * 30 + [2], 96), ([3, 0] * 100, 96), ([1] * 5000, 96),
+                                      ([0, 3, 0, 5, 1, 0], 24), ([1] * 70, 30), ([1] * 63, 500), ([2] * 64, 480), ([0, 2] * 40, 640), ([0, 3, 0, 5, 1, 0], 1536),
+                                      ([1] * 62 + [0], 1536), ([0] + [1] * 62, 700), ([1, 0] * 200, 1000), ([5, 0, 9], 9000)])
+def test_requests(counts, C, dtype):
     """Every request has its own vectors; empty requests; rows in front of the first and behind the last are left as they were."""
-    n, C, front, behind = len(counts), 96, 2, 3
+    n, front, behind = len(counts), 2, 3
     rows = front + sum(counts) + behind
     t = inputs(rows, C, dtype, n)
     cu = [front]
@@ -111,7 +113,8 @@ def test_requests(counts, dtype):
     rows8 = ps.RowsF8(rows, C)
     rows8.buffer.fill_(33)
     ps.gated_norm(**gpu(t), post="layer", pre="rms", cu_rows=ints(cu), rows8=rows8)
-    numbers, scales = rows8.buffer[:rows * 128].view(rows, 128), rows8.buffer[rows * 128:].view(rows, 4)
+    width, exponents = -(-C // 128) * 128, -(-C // 512) * 4
+    numbers, scales = rows8.buffer[:rows * width].view(rows, width), rows8.buffer[rows * width:].view(rows, exponents)
     for part in (slice(0, front), slice(rows - behind, rows)):
         assert torch.all(numbers[part] == 33) and torch.all(scales[part] == 33)
 
@@ -200,6 +203,19 @@ def test_many_rows():
     wy, wh = lo.gated_norm(**t, post="rms", pre="layer", request=request)
     near(y, wy, "bf16")
     near(h, wh, "bf16")
+
+
+def test_offsets_past_32_bits():
+    """2.5e9 values: the last rows are what they are in a call of their own."""
+    rows, C = 610000, 4096
+    x = torch.empty((rows, C), dtype=torch.bfloat16, device="cuda")
+    tail = make(1, (40, C), torch.bfloat16).cuda()
+    x.view(-1, 40, C)[:] = tail
+    x[-7:] = tail[:7] * 3
+    g = make(2, (C,), torch.bfloat16).cuda()
+    y, h = ps.gated_norm(x, x, post="rms", post_gain=g, pre="layer", y=torch.empty_like(x))
+    want = ps.gated_norm(x[-40:].clone(), x[-40:].clone(), post="rms", post_gain=g, pre="layer")
+    assert torch.equal(y[-40:], want[0]) and torch.equal(h[-40:], want[1]) and torch.equal(y[:33], y[-40:-7])
 
 
 def test_no_rows():

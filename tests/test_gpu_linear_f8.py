@@ -106,6 +106,18 @@ def test_large_layers(rows, K, N):
     assert torch.all((layer.forward(rows8).double() - want).abs() <= tol)
 
 
+def test_offsets_past_32_bits():
+    """2.5e9 outputs: the last rows are what they are in a call of their own (of as many rows as the tiles need)."""
+    rows, K, N = 610000, 64, 4096
+    x, w = torch.empty((rows, K), dtype=torch.bfloat16, device="cuda"), make(2, (K, N), torch.bfloat16, K ** -0.5).cuda()
+    x.view(-1, 1000, K)[:] = make(1, (1000, K), torch.bfloat16).cuda()
+    x[-5:] *= 2
+    layer = ps.LinearF8(w, None, ps.BF16)
+    got = layer.forward(x)
+    for part in (slice(rows - 3000, rows), slice(rows // 2, rows // 2 + 3000)):
+        assert torch.equal(got[part], layer.forward(x[part].clone()))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [1, 40, 200])
 def test_one_key_is_seen(rows, dtype):

@@ -54,6 +54,21 @@ def test_lengths(tokens):
     check(gk, k, pos, axis, freq, True)
 
 
+@pytest.mark.parametrize("layout", ["half", "next"])
+def test_offsets_past_32_bits(layout):
+    """2.5e9 values in and out: the last tokens are what they are in a call of their own."""
+    T, H, D = 300000, 64, 128
+    axis, freq = ps.rotary_ladder((16, 24, 24))
+    rot = ps.Rotary(axis, freq, layout)
+    q = torch.empty((T, H, D), dtype=torch.bfloat16, device="cuda")
+    q.view(-1, 100, H, D)[:] = make(1, (100, H, D), torch.bfloat16).cuda()
+    q[-3:] *= 2
+    pos = positions(2, T, 3, 1e5).cuda()
+    got, _ = rot.forward(q, None, pos)
+    for part in (slice(T - 50, T), slice(T // 2, T // 2 + 50)):
+        assert torch.equal(got[part], rot.forward(q[part].clone(), None, pos[part].contiguous())[0])
+
+
 def test_no_tokens():
     rot = ps.Rotary([0], [1.0])
     q = torch.empty((0, 2, 8), dtype=torch.float32, device="cuda")
