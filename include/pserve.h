@@ -445,7 +445,7 @@ int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t l
  *   A row of x (column of W) with an infinity or a NaN gives NaN.
  * pserve_linear_f8_create: w DEVICE [K][N], b DEVICE [N] or NULL, of dtype; synchronises `stream`; the caller's buffers are not referenced afterwards.
  * pserve_linear_f8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y), y DEVICE [rows][N];
- *   workspace DEVICE, 16-byte aligned, at least pserve_linear_f8_workspace bytes.  y must not overlap x.  pserve_linear_f8_forward_rows: the rows as
+ *   workspace DEVICE, 16-byte aligned, at least pserve_linear_f8_workspace bytes (0 where a few rows need none).  y must not overlap x.  pserve_linear_f8_forward_rows: the rows as
  *   rows8, no workspace.
  * Errors: EINVAL (NULL, sizes <= 0, K above 131072, N above 2^24, 2^26 rows and more, ldx < K, workspace too small, buffers off their alignment, another
  * device than the current one), ENOMEM, EHIP. */

@@ -994,7 +994,8 @@ class LinearF8:
         _need(b is None or (tuple(b.shape) == (w.shape[1],) and b.is_contiguous() and b.dtype == w.dtype), f"{who}: b must be contiguous [N] of the given dtype")
         self.dtype, self.K, self.N = dtype, _whole(who, "K", w.shape[0]), _whole(who, "N", w.shape[1])
         _check(lib().pserve_linear_f8_create(self.K, self.N, dtype, w.data_ptr(), None if b is None else b.data_ptr(), _stream(), C.byref(self._h)))
-        self._dtype, self._row_bytes = w.dtype, self.workspace_bytes(1)         # (workspace_bytes is linear in the rows)
+        # workspace_bytes is linear in the rows but for a few, which may need none
+        self._dtype, self._row_bytes, self._bare = w.dtype, self.workspace_bytes(1 << 20) >> 20, max((r for r in (0, 1, 16) if self.workspace_bytes(r) == 0))
 
     def workspace_bytes(self, rows: int) -> int:
         n = C.c_size_t()
@@ -1024,14 +1025,14 @@ class LinearF8:
             if t is not None and (t.shape != (rows, self.N) or not t.is_contiguous() or t.dtype != self._dtype):
                 raise PserveError(EINVAL, f"{who}: res and y must be contiguous [rows, {self.N}] of the layer's dtype")
         if y is None:
-            y = torch.empty((rows, self.N), dtype=self._dtype, device=source.device)
+            y = source.new_empty((rows, self.N), dtype=self._dtype)
         else:
             _apart(who, y, source, *([res] if res is not None and res.data_ptr() != y.data_ptr() else []))
         rp = None if res is None else res.data_ptr()
         if held:
             _check(lib().pserve_linear_f8_forward_rows(self._h, source.data_ptr(), rows, rp, y.data_ptr(), _stream()))
             return y
-        ws, nws, keep = _workspace(rows * self._row_bytes, workspace, x.device, who)
+        ws, nws, keep = _workspace(0 if rows <= self._bare else rows * self._row_bytes, workspace, x.device, who)
         _check(lib().pserve_linear_f8_forward(self._h, x.data_ptr(), ldx, rows, rp, ws, nws, y.data_ptr(), _stream()))
         return y
 

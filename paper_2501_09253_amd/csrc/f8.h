@@ -23,37 +23,76 @@ __host__ __device__ inline int32_t f8_width(int32_t K) { return (K + 127) / 128 
 __host__ __device__ inline int32_t f8_scales(int32_t K) { return (K + 511) / 512 * 4; }
 inline size_t f8_bytes(int64_t rows, int32_t K) { return (size_t)rows * (size_t)(f8_width(K) + f8_scales(K)); }
 
+// four numbers of a word: x / 2^e for two values of each pair, as the scaled conversion rounds them (the same as a multiplication and a conversion)
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
 struct F8Scale {
     uint32_t amax, byte;
-    float mul;                                          // 2^-e
+    float scale;                                        // 2^e
     __device__ __forceinline__ explicit F8Scale(uint32_t amax_bits) : amax(amax_bits) {
         // the exponent field counts up where the fraction passes 0.75 (448 = 1.75 * 2^8)
         const uint32_t up = (amax_bits + 0x1fffffu) >> 23;
         byte = min(max(up, F8_FIRST_BYTE + 8u) - 8u, F8_LAST_BYTE);
         if (amax_bits >= 0x7f800000u) byte = 127;
-        mul = __uint_as_float((254u - byte) << 23);
+        scale = __uint_as_float(byte << 23);
     }
-    __device__ __forceinline__ q8_u32x2 pack8(const float (&v)[8]) const {
-        float s[8];
+    __device__ __forceinline__ uint32_t word(float a, float b, float c, float d) const {
+        s16x2 o = {0, 0};
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, a, b, scale, false);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(o, c, d, scale, true);
+        return __builtin_bit_cast(uint32_t, o);
+    }
+    // N values as bytes
+    template <int N>
+    __device__ __forceinline__ void words(const float (&v)[N], uint32_t (&o)[N / 4]) const {
+        if (amax <= F8_LARGEST_BITS) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = v[i] * mul;
-        if (amax > F8_LARGEST_BITS) {                   // (the conversion does not cut off)
+            for (int i = 0; i < N / 4; ++i) o[i] = word(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        } else {                                        // what is too large is cut off; a block that is not finite is NaN
+            const float most = 448.f * 0x1p119f;
+            float s[N];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] = fminf(fmaxf(s[i], -448.f), 448.f);
+            for (int i = 0; i < N; ++i) s[i] = fminf(fmaxf(v[i], -most), most);
+#pragma unroll
+            for (int i = 0; i < N / 4; ++i) o[i] = amax >= 0x7f800000u ? F8_NAN4 : word(s[4 * i], s[4 * i + 1], s[4 * i + 2], s[4 * i + 3]);
+        }
+    }
+    // Eight values as they lie in memory
+    __device__ __forceinline__ q8_u32x2 pack8(const Raw8<float>& r) const {
+        float v[8];
+        uint32_t o[2];
+        values8(r, v);
+        words(v, o);
+        return q8_u32x2{o[0], o[1]};
+    }
+    __device__ __forceinline__ q8_u32x2 pack8(const Raw8<uint16_t>& r) const {
+        if (amax > F8_LARGEST_BITS) {
+            float v[8];
+            uint32_t o[2];
+            values8(r, v);
+            words(v, o);
+            return q8_u32x2{o[0], o[1]};
         }
         q8_u32x2 o;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(s[4 * h], s[4 * h + 1], 0, false);
-            w = __builtin_amdgcn_cvt_pk_fp8_f32(s[4 * h + 2], s[4 * h + 3], w, true);
-            o[h] = amax >= 0x7f800000u ? F8_NAN4 : (uint32_t)w;
+            s16x2 w = {0, 0};
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, (uint32_t)r.w[0][2 * h]), scale, false);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, (uint32_t)r.w[0][2 * h + 1]), scale, true);
+            o[h] = __builtin_bit_cast(uint32_t, w);
         }
         return o;
     }
-    __device__ __forceinline__ void pack(const float (&v)[8], uint8_t* o) const { *reinterpret_cast<q8_u32x2*>(o) = pack8(v); }
+    __device__ __forceinline__ void pack(const float (&v)[8], uint8_t* o) const {
+        uint32_t w[2];
+        words(v, w);
+        *reinterpret_cast<q8_u32x2*>(o) = q8_u32x2{w[0], w[1]};
+    }
     __device__ __forceinline__ void pack(const float (&v)[4], uint8_t* o) const {
-        const float w[8] = {v[0], v[1], v[2], v[3], 0.f, 0.f, 0.f, 0.f};
-        *reinterpret_cast<uint32_t*>(o) = pack8(w)[0];
+        uint32_t w[1];
+        words(v, w);
+        *reinterpret_cast<uint32_t*>(o) = w[0];
     }
 };
 
@@ -93,9 +132,10 @@ template <typename T> struct AnyPiece;
 template <> struct AnyPiece<uint16_t> { typedef u32x4 __attribute__((aligned(2))) type; };
 template <> struct AnyPiece<float> { typedef u32x4 __attribute__((aligned(4))) type; };
 
-// A load or store, past the caches where `past` says so.  (The empty statements keep the compiler from making one store of the two.)
-template <typename P>
-__device__ __forceinline__ u32x4 load_piece(const P* p, bool past) {
+// 16 bytes from or to any element's address, past the caches where `past` says so.  (The empty statements keep the compiler from making one of the two.)
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T* at, bool past) {
+    const auto* p = reinterpret_cast<const typename AnyPiece<T>::type*>(at);
     u32x4 v;
     if (past) {
         asm volatile("");
@@ -106,8 +146,9 @@ __device__ __forceinline__ u32x4 load_piece(const P* p, bool past) {
     }
     return v;
 }
-template <typename P>
-__device__ __forceinline__ void store_piece(P* p, const u32x4& v, bool past) {
+template <typename T>
+__device__ __forceinline__ void store_piece(T* at, const u32x4& v, bool past) {
+    auto* p = reinterpret_cast<typename AnyPiece<T>::type*>(at);
     if (past) {
         asm volatile("");
         __builtin_nontemporal_store(v, p);

@@ -22,7 +22,6 @@ struct pserve_linear_f8_s {
 namespace pserve {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 // 8 of a lane's 32 numbers times their scale, as bf16 (exact)
 __device__ __forceinline__ bf16x8 f8_as_bf16(const i32x8& v, int q, int byte) {
@@ -70,13 +69,13 @@ linear_f8_pack_kernel(const T* w, int32_t K, int32_t N, int32_t Kp, int32_t Sp, 
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[j][32 * q + 8 * i + e];
-        *reinterpret_cast<q8_u32x2*>(o + 8 * i) = z.pack8(v);
+        z.pack(v, o + 8 * i);
     }
     if (q == 0) scale[(int64_t)(n0 + j) * Sp + blockIdx.y] = (uint8_t)z.byte;
 }
 
 // ---- rows of x: a block of 128 is sixteen lanes of eight values each; blocks are numbered row by row
-template <typename T, bool VEC>
+template <typename T, bool EVEN>
 __global__ void __launch_bounds__(256)
 f8_rows_write_kernel(const T* x, int64_t ldx, int64_t rows, int32_t K, uint8_t* x8, uint8_t* sx) {
     const int Kp = f8_width(K), Sp = f8_scales(K), KB = Kp / 128, lane = threadIdx.x & 15;
@@ -85,18 +84,19 @@ f8_rows_write_kernel(const T* x, int64_t ldx, int64_t rows, int32_t K, uint8_t* 
     const int64_t row = blk / KB;
     const int b = (int)(blk - row * KB), c = 16 * b + lane;
     const T* p = x + row * ldx + 8 * c;
-    float v[8];
-    if (VEC) {
-        if (8 * c < K) load8(p, v);
-        else
+    typedef typename AnyPiece<T>::type Any;
+    Raw8<T> r;
+    if (EVEN ? 8 * c < K : 8 * c + 8 <= K) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) r.w[h] = *reinterpret_cast<const Any*>(p + h * (16 / sizeof(T)));
     } else {
+        T v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 8 * c + e < K ? load1(p + e) : 0.f;
+        for (int e = 0; e < 8; ++e) v[e] = !EVEN && 8 * c + e < K ? p[e] : T(0);
+        __builtin_memcpy(&r, v, sizeof r);
     }
-    const F8Scale z(lanes_max<16>(f8_largest(v)));
-    *reinterpret_cast<q8_u32x2*>(x8 + row * Kp + 8 * c) = z.pack8(v);
+    const F8Scale z(lanes_max<16>(largest8(0u, r)));
+    *reinterpret_cast<q8_u32x2*>(x8 + row * Kp + 8 * c) = z.pack8(r);
     if (lane == 0) sx[row * Sp + b] = (uint8_t)z.byte;
     if (lane == 0 && b == 0)
         for (int i = KB; i < Sp; ++i) sx[row * Sp + i] = 127;
@@ -120,7 +120,7 @@ f8_rows_read_kernel(const uint8_t* x8, const uint8_t* sx, int64_t rows, int32_t 
 template <typename T>
 static int launch_rows_write(const void* x, int64_t ldx, int64_t rows, int32_t K, uint8_t* x8, uint8_t* sx, hipStream_t st) {
     const dim3 grid = block_lines(cdiv(rows * (f8_width(K) / 128), 16));
-    if (K % 8 == 0 && ldx % (16 / sizeof(T)) == 0 && !((uintptr_t)x & 15)) f8_rows_write_kernel<T, true><<<grid, 256, 0, st>>>((const T*)x, ldx, rows, K, x8, sx);
+    if (K % 8 == 0) f8_rows_write_kernel<T, true><<<grid, 256, 0, st>>>((const T*)x, ldx, rows, K, x8, sx);
     else f8_rows_write_kernel<T, false><<<grid, 256, 0, st>>>((const T*)x, ldx, rows, K, x8, sx);
     return check_launch("f8_rows_write_kernel");
 }
@@ -208,9 +208,7 @@ linear_f8_few_kernel(LinearF8Args a) {
                 const F8Scale z(max_32_apart(max_16_apart(m)));      // (of the lanes with the same number mod 16)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    float v[8];
-                    values8(raw[set][i][c], v);
-                    const q8_u32x2 p = z.pack8(v);
+                    const q8_u32x2 p = z.pack8(raw[set][i][c]);
                     x[0][i][2 * c] = (int)p[0];
                     x[0][i][2 * c + 1] = (int)p[1];
                 }
@@ -269,8 +267,7 @@ static int launch_few_as(const LinearF8Args& a, hipStream_t st) {
 constexpr int LF_FEW = 32;                      // rows
 // us in a captured stream, a launch of 2.4 for the rows of x included: 12 x 4096 x 4096 bf16 9.7 rounded in here, 9.9 in a launch of its own (which costs the host another
 // launch, too); 16 x 8192 x 8192 34 and 23, 32 x 4096 x 4096 14.6 and 13.4, 12 x 4096 x 4096 fp32 13.1 and 10.1: every block reads all of x
-template <typename T>
-static bool few_from_x(const LinearF8Args& a) { return sizeof(T) == 2 && a.rows <= 16 && a.N < 6144; }
+static bool few_from_x(int dtype, int64_t rows, int32_t N) { return dtype == PSERVE_BF16 && rows <= 16 && N < 6144; }
 // 32 channels a block where that still makes 192 blocks (16 x 8192 x 8192 25.5 -> 19.8, 12 x 1536 x 6144 5.5 -> 4.9, but 12 x 4096 x 4096 7.5 -> 10.0).  Four
 // row tiles are slower than tiles in LDS (33 x 4096 x 4096 17.4 and 14.5)
 template <typename T>
@@ -504,7 +501,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
                 const T* rp = (const T*)a.res + row * a.N + n;
                 u32x4 v = {0, 0, 0, 0};
                 if (row < a.rows) {
-                    if (n + CV <= a.N) v = load_piece(reinterpret_cast<const Any*>(rp), lines);
+                    if (n + CV <= a.N) v = load_piece(rp, lines);
                     else if (n < a.N) {
                         T e[CV];
 #pragma unroll
@@ -581,7 +578,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
                 const u32x4 o = ep[rr * 8 + (ec ^ ((rr >> 1) & 7))];
                 T* yp = (T*)a.y + row * a.N + n;
                 if (row < a.rows && n + CV <= a.N) {
-                    store_piece(reinterpret_cast<Any*>(yp), o, lines);
+                    store_piece(yp, o, lines);
                 } else if (row < a.rows) {
                     T e[CV];
                     __builtin_memcpy(e, &o, sizeof o);
@@ -638,7 +635,7 @@ static int launch_tile(const LinearF8Args& a, hipStream_t st) { return a.res ? l
 template <typename T>
 static int forward(LinearF8Args a, hipStream_t st) {
     const bool few = a.rows <= LF_FEW;
-    if (a.x && !(few && few_from_x<T>(a))) {
+    if (a.x && !few_from_x(sizeof(T) == 2 ? PSERVE_BF16 : PSERVE_F32, a.rows, a.N)) {
         PS_TRY(launch_rows_write<T>(a.x, a.ldx, a.rows, a.K, a.x8, a.sx, st));
         a.x = nullptr;
     }
@@ -658,7 +655,10 @@ static int run_product(const char* who, const pserve_linear_f8_t* op, LinearF8Ar
     PS_REQUIRE(dev == op->device, "%s: the weights are on device %d, the current one is %d", who, op->device, dev);
     const uintptr_t es = dtype_size(op->dtype);
     PS_REQUIRE(!(((uintptr_t)a.x | (uintptr_t)y | (uintptr_t)residual) & (es - 1)), "%s: x, y or residual is not aligned to its type", who);
-    a.x8 = (uint8_t*)rows8; a.sx = a.x8 + (size_t)a.rows * op->Kp;
+    if (rows8) {
+        a.x8 = (uint8_t*)rows8;
+        a.sx = a.x8 + (size_t)a.rows * op->Kp;
+    }
     a.res = residual; a.y = y;
     a.w8 = op->w; a.sw = op->scale; a.b = op->b;
     a.K = op->K; a.N = op->N; a.Kp = op->Kp; a.Np = op->Np; a.Sp = op->Sp;
@@ -742,7 +742,7 @@ void pserve_linear_f8_free(pserve_linear_f8_t* op) { delete op; }
 int pserve_linear_f8_workspace(const pserve_linear_f8_t* op, int64_t rows, size_t* bytes) {
     PS_REQUIRE(op && bytes, "pserve_linear_f8_workspace: NULL argument");
     PS_TRY(rows_ok("pserve_linear_f8", rows, op->K));
-    *bytes = f8_bytes(rows, op->K);
+    *bytes = few_from_x(op->dtype, rows, op->N) ? 0 : f8_bytes(rows, op->K);
     return PSERVE_OK;
 }
 
@@ -753,7 +753,7 @@ int pserve_linear_f8_forward(const pserve_linear_f8_t* op, const void* x, int64_
     size_t need = 0;
     PS_TRY(pserve_linear_f8_workspace(op, rows, &need));
     if (rows == 0) return PSERVE_OK;
-    PS_REQUIRE(x && y && workspace, "%s: NULL buffer", who);
+    PS_REQUIRE(x && y && (workspace || need == 0), "%s: NULL buffer", who);
     PS_REQUIRE(ldx >= op->K || rows == 1, "%s: rows of x %lld apart, K = %d", who, (long long)ldx, op->K);
     PS_REQUIRE(workspace_bytes >= need && !((uintptr_t)workspace & 15), "%s: workspace of %zu bytes, %zu needed (16-byte aligned)", who, workspace_bytes, need);
     LinearF8Args a{};

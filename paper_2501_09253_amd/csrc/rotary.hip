@@ -139,7 +139,7 @@ rotary_kernel(RotaryArgs a, Divisor items, Divisor heads) {
             if (len[k] == V) {
                 u32x4 o;
                 __builtin_memcpy(&o, v[k], sizeof o);
-                store_piece(reinterpret_cast<Any*>(out + at[k]), o, a.lines);
+                store_piece(out + at[k], o, a.lines);
             } else {
 #pragma unroll
                 for (int e = 0; e < V; ++e)
