@@ -18,9 +18,11 @@ constexpr uint32_t F8_NAN4 = 0x7f7f7f7fu;
 constexpr uint32_t F8_LARGEST_BITS = 0x7f600000u;      // 448 * 2^119
 constexpr uint32_t F8_FIRST_BYTE = 127 - 100, F8_LAST_BYTE = 127 + 119;
 
-// rows of K values: [rows][f8_width(K)] numbers, then [rows][f8_scales(K)] scale bytes (whole words of four)
+// rows of K values: [rows][f8_width(K)] numbers, then the scale bytes in words of four blocks, [f8_scales(K) / 4][rows]: what neighbouring lanes read for neighbouring
+// rows is in one line (with the bytes of a row side by side, 32 or 64 apart, reading them was half the time of a layer of few rows)
 __host__ __device__ inline int32_t f8_width(int32_t K) { return (K + 127) / 128 * 128; }
 __host__ __device__ inline int32_t f8_scales(int32_t K) { return (K + 511) / 512 * 4; }
+__device__ __forceinline__ int64_t f8_scale_at(int64_t rows, int64_t row, int b) { return 4 * ((b >> 2) * rows + row) + (b & 3); }
 inline size_t f8_bytes(int64_t rows, int32_t K) { return (size_t)rows * (size_t)(f8_width(K) + f8_scales(K)); }
 
 // four numbers of a word: x / 2^e for two values of each pair, as the scaled conversion rounds them (the same as a multiplication and a conversion)

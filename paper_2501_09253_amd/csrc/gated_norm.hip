@@ -246,9 +246,9 @@ gated_norm_kernel(NormArgs a) {
             uint32_t m = lanes_max<16>(f8_largest(v[i]));
             if (LANES == 32) m = max_16_apart(m);
             F8Scale(m).pack(v[i], a.v8 + row * Kp + V * c);
-            if (c % LANES == 0) a.s8[row * Sp + c / LANES] = (uint8_t)F8Scale(m).byte;
+            if (c % LANES == 0) a.s8[f8_scale_at(a.rows, row, c / LANES)] = (uint8_t)F8Scale(m).byte;
             if (c == 0)
-                for (int b = Kp / 128; b < Sp; ++b) a.s8[row * Sp + b] = 127;
+                for (int b = Kp / 128; b < Sp; ++b) a.s8[f8_scale_at(a.rows, row, b)] = 127;
         }
     }
 }

@@ -12,9 +12,9 @@
 using namespace pserve;
 
 struct pserve_linear_f8_s {
-    int32_t K = 0, N = 0, Kp = 0, Np = 0, Sp = 0, dtype = 0;
+    int32_t K = 0, N = 0, Kp = 0, Np = 0, dtype = 0;
     int device = 0;
-    uint8_t *w = nullptr, *scale = nullptr;     // [Np][Kp], [Np][Sp]
+    uint8_t *w = nullptr, *scale = nullptr;     // [Np][Kp], [words of four blocks][Np][4]
     float* b = nullptr;                         // [Np]
     pserve::DevicePool pool;
 };
@@ -39,17 +39,17 @@ __device__ __forceinline__ bf16x8 f8_as_bf16(const i32x8& v, int q, int byte) {
 struct LinearF8Args {
     const void *x, *res;
     void* y;
-    uint8_t *x8, *sx;                           // [rows][Kp], [rows][Sp]
+    uint8_t *x8, *sx;                           // [rows][Kp], [words of four blocks][rows][4]
     const uint8_t *w8, *sw;
     const float* b;
     int64_t rows, ldx;
-    int32_t K, N, Kp, Np, Sp;
+    int32_t K, N, Kp, Np;
 };
 
 // ---- weights: a tile of 128 of K x 64 channels, turned round in LDS
 template <typename T>
 __global__ void __launch_bounds__(256)
-linear_f8_pack_kernel(const T* w, int32_t K, int32_t N, int32_t Kp, int32_t Sp, uint8_t* out, uint8_t* scale) {
+linear_f8_pack_kernel(const T* w, int32_t K, int32_t N, int32_t Kp, int32_t Np, uint8_t* out, uint8_t* scale) {
     __shared__ float tile[64][132];
     __shared__ uint32_t s_max[4][64];
     const int n0 = blockIdx.x * 64, k0 = blockIdx.y * 128, c = threadIdx.x & 63, r = threadIdx.x >> 6, n = n0 + c;
@@ -71,7 +71,7 @@ linear_f8_pack_kernel(const T* w, int32_t K, int32_t N, int32_t Kp, int32_t Sp, 
         for (int e = 0; e < 8; ++e) v[e] = tile[j][32 * q + 8 * i + e];
         z.pack(v, o + 8 * i);
     }
-    if (q == 0) scale[(int64_t)(n0 + j) * Sp + blockIdx.y] = (uint8_t)z.byte;
+    if (q == 0) scale[f8_scale_at(Np, n0 + j, blockIdx.y)] = (uint8_t)z.byte;
 }
 
 // ---- rows of x: a block of 128 is sixteen lanes of eight values each; blocks are numbered row by row
@@ -97,19 +97,19 @@ f8_rows_write_kernel(const T* x, int64_t ldx, int64_t rows, int32_t K, uint8_t* 
     }
     const F8Scale z(lanes_max<16>(largest8(0u, r)));
     *reinterpret_cast<q8_u32x2*>(x8 + row * Kp + 8 * c) = z.pack8(r);
-    if (lane == 0) sx[row * Sp + b] = (uint8_t)z.byte;
+    if (lane == 0) sx[f8_scale_at(rows, row, b)] = (uint8_t)z.byte;
     if (lane == 0 && b == 0)
-        for (int i = KB; i < Sp; ++i) sx[row * Sp + i] = 127;
+        for (int i = KB; i < Sp; ++i) sx[f8_scale_at(rows, row, i)] = 127;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256)
 f8_rows_read_kernel(const uint8_t* x8, const uint8_t* sx, int64_t rows, int32_t K, T* x, int64_t ldx) {
-    const int Kp = f8_width(K), Sp = f8_scales(K), words = (K + 3) / 4;
+    const int Kp = f8_width(K), words = (K + 3) / 4;
     const int64_t i = block_of_lines() * 256 + threadIdx.x, row = i / words;
     if (row >= rows) return;
     const int k = 4 * (int)(i - row * words);
-    const float s = f8_scale_value(sx[row * Sp + k / 128]);
+    const float s = f8_scale_value(sx[f8_scale_at(rows, row, k / 128)]);
     const uint32_t w = *reinterpret_cast<const uint32_t*>(x8 + row * Kp + k);
     const float v[4] = {__builtin_amdgcn_cvt_f32_fp8(w, 0), __builtin_amdgcn_cvt_f32_fp8(w, 1), __builtin_amdgcn_cvt_f32_fp8(w, 2), __builtin_amdgcn_cvt_f32_fp8(w, 3)};
 #pragma unroll
@@ -129,30 +129,30 @@ static int launch_rows_write(const void* x, int64_t ldx, int64_t rows, int32_t K
 // block, 16 g4 .. + 15 and 64 + 16 g4 .. + 15), the next block's in flight; the sums meet in LDS, in a fixed order.  FROM_X: rows of x are rounded on the way
 // in, by every block for itself (a row's block of 128 is four lanes).
 
-template <typename T, int MT, int NT, int WV, bool FROM_X>
-__global__ void __launch_bounds__(64 * WV)
+template <typename T, int MT, int NT, bool FROM_X>
+__global__ void __launch_bounds__(512)
 linear_f8_few_kernel(LinearF8Args a) {
-    constexpr int BM = 16 * MT, BN = 16 * NT, RS = BN + 4;              // RS: values of a row in LDS
+    constexpr int WV = 8, BM = 16 * MT, BN = 16 * NT, RS = BN + 4;      // wavefronts; RS: values of a row in LDS
     __shared__ __attribute__((aligned(16))) float s_sum[WV][BM * RS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, g4 = lane >> 4;
     const int n0 = blockIdx.x * BN;
-    const int KT = a.Kp / 128;                                          // blocks, dealt to the wavefronts in shares
-    const int per = (KT + WV - 1) / WV, k0 = min(KT, wave * per), k1 = min(KT, k0 + per);
+    const int64_t m0 = (int64_t)blockIdx.y * BM;
+    const int KT = a.Kp / 128;                                          // blocks, dealt to the wavefronts in turn
     const uint8_t *wp[NT], *wsp[NT], *xp[MT], *xsp[MT];
     const T* xv[MT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
         wp[j] = a.w8 + (int64_t)(n0 + 16 * j + col) * a.Kp + 16 * g4;  // (there are N rounded up to 256)
-        wsp[j] = a.sw + (int64_t)(n0 + 16 * j + col) * a.Sp;
+        wsp[j] = a.sw + 4 * (int64_t)(n0 + 16 * j + col);
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int64_t r = min((int64_t)(16 * i + col), a.rows - 1);
+        const int64_t r = min(m0 + 16 * i + col, a.rows - 1);
         if constexpr (FROM_X) {
             xv[i] = (const T*)a.x + r * a.ldx;
         } else {
             xp[i] = a.x8 + r * a.Kp + 16 * g4;
-            xsp[i] = a.sx + r * a.Sp;
+            xsp[i] = a.sx + 4 * r;
         }
     }
     typedef typename AnyPiece<T>::type Any;
@@ -172,7 +172,7 @@ linear_f8_few_kernel(LinearF8Args a) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
             w[set][j] = operand(wp[j] + (int64_t)k * 128);
-            ws[set][j] = wsp[j][k];
+            ws[set][j] = wsp[j][f8_scale_at(a.Np, 0, k)];
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
@@ -193,7 +193,7 @@ linear_f8_few_kernel(LinearF8Args a) {
                 }
             } else {
                 x[set][i] = operand(xp[i] + (int64_t)k * 128);
-                xs[set][i] = xsp[i][k];
+                xs[set][i] = xsp[i][f8_scale_at(a.rows, 0, k)];
             }
         }
     };
@@ -226,14 +226,13 @@ linear_f8_few_kernel(LinearF8Args a) {
             }
         }
     };
-    if (k0 < k1) load(0, k0);
-    for (int k = k0; k < k1; k += 2) {
-        if (k + 1 < k1) load(1, k + 1);
-        mma(0);
-        if (k + 1 >= k1) break;
-        if (k + 2 < k1) load(0, k + 2);
-        mma(1);
-    }
+    // (each end has code of its own: where a load may or may not have been made, the wait in front of an instruction is for all of them)
+    int k = wave, n = (KT - wave + WV - 1) / WV;            // next block, how many
+    auto next = [&](int set) { load(set, k); k += WV; };
+    if (n > 0) next(0);
+    for (; n >= 3; n -= 2) { next(1); mma(0); next(0); mma(1); }
+    if (n == 2) { next(1); mma(0); mma(1); }
+    else if (n == 1) mma(0);
     // ---- the wavefronts' sums meet: the lane has row `col` of a tile and channels 4 g4 .. + 3
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -242,13 +241,13 @@ linear_f8_few_kernel(LinearF8Args a) {
     __syncthreads();
     for (int idx = tid; idx < BM * BN / 4; idx += 64 * WV) {
         const int r = idx / (BN / 4), c = idx % (BN / 4) * 4, n = n0 + c;
-        if (r >= a.rows || n >= a.N) continue;
+        if (m0 + r >= a.rows || n >= a.N) continue;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < WV; ++i) s += *reinterpret_cast<const f32x4*>(&s_sum[i][r * RS + c]);
         const f32x4 b = a.b ? *reinterpret_cast<const f32x4*>(a.b + n) : f32x4{0.f, 0.f, 0.f, 0.f};
-        T* yp = (T*)a.y + (int64_t)r * a.N + n;
-        const T* rp = (const T*)a.res + (int64_t)r * a.N + n;
+        T* yp = (T*)a.y + (m0 + r) * a.N + n;
+        const T* rp = (const T*)a.res + (m0 + r) * a.N + n;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (n + e >= a.N) break;
@@ -259,25 +258,14 @@ linear_f8_few_kernel(LinearF8Args a) {
     }
 }
 
-template <typename T, int MT, int NT, int WV, bool FROM_X>
+template <typename T, int MT, int NT, bool FROM_X>
 static int launch_few_as(const LinearF8Args& a, hipStream_t st) {
-    linear_f8_few_kernel<T, MT, NT, WV, FROM_X><<<(unsigned)cdiv(a.N, 16 * NT), 64 * WV, 0, st>>>(a);
+    linear_f8_few_kernel<T, MT, NT, FROM_X><<<dim3((unsigned)cdiv(a.N, 16 * NT), (unsigned)cdiv(a.rows, 16 * MT)), 512, 0, st>>>(a);
     return check_launch("linear_f8_few_kernel");
 }
-constexpr int LF_FEW = 32;                      // rows
-// us in a captured stream, a launch of 2.4 for the rows of x included: 12 x 4096 x 4096 bf16 9.7 rounded in here, 9.9 in a launch of its own (which costs the host another
-// launch, too); 16 x 8192 x 8192 34 and 23, 32 x 4096 x 4096 14.6 and 13.4, 12 x 4096 x 4096 fp32 13.1 and 10.1: every block reads all of x
-static bool few_from_x(int dtype, int64_t rows, int32_t N) { return dtype == PSERVE_BF16 && rows <= 16 && N < 6144; }
-// 32 channels a block where that still makes 192 blocks (16 x 8192 x 8192 25.5 -> 19.8, 12 x 1536 x 6144 5.5 -> 4.9, but 12 x 4096 x 4096 7.5 -> 10.0).  Four
-// row tiles are slower than tiles in LDS (33 x 4096 x 4096 17.4 and 14.5)
-template <typename T>
-static int launch_few(const LinearF8Args& a, hipStream_t st) {
-    if constexpr (sizeof(T) == 2)
-        if (a.x) return a.Kp >= 2048 ? launch_few_as<T, 1, 1, 16, true>(a, st) : launch_few_as<T, 1, 1, 8, true>(a, st);
-    if (a.N >= 6144) return a.rows <= 16 ? launch_few_as<T, 1, 2, 8, false>(a, st) : launch_few_as<T, 2, 2, 8, false>(a, st);
-    if (a.rows <= 16) return a.Kp >= 2048 ? launch_few_as<T, 1, 1, 16, false>(a, st) : launch_few_as<T, 1, 1, 8, false>(a, st);
-    return a.Kp >= 2048 ? launch_few_as<T, 2, 1, 16, false>(a, st) : launch_few_as<T, 2, 1, 8, false>(a, st);
-}
+// Rows rounded on the way in: every block reads all of x.  us in a captured stream, with a launch for the rows of x: 12 x 4096 x 4096 bf16 8.2 rounded in here, 8.9 in a
+// launch of its own (which costs the host another launch, too), 12 x 8192 x 640 12.5 and 12.4, 12 x 8192 x 8192 27 and 21
+static bool few_from_x(int dtype, int64_t rows, int32_t N) { return dtype == PSERVE_BF16 && rows <= 16 && N <= 4096; }
 
 // ---- many tiles: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, a ring of NS stages of HB half blocks (64 of K) in LDS.
 // A lane's operand of the 32 x 32 x 64 instruction is two 16-byte chunks of a row, chunks fh and 2 + fh of the half block's four (any order of K
@@ -340,7 +328,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
 #pragma unroll
         for (int l = 0; l < S_LD; ++l) {
             const int r = tid + l * 64 * NW;
-            s_base[l] = r < BM ? a.sx + (m0 + min(r, last)) * a.Sp : a.sw + (int64_t)(n0 + min(r - BM, lastB)) * a.Sp;
+            s_base[l] = r < BM ? a.sx + 4 * (m0 + min(r, last)) : a.sw + 4 * (int64_t)(n0 + min(r - BM, lastB));
         }
     };
     int odd = 0;                                            // half of the biases
@@ -354,7 +342,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
 #pragma unroll
         for (int l = 0; l < S_LD; ++l)
             if (64 * (wave + l * NW) < BM + BN)
-                __builtin_amdgcn_global_load_lds((const void*)(s_base[l] + 4 * group), (lds_void*)(s_scale + (group & 1) * (BM + BN) + 64 * (wave + l * NW)), 4, 0, 0);
+                __builtin_amdgcn_global_load_lds((const void*)(s_base[l] + 4 * group * (64 * (wave + l * NW) < BM ? a.rows : (int64_t)a.Np)), (lds_void*)(s_scale + (group & 1) * (BM + BN) + 64 * (wave + l * NW)), 4, 0, 0);
     };
     // step h of 64 HB of K into stage st.  One load instruction a call, so that a refill is spread over the matrix instructions behind the barrier that frees
     // its stage
@@ -608,38 +596,49 @@ static int launch_tile_as(const LinearF8Args& a, hipStream_t st) {
     linear_f8_tile_kernel<T, RES, WGM, WGN, TM, TN, HB, NS><<<grid, 64 * Cfg::NW, Cfg::LDS, st>>>(a, (int)mt, (int)total);
     return check_launch("linear_f8_tile_kernel");
 }
-// Of the tiles the one with the least time by its rounds (256 blocks at a time of the largest tile, 512 of the others, of which the last round's are alone
-// on their CUs), us a round: so much for each block of K and so much for its beginning and end, fitted to (256 x 256 / 128 x 128 / 64 x 128 us, bf16) 12,544 x 1536 x 6144
+// The kernel with the least time by its rounds, us of a launch in a captured stream.
+// Blocks of few rows, 256 at once: so much for each 16 rows of operands and block of K (measured at K = 8192, 256 blocks of 16 x 16 / 16 x 32 / 32 x 32:
+// 10.4 / 15.1 / 18.5, K = 1536 3.8 / 4.7 / 5.3).  Tiles: 256 at once of the largest, 512 of the others, of which the last round's are alone
+// on their CUs; so much for each block of K and so much for its beginning and end, fitted to (256 x 256 / 128 x 128 / 64 x 128 us, bf16) 12,544 x 1536 x 6144
 // with a residual 158 / 164 / 197, 12,544 x 6144 x 1536 with one 164 / 144 / 177, 2048 x 4096 x 4096 46 / 36 / 45, 3000 x 3000 x 3000 37 / 43 / 41, 2048 x 2048 x 2048
 // 29 / 17 / 14, 100 x 2048 x 8192 25 / 13 / 9, 6000 x 1000 x 3000 with a residual 53 / 40 / 43; fp32: 8000 x 500 x 1500 with one 64 / 37 / 36 (the largest
-// tile's operands spill there, and it is left out), 500 x 3000 x 2000 68 / 26 / 19
+// tile's operands spill there, and it is left out), 500 x 3000 x 2000 68 / 26 / 19.  Tiles against few rows: 256 x 512 x 1024 5.1 / 3.7, 64 x 8192 x 1024 25 / 15,
+// 33 x 4096 x 4096 14.6 / 11, 200 x 4096 x 4096 15 / 32
 template <typename T, bool RES>
-static int launch_tile_res(const LinearF8Args& a, hipStream_t st) {
+static int launch_product(const LinearF8Args& a, hipStream_t st) {
     constexpr bool HALF = sizeof(T) == 2;
     const double KT = a.Kp / 128;
-    auto cost = [&](int bm, int bn, int at_once, double step, double ends) {
-        const int64_t tiles = cdiv(a.rows, bm) * cdiv(a.N, bn), rest = tiles % at_once;
-        const double last = rest == 0 ? 0.0 : at_once == 256 ? 1.0 : 0.55 + 0.45 * (double)rest / at_once;
-        return ((double)(tiles / at_once) + last) * (step * KT + ends);
+    auto few = [&](int mt, int nt) {
+        const int64_t blocks = cdiv(a.rows, 16 * mt) * cdiv(a.N, 16 * nt);
+        return blocks > 2048 ? 1e9 : 2.4 + (double)cdiv(blocks, 256) * (0.0625 * (mt + nt) * KT + 0.4);
     };
-    const double small = HALF ? cost(64, 128, 512, 0.64, RES ? 4.5 : 4.0) : cost(64, 128, 512, 1.05, 7.5);
-    const double mid = HALF ? cost(128, 128, 512, 1.06, RES ? 6.0 : 5.0) : cost(128, 128, 512, 1.85, 13.0);
+    auto tiles = [&](int bm, int bn, int at_once, double step, double ends) {
+        const int64_t total = cdiv(a.rows, bm) * cdiv(a.N, bn), rest = total % at_once;
+        const double last = rest == 0 ? 0.0 : at_once == 256 ? 1.0 : 0.55 + 0.45 * (double)rest / at_once;
+        return ((double)(total / at_once) + last) * (step * KT + ends);
+    };
+    const double small = HALF ? tiles(64, 128, 512, 0.64, RES ? 4.5 : 4.0) : tiles(64, 128, 512, 1.05, 7.5);
+    const double mid = HALF ? tiles(128, 128, 512, 1.06, RES ? 6.0 : 5.0) : tiles(128, 128, 512, 1.85, 13.0);
+    const double large = HALF ? tiles(256, 256, 256, 1.5, RES ? 14.0 : 11.0) : 1e9;
+    const double f11 = few(1, 1), f12 = few(1, 2), f22 = few(2, 2);
+    if (std::min(f11, std::min(f12, f22)) < std::min(small, std::min(mid, large)) + (HALF ? 1.3 : 0.0)) {      // (a launch of few bf16 tiles takes 1.3 more than the fit says)
+        if (f11 <= f12 && f11 <= f22) return launch_few_as<T, 1, 1, false>(a, st);
+        return f12 <= f22 ? launch_few_as<T, 1, 2, false>(a, st) : launch_few_as<T, 2, 2, false>(a, st);
+    }
     if constexpr (HALF)
-        if (cost(256, 256, 256, 1.5, RES ? 14.0 : 11.0) <= std::min(mid, small)) return launch_tile_as<T, RES, 4, 2, 2, 4, 1, 4>(a, st);
+        if (large <= std::min(mid, small)) return launch_tile_as<T, RES, 4, 2, 2, 4, 1, 4>(a, st);
     if (mid <= small) return launch_tile_as<T, RES, 2, 2, 2, 2, 2, 2>(a, st);
     return launch_tile_as<T, RES, 2, 2, 1, 2, 2, 3>(a, st);
 }
-template <typename T>
-static int launch_tile(const LinearF8Args& a, hipStream_t st) { return a.res ? launch_tile_res<T, true>(a, st) : launch_tile_res<T, false>(a, st); }
 
 template <typename T>
 static int forward(LinearF8Args a, hipStream_t st) {
-    const bool few = a.rows <= LF_FEW;
-    if (a.x && !few_from_x(sizeof(T) == 2 ? PSERVE_BF16 : PSERVE_F32, a.rows, a.N)) {
+    if (a.x) {
+        if constexpr (sizeof(T) == 2)
+            if (few_from_x(PSERVE_BF16, a.rows, a.N)) return launch_few_as<T, 1, 1, true>(a, st);
         PS_TRY(launch_rows_write<T>(a.x, a.ldx, a.rows, a.K, a.x8, a.sx, st));
-        a.x = nullptr;
     }
-    return few ? launch_few<T>(a, st) : launch_tile<T>(a, st);
+    return a.res ? launch_product<T, true>(a, st) : launch_product<T, false>(a, st);
 }
 
 static int rows_ok(const char* who, int64_t rows, int32_t K) {
@@ -661,7 +660,7 @@ static int run_product(const char* who, const pserve_linear_f8_t* op, LinearF8Ar
     }
     a.res = residual; a.y = y;
     a.w8 = op->w; a.sw = op->scale; a.b = op->b;
-    a.K = op->K; a.N = op->N; a.Kp = op->Kp; a.Np = op->Np; a.Sp = op->Sp;
+    a.K = op->K; a.N = op->N; a.Kp = op->Kp; a.Np = op->Np;
     return op->dtype == PSERVE_BF16 ? forward<uint16_t>(a, st) : forward<float>(a, st);
 }
 
@@ -716,15 +715,16 @@ int pserve_linear_f8_create(int32_t K, int32_t N, int dtype, const void* w, cons
     return guarded(who, [&]() -> int {
         std::unique_ptr<pserve_linear_f8_t> op(new pserve_linear_f8_t());
         op->K = K; op->N = N; op->dtype = dtype;
-        op->Kp = f8_width(K); op->Np = (int32_t)cdiv(N, 256) * 256; op->Sp = f8_scales(K);
+        op->Kp = f8_width(K); op->Np = (int32_t)cdiv(N, 256) * 256;
         PS_CHECK_HIP(hipGetDevice(&op->device));
         hipStream_t st = (hipStream_t)stream;
         PS_TRY(op->pool.alloc((void**)&op->w, (size_t)op->Np * op->Kp));
-        PS_TRY(op->pool.alloc((void**)&op->scale, (size_t)op->Np * op->Sp));
-        PS_CHECK_HIP(hipMemsetAsync(op->scale, 127, (size_t)op->Np * op->Sp, st));
+        const size_t scales = (size_t)op->Np * f8_scales(K);
+        PS_TRY(op->pool.alloc((void**)&op->scale, scales));
+        PS_CHECK_HIP(hipMemsetAsync(op->scale, 127, scales, st));
         const dim3 grid(op->Np / 64, op->Kp / 128);
-        if (dtype == PSERVE_BF16) linear_f8_pack_kernel<<<grid, 256, 0, st>>>((const uint16_t*)w, K, N, op->Kp, op->Sp, op->w, op->scale);
-        else linear_f8_pack_kernel<<<grid, 256, 0, st>>>((const float*)w, K, N, op->Kp, op->Sp, op->w, op->scale);
+        if (dtype == PSERVE_BF16) linear_f8_pack_kernel<<<grid, 256, 0, st>>>((const uint16_t*)w, K, N, op->Kp, op->Np, op->w, op->scale);
+        else linear_f8_pack_kernel<<<grid, 256, 0, st>>>((const float*)w, K, N, op->Kp, op->Np, op->w, op->scale);
         PS_TRY(check_launch("linear_f8_pack_kernel"));
         if (b) {
             PS_TRY(op->pool.alloc_t(&op->b, op->Np));

@@ -114,7 +114,7 @@ def test_requests(counts, C, dtype):
     rows8.buffer.fill_(33)
     ps.gated_norm(**gpu(t), post="layer", pre="rms", cu_rows=ints(cu), rows8=rows8)
     width, exponents = -(-C // 128) * 128, -(-C // 512) * 4
-    numbers, scales = rows8.buffer[:rows * width].view(rows, width), rows8.buffer[rows * width:].view(rows, exponents)
+    numbers, scales = rows8.buffer[:rows * width].view(rows, width), rows8.buffer[rows * width:].view(exponents // 4, rows, 4).transpose(0, 1)
     for part in (slice(0, front), slice(rows - behind, rows)):
         assert torch.all(numbers[part] == 33) and torch.all(scales[part] == 33)
 

@@ -33,10 +33,10 @@ def test_rows_bit_for_bit(rows, K, dtype):
     rows8 = ps.RowsF8(rows, K).write(x.cuda())
     code, scale, held = lo.f8_held(x)
     Kp, Sp = code.shape[1], -(-K // 512) * 4
-    numbers, scales = rows8.buffer[:rows * Kp].view(rows, Kp).cpu(), rows8.buffer[rows * Kp:].view(rows, Sp).cpu()
+    numbers, scales = rows8.buffer[:rows * Kp].view(rows, Kp).cpu(), rows8.buffer[rows * Kp:].view(Sp // 4, rows, 4).transpose(0, 1).reshape(rows, Sp).cpu()
     assert rows8.buffer.numel() == rows * (Kp + Sp)
     assert torch.equal(numbers & 127, code & 127) and torch.equal((numbers >= 128) & (code & 127 > 0), (code >= 128) & (code & 127 > 0))
-    assert torch.equal(scales[:, :scale.shape[1]], scale)
+    assert torch.equal(scales[:, :scale.shape[1]], scale) and torch.all(scales[:, scale.shape[1]:] == 127)
     for d in (ps.F32, ps.BF16):
         assert torch.equal(rows8.read(d).double().cpu(), held)
 
@@ -72,7 +72,8 @@ def test_rows_that_are_not_finite_and_rows_apart(dtype):
 
 SHAPES = [(1, 64, 64), (1, 1, 1), (3, 77, 5), (12, 256, 512), (16, 4100, 130), (17, 128, 255), (33, 640, 1280), (64, 1000, 77), (130, 320, 264),
           (257, 129, 1000), (300, 2048, 640), (128, 128, 128), (129, 8200, 40), (700, 1536, 768), (1100, 384, 1152), (2, 16384, 33), (15, 513, 16), (20, 2300, 100), (31, 300, 6200), (16, 2049, 6145), (17, 5000, 50),
-          (1300, 1100, 1030), (1281, 100, 1001), (5000, 700, 3400), (4200, 136, 4099)]
+          (1300, 1100, 1030), (1281, 100, 1001), (5000, 700, 3400), (4200, 136, 4099),
+          (40, 4100, 130), (250, 1027, 515), (100, 64, 4000), (17, 1500, 2050), (48, 2900, 33)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -119,10 +120,10 @@ def test_offsets_past_32_bits():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [1, 40, 200])
-def test_one_key_is_seen(rows, dtype):
+@pytest.mark.parametrize("rows,N", [(1, 96), (40, 96), (200, 96), (1500, 1500)])
+def test_one_key_is_seen(rows, N, dtype):
     """Every value of K counts once and with its own block's scale: x picks single values out of W, block after block."""
-    K, N = 700, 96
+    K = 700
     w = make(2, (K, N), DT[dtype]) * torch.logspace(-4, 4, K)[:, None].to(DT[dtype])
     layer = ps.LinearF8(w.cuda(), None, CODE[dtype])
     held = lo.f8_held(w.t().contiguous())[2].t()
@@ -136,7 +137,7 @@ def test_one_key_is_seen(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [5, 200])
+@pytest.mark.parametrize("rows", [5, 200, 20000])
 def test_rows_apart_and_in_place(rows, dtype):
     K, N = 96, 160
     wide, w, b = make(1, (rows, K + 24), DT[dtype]), make(2, (K, N), DT[dtype]), make(3, (N,), DT[dtype])
@@ -156,7 +157,7 @@ def test_rows_apart_and_in_place(rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows", [7, 150])
+@pytest.mark.parametrize("rows", [7, 150, 40000])
 def test_zeros_extremes_and_what_is_not_finite(rows, dtype):
     x, w = make(1, (rows, 300), DT[dtype]), make(2, (300, 48), DT[dtype])
     x[0], w[:, 3] = 0, 0
@@ -181,7 +182,7 @@ def test_largest_numbers():
     check(layer.forward(x.bfloat16().cuda()), x.bfloat16(), w.bfloat16(), None, None)
 
 
-@pytest.mark.parametrize("rows", [3, 150])
+@pytest.mark.parametrize("rows", [3, 150, 10000])
 def test_graph_streams_and_workspace(rows):
     x, w, res = make(1, (rows, 320), torch.bfloat16).cuda(), make(2, (320, 192), torch.bfloat16).cuda(), make(3, (rows, 192), torch.bfloat16).cuda()
     layer = ps.LinearF8(w, None, ps.BF16)

@@ -113,8 +113,8 @@ def test_rows_and_layers_refuse():
     refused(L.pserve_linear_f8_forward(None, P, 8, 4, None, P, 1000, P, None), "NULL")
     refused(L.pserve_linear_f8_forward_rows(None, P, 4, None, P, None), "NULL")
     refused(L.pserve_linear_f8_workspace(None, 4, C.byref(need)), "NULL")
-    layer = (C.c_int64 * 64)()                                  # an image of the fields that the checks read: K, N; rounded up; scales, dtype
-    layer[0], layer[1], layer[2] = 100 | 8 << 32, 128 | 256 << 32, 4 | 1 << 32
+    layer = (C.c_int64 * 64)()                                  # an image of the fields that the checks read: K, N; rounded up; dtype
+    layer[0], layer[1], layer[2] = 100 | 8 << 32, 128 | 256 << 32, 1
     assert L.pserve_linear_f8_workspace(layer, 40, C.byref(need)) == 0 and need.value == 40 * 132
     assert L.pserve_linear_f8_workspace(layer, 5, C.byref(need)) == 0 and need.value == 0      # (rounded on the way in)
     refused(L.pserve_linear_f8_workspace(layer, 1 << 26, C.byref(need)), "rows")
