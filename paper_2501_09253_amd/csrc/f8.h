@@ -19,7 +19,7 @@ constexpr uint32_t F8_LARGEST_BITS = 0x7f600000u;      // 448 * 2^119
 constexpr uint32_t F8_FIRST_BYTE = 127 - 100, F8_LAST_BYTE = 127 + 119;
 
 // rows of K values: [rows][f8_width(K)] numbers, then the scale bytes in words of four blocks, [f8_scales(K) / 4][rows]: what neighbouring lanes read for neighbouring
-// rows is in one line (with the bytes of a row side by side, 32 or 64 apart, reading them was half the time of a layer of few rows)
+// rows is in one line (with a row's bytes side by side, lanes 32 or 64 bytes apart, 16 x 8192 x 8192 took 20 us for 17.5, 8192^3 450 for 439)
 __host__ __device__ inline int32_t f8_width(int32_t K) { return (K + 127) / 128 * 128; }
 __host__ __device__ inline int32_t f8_scales(int32_t K) { return (K + 511) / 512 * 4; }
 __device__ __forceinline__ int64_t f8_scale_at(int64_t rows, int64_t row, int b) { return 4 * ((b >> 2) * rows + row) + (b & 3); }

@@ -6,6 +6,8 @@
 // s the request of the row, N nothing, v / sqrt(mean v^2 + eps) or (v - mean) / sqrt(variance + eps).  Bound by memory: a row is read
 // into registers once, both norms' sums are taken there (fp32; the variance from the deviations, a second walk over the registers), y
 // is rounded where it is stored and only there.  h is rounded to the call's type or to 8-bit rows, whose blocks of 128 are sixteen lanes.
+// 12,544 x 1536, bf16, both norms, gate, scale and shift: 29 us, 5.2 TB/s (a copy: 5.0; part of the inputs comes from the last-level cache); into 8-bit rows 34
+// (the rounding's instructions).  32 x 4096: 4.9, two sums' meetings behind the way to memory.
 #include "f8.h"
 
 using namespace pserve;
