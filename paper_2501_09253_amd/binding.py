@@ -994,8 +994,10 @@ class LinearF8:
         _need(b is None or (tuple(b.shape) == (w.shape[1],) and b.is_contiguous() and b.dtype == w.dtype), f"{who}: b must be contiguous [N] of the given dtype")
         self.dtype, self.K, self.N = dtype, _whole(who, "K", w.shape[0]), _whole(who, "N", w.shape[1])
         _check(lib().pserve_linear_f8_create(self.K, self.N, dtype, w.data_ptr(), None if b is None else b.data_ptr(), _stream(), C.byref(self._h)))
-        # workspace_bytes is linear in the rows but for a few, which may need none
-        self._dtype, self._row_bytes, self._bare = w.dtype, self.workspace_bytes(1 << 20) >> 20, max((r for r in (0, 1, 16) if self.workspace_bytes(r) == 0))
+        # workspace_bytes is linear in the rows but for a few, which need none
+        self._dtype, self._row_bytes, self._bare = w.dtype, self.workspace_bytes(1 << 20) >> 20, 0
+        while self.workspace_bytes(self._bare + 16) == 0:
+            self._bare += 16
 
     def workspace_bytes(self, rows: int) -> int:
         n = C.c_size_t()

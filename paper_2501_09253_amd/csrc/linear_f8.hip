@@ -268,9 +268,16 @@ static int launch_few_as(const LinearF8Args& a, hipStream_t st) {
     linear_f8_few_kernel<T, MT, NT, FROM_X><<<dim3((unsigned)cdiv(a.N, 16 * NT), (unsigned)cdiv(a.rows, 16 * MT)), 512, 0, st>>>(a);
     return check_launch("linear_f8_few_kernel");
 }
-// Rows rounded on the way in: every block reads all of x.  us in a captured stream, with a launch for the rows of x: 12 x 4096 x 4096 bf16 8.2 rounded in here, 8.9 in a
-// launch of its own (which costs the host another launch, too), 12 x 8192 x 640 12.5 and 12.4, 12 x 8192 x 8192 27 and 21
-static bool few_from_x(int dtype, int64_t rows, int32_t N) { return dtype == PSERVE_BF16 && rows <= 16 && N <= 4096; }
+// Few rows rounded on the way in, by blocks of 16 x 16: every one reads and rounds all of its rows, but it is one launch and not two (2.4 us in a captured stream, 3 of the
+// host's).  By rounds of 256 blocks and K; us in one / two launches: bf16 12 x 4096 x 4096 8.2 / 9.0, 64 x 1024 x 1024 4.8 / 6.4, 64 x 8192 x 1024 14.7 / 13.9, two rounds
+// 12 x 1536 x 8192 7.4 / 8.2, 64 x 2048 x 2048 8.8 / 8.4; fp32 64 x 1024 x 1024 5.5 / 6.5, 12 x 2048 x 4096 7.6 / 7.7, 12 x 4096 x 4096 11.7 / 9.7, two rounds
+// 64 x 512 x 2048 5.5 / 6.2
+static bool few_from_x(int dtype, int64_t rows, int32_t K, int32_t N) {
+    if (rows > 16384) return false;
+    const int64_t rounds = cdiv(cdiv(rows, 16) * cdiv(N, 16), 256);
+    const bool half = dtype == PSERVE_BF16;
+    return rounds == 1 ? K <= (half ? 6144 : 2048) : rounds <= 4 && rounds * K <= (half ? 2560 : 1024);
+}
 
 // ---- many tiles: WGM x WGN wavefronts of 32 TM rows x 32 TN channels, a ring of NS stages of HB half blocks (64 of K) in LDS.
 // A lane's operand of the 32 x 32 x 64 instruction is two 16-byte chunks of a row, chunks fh and 2 + fh of the half block's four (any order of K
@@ -639,8 +646,7 @@ static int launch_product(const LinearF8Args& a, hipStream_t st) {
 template <typename T>
 static int forward(LinearF8Args a, hipStream_t st) {
     if (a.x) {
-        if constexpr (sizeof(T) == 2)
-            if (few_from_x(PSERVE_BF16, a.rows, a.N)) return launch_few_as<T, 1, 1, true>(a, st);
+        if (few_from_x(sizeof(T) == 2 ? PSERVE_BF16 : PSERVE_F32, a.rows, a.K, a.N)) return launch_few_as<T, 1, 1, true>(a, st);
         PS_TRY(launch_rows_write<T>(a.x, a.ldx, a.rows, a.K, a.x8, a.sx, st));
     }
     return a.res ? launch_product<T, true>(a, st) : launch_product<T, false>(a, st);
@@ -747,7 +753,7 @@ void pserve_linear_f8_free(pserve_linear_f8_t* op) { delete op; }
 int pserve_linear_f8_workspace(const pserve_linear_f8_t* op, int64_t rows, size_t* bytes) {
     PS_REQUIRE(op && bytes, "pserve_linear_f8_workspace: NULL argument");
     PS_TRY(rows_ok("pserve_linear_f8", rows, op->K));
-    *bytes = few_from_x(op->dtype, rows, op->N) ? 0 : f8_bytes(rows, op->K);
+    *bytes = few_from_x(op->dtype, rows, op->K, op->N) ? 0 : f8_bytes(rows, op->K);
     return PSERVE_OK;
 }
 

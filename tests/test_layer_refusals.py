@@ -115,13 +115,13 @@ def test_rows_and_layers_refuse():
     refused(L.pserve_linear_f8_workspace(None, 4, C.byref(need)), "NULL")
     layer = (C.c_int64 * 64)()                                  # an image of the fields that the checks read: K, N; rounded up; dtype
     layer[0], layer[1], layer[2] = 100 | 8 << 32, 128 | 256 << 32, 1
-    assert L.pserve_linear_f8_workspace(layer, 40, C.byref(need)) == 0 and need.value == 40 * 132
+    assert L.pserve_linear_f8_workspace(layer, 40000, C.byref(need)) == 0 and need.value == 40000 * 132
     assert L.pserve_linear_f8_workspace(layer, 5, C.byref(need)) == 0 and need.value == 0      # (rounded on the way in)
     refused(L.pserve_linear_f8_workspace(layer, 1 << 26, C.byref(need)), "rows")
-    refused(L.pserve_linear_f8_forward(layer, P, 99, 40, None, P, 5280, P, None), "apart")
-    refused(L.pserve_linear_f8_forward(layer, P, 100, 40, None, P, 5279, P, None), "workspace")
-    refused(L.pserve_linear_f8_forward(layer, P, 100, 40, None, P + 8, 5280, P, None), "workspace")
-    refused(L.pserve_linear_f8_forward(layer, P, 100, 40, None, None, 5280, P, None), "NULL")
+    refused(L.pserve_linear_f8_forward(layer, P, 99, 40000, None, P, 5280000, P, None), "apart")
+    refused(L.pserve_linear_f8_forward(layer, P, 100, 40000, None, P, 5279999, P, None), "workspace")
+    refused(L.pserve_linear_f8_forward(layer, P, 100, 40000, None, P + 8, 5280000, P, None), "workspace")
+    refused(L.pserve_linear_f8_forward(layer, P, 100, 40000, None, None, 5280000, P, None), "NULL")
     refused(L.pserve_linear_f8_forward_rows(layer, P + 4, 5, None, P, None), "aligned")
     refused(L.pserve_linear_f8_forward_rows(layer, None, 5, None, P, None), "NULL")
     assert L.pserve_linear_f8_forward(layer, None, 100, 0, None, None, 0, None, None) == 0
