@@ -437,7 +437,8 @@ int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t l
  *   consecutive values of a row, the smallest of 2^-100 .. 2^119 with which no value of the block passes 448 (values beyond 448 * 2^119 are cut off
  *   there); a value is rounded once, to nearest, halves to even.  A block with an infinity or a NaN is NaN throughout.
  *   rows8 DEVICE, 16-byte aligned, pserve_f8_rows_bytes bytes: numbers [rows][K rounded up to 128] (zeros behind K), then the exponents + 127 as bytes
- *   [K / 512 rounded up][rows][4]: four blocks of a row side by side (127 behind the last block).
+ *   [K / 512 rounded up][rows][4]: four blocks of a row side by side (127 behind the last block).  Calls that take them take all rows: their number is part
+ *   of the layout.
  * pserve_f8_rows_write: x DEVICE [rows][K] of dtype, ldx elements between rows.  pserve_f8_rows_read: the values held, rounded to dtype (exact).
  * pserve_linear_f8: y = x W + b (+ residual) with rows of x and columns of W in that form.  W [K][N] is rounded once, a power of two for each output
  *   channel and 128 values of K; x in the call or before it (forward_rows).  Products are exact and summed in fp32; bf16 layers drop, of eight products

@@ -604,19 +604,23 @@ def _workspace(need: int, workspace, device, who: str):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
+def _end(t) -> int:
+    """The address behind a tensor's last value (dense or strided)."""
+    if t.is_contiguous():
+        return t.data_ptr() + t.nbytes
+    if t.numel() == 0:
+        return t.data_ptr()
+    return t.data_ptr() + (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) * t.element_size()
+
+
 def _apart(who: str, out, *inputs):
-    """`out` shares no byte with an input (dense or strided: the extents are compared)."""
-    def extent(t):
-        values = t.numel() if t.is_contiguous() else 1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
-        at = t.data_ptr()
-        return at, at + values * t.element_size()
-    if out.numel() == 0:
+    """`out` shares no byte with an input (the extents are compared)."""
+    o0, o1 = out.data_ptr(), _end(out)
+    if o0 == o1:
         return
-    o0, o1 = extent(out)
     for t in inputs:
-        if t is not None and t.numel():
-            a0, a1 = extent(t)
-            _need(a1 <= o0 or o1 <= a0, f"{who}: the output overlaps an input")
+        if t is not None and t.data_ptr() < o1:
+            _need(_end(t) <= max(o0, t.data_ptr()), f"{who}: the output overlaps an input")
 
 
 def _number(scale):
