@@ -619,8 +619,10 @@ def _apart(who: str, out, *inputs):
     if o0 == o1:
         return
     for t in inputs:
-        if t is not None and t.data_ptr() < o1:
-            _need(_end(t) <= max(o0, t.data_ptr()), f"{who}: the output overlaps an input")
+        if t is not None:
+            at = t.data_ptr()
+            if at < o1 and at < (end := at + t.nbytes if t.is_contiguous() else _end(t)) and end > o0:
+                raise PserveError(EINVAL, f"{who}: the output overlaps an input")
 
 
 def _number(scale):
@@ -1015,8 +1017,10 @@ class LinearF8:
         held = isinstance(x, RowsF8)
         _here(who, x.buffer if held else x, res, y, workspace)
         if held:
-            _need(x.K == self.K, f"{who}: rows of {x.K} values, K = {self.K}")
-            _need(workspace is None, f"{who}: rows in 8 bits take no workspace")
+            if x.K != self.K:
+                raise PserveError(EINVAL, f"{who}: rows of {x.K} values, K = {self.K}")
+            if workspace is not None:
+                raise PserveError(EINVAL, f"{who}: rows in 8 bits take no workspace")
             rows, source = x.rows, x.buffer
         else:
             if x.dim() != 2 or x.shape[1] != self.K or x.dtype != self._dtype:
@@ -1122,8 +1126,10 @@ def gated_norm(x, f=None, *, post: Optional[str] = None, post_gain=None, post_bi
         spaced.append(st[0] if rows > 1 else Cc)
         setattr(buffers, name, t.data_ptr())
     if rows8 is not None:
-        _need(h is None, f"{who}: h and rows8 at once")
-        _need((rows8.rows, rows8.K) == (rows, Cc), f"{who}: rows8 must have {rows} rows of {Cc} values")
+        if h is not None:
+            raise PserveError(EINVAL, f"{who}: h and rows8 at once")
+        if rows8.rows != rows or rows8.K != Cc:
+            raise PserveError(EINVAL, f"{who}: rows8 must have {rows} rows of {Cc} values")
     if y is not None or h is not None or rows8 is not None:
         vectors = (post_gain, post_bias, gate, pre_gain, pre_bias, scale, shift, cu_rows, which)
         for out, other in ((y, h), (h, y)):
