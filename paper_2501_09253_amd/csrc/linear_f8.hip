@@ -622,7 +622,7 @@ static int launch_product(const LinearF8Args& a, hipStream_t st) {
     const double KT = a.Kp / 128;
     auto few = [&](int mt, int nt) {
         const int64_t blocks = cdiv(a.rows, 16 * mt) * cdiv(a.N, 16 * nt);
-        return blocks > 2048 ? 1e9 : 2.4 + (double)cdiv(blocks, 256) * (0.0625 * (mt + nt) * KT + 0.4);
+        return blocks > 2048 ? 1e9 : 2.4 + (double)cdiv(blocks, 256) * (0.0625 * (mt + nt) * KT + (HALF ? 0.3 : 0.5));
     };
     auto tiles = [&](int bm, int bn, int at_once, double step, double ends) {
         const int64_t total = cdiv(a.rows, bm) * cdiv(a.N, bn), rest = total % at_once;
