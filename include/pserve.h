@@ -442,7 +442,8 @@ int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t l
  * pserve_f8_rows_write: x DEVICE [rows][K] of dtype, ldx elements between rows.  pserve_f8_rows_read: the values held, rounded to dtype (exact).
  * pserve_linear_f8: y = x W + b (+ residual) with rows of x and columns of W in that form.  W [K][N] is rounded once, a power of two for each output
  *   channel and 128 values of K; x in the call or before it (forward_rows).  Products are exact and summed in fp32; bf16 layers drop, of eight products
- *   of neighbouring K, what lies below 2^-13 of the largest (1e-4 of a result's size; its rounding takes 1.7e-3).  Then + b + residual, rounded once.
+ *   of neighbouring K, what lies below 2^-13 of the largest (of normal values 2e-5 of a result's size together; its rounding takes 1.7e-3, and comes out one
+ *   step apart for one result in a hundred).  Then + b + residual, rounded once.
  *   A row of x (column of W) with an infinity or a NaN gives NaN.
  * pserve_linear_f8_create: w DEVICE [K][N], b DEVICE [N] or NULL, of dtype; synchronises `stream`; the caller's buffers are not referenced afterwards.
  * pserve_linear_f8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y), y DEVICE [rows][N];
