@@ -618,31 +618,40 @@ static int launch_tile_as(const LinearF8Args& a, hipStream_t st) {
 // 29 / 17 / 14, 100 x 2048 x 8192 25 / 13 / 9, 6000 x 1000 x 3000 with a residual 53 / 40 / 43; fp32: 8000 x 500 x 1500 with one 64 / 37 / 36 (the largest
 // tile's operands spill there, and it is left out), 500 x 3000 x 2000 68 / 26 / 19.  Tiles against few rows: 256 x 512 x 1024 5.1 / 3.7, 64 x 8192 x 1024 25 / 15,
 // 33 x 4096 x 4096 14.6 / 11, 200 x 4096 x 4096 15 / 32
-template <typename T, bool RES>
-static int launch_product(const LinearF8Args& a, hipStream_t st) {
-    constexpr bool HALF = sizeof(T) == 2;
-    const double KT = a.Kp / 128;
+enum { LF_FROM_X = 1, LF_FEW_16_16 = 11, LF_FEW_16_32 = 12, LF_FEW_32_32 = 22, LF_TILES_64 = 64, LF_TILES_128 = 128, LF_TILES_256 = 256 };      // (few: groups of 16 rows, of 16 channels)
+static int product_form(bool half, bool res, int64_t rows, int32_t K, int32_t N) {
+    const double KT = f8_width(K) / 128;
     auto few = [&](int mt, int nt) {
-        const int64_t blocks = cdiv(a.rows, 16 * mt) * cdiv(a.N, 16 * nt);
-        return blocks > 2048 ? 1e9 : 2.4 + (double)cdiv(blocks, 256) * (0.0625 * (mt + nt) * KT + (HALF ? 0.3 : 0.5));
+        const int64_t blocks = cdiv(rows, 16 * mt) * cdiv(N, 16 * nt);
+        return blocks > 2048 ? 1e9 : 2.4 + (double)cdiv(blocks, 256) * (0.0625 * (mt + nt) * KT + (half ? 0.3 : 0.5));
     };
     auto tiles = [&](int bm, int bn, int at_once, double step, double ends) {
-        const int64_t total = cdiv(a.rows, bm) * cdiv(a.N, bn), rest = total % at_once;
+        const int64_t total = cdiv(rows, bm) * cdiv(N, bn), rest = total % at_once;
         const double last = rest == 0 ? 0.0 : at_once == 256 ? 1.0 : 0.55 + 0.45 * (double)rest / at_once;
         return ((double)(total / at_once) + last) * (step * KT + ends);
     };
-    const double small = HALF ? tiles(64, 128, 512, 0.64, RES ? 4.5 : 4.0) : tiles(64, 128, 512, 1.05, 7.5);
-    const double mid = HALF ? tiles(128, 128, 512, 1.06, RES ? 6.0 : 5.0) : tiles(128, 128, 512, 1.85, 13.0);
-    const double large = HALF ? tiles(256, 256, 256, 1.5, RES ? 14.0 : 11.0) : 1e9;
+    const double small = half ? tiles(64, 128, 512, 0.64, res ? 4.5 : 4.0) : tiles(64, 128, 512, 1.05, 7.5);
+    const double mid = half ? tiles(128, 128, 512, 1.06, res ? 6.0 : 5.0) : tiles(128, 128, 512, 1.85, 13.0);
+    const double large = half ? tiles(256, 256, 256, 1.5, res ? 14.0 : 11.0) : 1e9;
     const double f11 = few(1, 1), f12 = few(1, 2), f22 = few(2, 2);
-    if (std::min(f11, std::min(f12, f22)) < std::min(small, std::min(mid, large)) + (HALF ? 1.3 : 0.0)) {      // (a launch of few bf16 tiles takes 1.3 more than the fit says)
-        if (f11 <= f12 && f11 <= f22) return launch_few_as<T, 1, 1, false>(a, st);
-        return f12 <= f22 ? launch_few_as<T, 1, 2, false>(a, st) : launch_few_as<T, 2, 2, false>(a, st);
+    if (std::min(f11, std::min(f12, f22)) < std::min(small, std::min(mid, large)) + (half ? 1.3 : 0.0))      // (a launch of few bf16 tiles takes 1.3 more than the fit says)
+        return f11 <= f12 && f11 <= f22 ? LF_FEW_16_16 : f12 <= f22 ? LF_FEW_16_32 : LF_FEW_32_32;
+    if (half && large <= std::min(mid, small)) return LF_TILES_256;
+    return mid <= small ? LF_TILES_128 : LF_TILES_64;
+}
+
+template <typename T, bool RES>
+static int launch_product(const LinearF8Args& a, hipStream_t st) {
+    const int form = product_form(sizeof(T) == 2, RES, a.rows, a.K, a.N);
+    if constexpr (sizeof(T) == 2)
+        if (form == LF_TILES_256) return launch_tile_as<T, RES, 4, 2, 2, 4, 1, 4>(a, st);
+    switch (form) {
+        case LF_FEW_16_16: return launch_few_as<T, 1, 1, false>(a, st);
+        case LF_FEW_16_32: return launch_few_as<T, 1, 2, false>(a, st);
+        case LF_FEW_32_32: return launch_few_as<T, 2, 2, false>(a, st);
+        case LF_TILES_128: return launch_tile_as<T, RES, 2, 2, 2, 2, 2, 2>(a, st);
+        default: return launch_tile_as<T, RES, 2, 2, 1, 2, 2, 3>(a, st);
     }
-    if constexpr (HALF)
-        if (large <= std::min(mid, small)) return launch_tile_as<T, RES, 4, 2, 2, 4, 1, 4>(a, st);
-    if (mid <= small) return launch_tile_as<T, RES, 2, 2, 2, 2, 2, 2>(a, st);
-    return launch_tile_as<T, RES, 2, 2, 1, 2, 2, 3>(a, st);
 }
 
 template <typename T>
@@ -680,6 +689,11 @@ static int run_product(const char* who, const pserve_linear_f8_t* op, LinearF8Ar
 }  // namespace pserve
 
 extern "C" {
+
+// For tests (not in the header): the form of the product that a call takes, see LF_FROM_X ..
+int pserve_test_linear_f8_form(int dtype, int64_t rows, int32_t K, int32_t N, int from_x, int residual) {
+    return from_x && few_from_x(dtype, rows, K, N) ? LF_FROM_X : product_form(dtype == PSERVE_BF16, residual != 0, rows, K, N);
+}
 
 int pserve_f8_rows_bytes(int64_t rows, int32_t K, size_t* bytes) {
     PS_REQUIRE(bytes, "pserve_f8_rows_bytes: NULL argument");
