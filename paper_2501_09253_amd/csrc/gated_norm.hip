@@ -263,24 +263,39 @@ static int launch_norm_as(const NormArgs& a, hipStream_t st) {
 }
 // A row is a wavefront's, or a part of one, where its 16-byte chunks are that many lanes, and a block's else.  Outputs go past the caches (12,544 x 1536,
 // bf16, y and h: 39 -> 32 us, 4.9 TB/s; 300,000 x 64 41 -> 32); 8-bit rows do not: the product reads them next.
+// 10 x threads of a row (0: a block) + chunks of a thread
+static int norm_form(size_t size, int64_t rows, int32_t C, bool rows8) {
+    const int chunks = (int)cdiv(C, 16 / (int)size), least = rows8 ? F8_BLOCK * (int)size / 16 : 1;                 // (8-bit rows have whole blocks)
+    if (chunks <= 8 && least <= 8) return 81;
+    if (chunks <= 16 && least <= 16) return 161;
+    if (chunks <= 32) return 321;
+    if (chunks <= 64) return 641;
+    // (60,000 x 640, bf16: 91 us by blocks of 128, 75 by wavefronts; 500 x 640 the other way round)
+    if (chunks <= 128 && rows >= 8192) return 642;
+    return chunks <= 512 ? 1 : chunks <= 2048 ? 2 : 4;
+}
 template <typename T, bool EVEN>
 static int launch_norm(const NormArgs& a, hipStream_t st) {
-    const int chunks = (int)cdiv(a.C, 16 / sizeof(T)), least = a.v8 ? F8_BLOCK * (int)sizeof(T) / 16 : 1;           // (8-bit rows have whole blocks)
-    if (chunks <= 8 && least <= 8) return launch_norm_as<T, 8, 1, EVEN>(a, st);
-    if (chunks <= 16 && least <= 16) return launch_norm_as<T, 16, 1, EVEN>(a, st);
-    if (chunks <= 32) return launch_norm_as<T, 32, 1, EVEN>(a, st);
-    if (chunks <= 64) return launch_norm_as<T, 64, 1, EVEN>(a, st);
-    // (60,000 x 640, bf16: 91 us by blocks of 128, 75 by wavefronts; 500 x 640 the other way round)
-    if (chunks <= 128 && a.rows >= 8192) return launch_norm_as<T, 64, 2, EVEN>(a, st);
-    if (chunks <= 512) return launch_norm_as<T, 0, 1, EVEN>(a, st);
-    if (sizeof(T) == 2 || chunks <= 2048) return launch_norm_as<T, 0, 2, EVEN>(a, st);
-    if constexpr (sizeof(T) == 4) return launch_norm_as<T, 0, 4, EVEN>(a, st);
-    return PSERVE_OK;
+    const int form = norm_form(sizeof(T), a.rows, a.C, a.v8 != nullptr);
+    if constexpr (sizeof(T) == 4)               // (bf16: up to 2048 chunks)
+        if (form == 4) return launch_norm_as<T, 0, 4, EVEN>(a, st);
+    switch (form) {
+        case 81: return launch_norm_as<T, 8, 1, EVEN>(a, st);
+        case 161: return launch_norm_as<T, 16, 1, EVEN>(a, st);
+        case 321: return launch_norm_as<T, 32, 1, EVEN>(a, st);
+        case 641: return launch_norm_as<T, 64, 1, EVEN>(a, st);
+        case 642: return launch_norm_as<T, 64, 2, EVEN>(a, st);
+        case 1: return launch_norm_as<T, 0, 1, EVEN>(a, st);
+        default: return launch_norm_as<T, 0, 2, EVEN>(a, st);
+    }
 }
 
 }  // namespace pserve
 
 extern "C" {
+
+// For tests (not in the header): the form of a call, see norm_form
+int pserve_test_gated_norm_form(int dtype, int64_t rows, int32_t C, int rows8) { return norm_form(dtype_size(dtype), rows, C, rows8 != 0); }
 
 int pserve_gated_norm(const pserve_gated_norm_desc* d, const pserve_gated_norm_buffers* b, void* stream) {
     static const char who[] = "pserve_gated_norm";
