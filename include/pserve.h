@@ -428,7 +428,8 @@ int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t l
  *   (one of them must be).  y or h may be x or f (with the same stride); nothing else may overlap.
  *   cu_rows DEVICE int32 [n + 1], ascending: request s has the rows cu_rows[s] .. cu_rows[s + 1] - 1; NULL (n = 1 only): all rows.  which DEVICE
  *   int32 [n] or NULL: request s has the vectors which[s] of gate, scale and shift instead of s.  Rows of no request, and those of one whose
- *   which[s] is outside 0 .. n - 1, are left as they were.  A plan's CU_SEQLENS and PERM serve a plan's rows with vectors in caller order.
+ *   which[s] is outside 0 .. n - 1, are left as they were (undefined in a buffer that nothing was written to; a layer that takes such rows gives
+ *   undefined results for them, and for no other row).  A plan's CU_SEQLENS and PERM serve a plan's rows with vectors in caller order.
  *   rows8: h goes into 8-bit rows (below) of `rows` rows of C values, rounded once, in the place of h.
  * Errors: EINVAL (NULL, n <= 0, C above 16384, unknown dtype or norm, eps negative or not finite, scales not finite, 2^31 rows and more, row strides
  * below C, buffers off their type's alignment, h and rows8 at once, parts of a formula whose f or h is not there), EHIP.

@@ -952,7 +952,8 @@ def _interleaved(a, b) -> bool:
 
 
 class RowsF8:
-    """pserve_f8_rows: `rows` rows of K values in 8-bit floating point, a power of two for each block of 128."""
+    """pserve_f8_rows: `rows` rows of K values in 8-bit floating point, a power of two for each block of 128.  A row holds anything until it is written; a
+    layer's result for it is undefined then, those of the other rows are not touched by it."""
 
     def __init__(self, rows: int, K: int):
         import torch
@@ -1071,7 +1072,8 @@ def gated_norm(x, f=None, *, post: Optional[str] = None, post_gain=None, post_bi
     x, f [rows, C] (rows may lie further apart); gains and biases [C]; gate, scale, shift [n, C], one for each request; cu_rows int32 [n + 1]
     on the device: the rows of the requests (None: all rows are one request's), which int32 [n]: the vectors a request takes instead of its
     own.  plan: a plan's rows, with vectors in caller order.  What is None is left out.  y is returned where f is given (or y is), h where any part of its formula is
-    (or h is); rows8: h goes there, in 8 bits.  y or h may be x or f.  Rows of no request are not written.  Returns (y, h)."""
+    (or h is); rows8: h goes there, in 8 bits.  y or h may be x or f.  Rows of no request are not written: in buffers of the caller's they stay as they were,
+    in a y or h that is made here (and in RowsF8 not written before) they hold anything.  Returns (y, h)."""
     import torch
     who = "gated_norm"
     _here(who, x, f, post_gain, post_bias, gate, pre_gain, pre_bias, scale, shift, cu_rows, which, y, h, None if rows8 is None else rows8.buffer)

@@ -81,3 +81,20 @@ def test_a_layer_over_a_joint_plan(dtype, graph):
     wy, wh = lo.gated_norm(x, out, post="rms", post_gain=g2, gate=gate, pre="rms", pre_gain=g3, request=request)
     near(y, wy, dtype)
     near(h, wh, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,C,N", [(40, 640, 200), (40, 4100, 130), (300, 2048, 640), (700, 640, 768), (5000, 384, 3400), (8000, 600, 4001)])
+def test_rows_that_were_never_written(rows, C, N, dtype):
+    """What rows of no request hold in new 8-bit rows, numbers and powers of two that are NaN among it, has no part in the other rows' results."""
+    dt = DT[dtype]
+    x, layer = make(1, (rows, C), dt).cuda(), ps.LinearF8(make(2, (C, N), dt, C ** -0.5).cuda(), None, CODE[dtype])
+    cu = torch.tensor([1, rows // 2, rows - 2], dtype=torch.int32, device="cuda")
+    want = None
+    for fill in (0, 255, 127, 254):
+        rows8 = ps.RowsF8(rows, C)
+        rows8.buffer.fill_(fill)
+        ps.gated_norm(x, pre="rms", cu_rows=cu, rows8=rows8)
+        got = layer.forward(rows8)[1:rows - 2]
+        want = got if want is None else want
+        assert torch.isfinite(got).all() and torch.equal(got, want)
