@@ -336,7 +336,7 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  *   number of shares of the keys depends on them, never which keys count.
  *   workspace DEVICE, at least pserve_prompt_attention_workspace bytes (0 where none is needed; it holds the partial results
  *   of the shares and may be used for something else after the call in stream order): enough for this call and for
- *   pserve_kv8_attention with the same desc, with k_tokens = 0 for the latter alone.  o must not overlap an input.
+ *   pserve_kv8_attention with the same desc, with k_tokens = 0 for the latter alone.  o must not overlap an input, the workspace no other buffer.
  * Errors: EINVAL (NULL, n <= 0, heads % kv_heads, heads above 4096, head_dim not a multiple of 16 or above 128, unknown dtype,
  * negative sizes, more than 2^30 keys, pointers or strides that are no multiples of 16 bytes, strides of 2^24 elements and more
  * between tokens (the stride of a dimension of one is not looked at), a scale that times log2(e) is not finite in fp32, more
@@ -365,7 +365,7 @@ int  pserve_resample_forward(const pserve_resample_t* op, const pserve_plan_t* p
  * pserve_linear8_create: w DEVICE [K][N], b DEVICE [N] or NULL, of dtype; synchronises `stream`.  K + 4 bytes a column are
  *   kept (rounded up to 128 values, columns to 256); the caller's buffers are not referenced afterwards.
  * pserve_linear8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y),
- *   y DEVICE [rows][N]; workspace DEVICE, 16-byte aligned, at least pserve_linear8_workspace bytes.  y must not overlap x.
+ *   y DEVICE [rows][N]; workspace DEVICE, 16-byte aligned, at least pserve_linear8_workspace bytes.  y must not overlap x, the workspace no other buffer.
  * Errors: EINVAL (NULL, sizes <= 0, K above 131072, N above 2^24, 2^26 rows and more, ldx < K, workspace too small, another device than the current one),
  * ENOMEM, EHIP. */
 typedef struct {
@@ -448,7 +448,7 @@ int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t l
  *   A row of x (column of W) with an infinity or a NaN gives NaN.
  * pserve_linear_f8_create: w DEVICE [K][N], b DEVICE [N] or NULL, of dtype; synchronises `stream`; the caller's buffers are not referenced afterwards.
  * pserve_linear_f8_forward: x DEVICE [rows][K] with ldx elements between rows, residual DEVICE [rows][N] or NULL (it may be y), y DEVICE [rows][N];
- *   workspace DEVICE, 16-byte aligned, at least pserve_linear_f8_workspace bytes (0 where a few rows need none).  y must not overlap x.  pserve_linear_f8_forward_rows: the rows as
+ *   workspace DEVICE, 16-byte aligned, at least pserve_linear_f8_workspace bytes (0 where a few rows need none).  y must not overlap x, the workspace no other buffer.  pserve_linear_f8_forward_rows: the rows as
  *   rows8, no workspace.
  * Errors: EINVAL (NULL, sizes <= 0, K above 131072, N above 2^24, 2^26 rows and more, ldx < K, workspace too small, buffers off their alignment, another
  * device than the current one), ENOMEM, EHIP. */

@@ -592,8 +592,9 @@ def _ints(who: str, t, dtype, shape, name: str):
         raise PserveError(EINVAL, f"{who}: {name} must be contiguous {dtype} {tuple(shape)}")
 
 
-def _workspace(need: int, workspace, device, who: str):
-    """The caller's workspace, or one from torch's allocator for this call: (pointer, bytes, what keeps it alive)."""
+def _workspace(need: int, workspace, device, who: str, *beside):
+    """The caller's workspace, or one from torch's allocator for this call: (pointer, bytes, what keeps it alive).  `beside`: the call's buffers (None:
+    absent), which the bytes that the call needs of the caller's must lie apart from (the extents are compared)."""
     import torch
     if workspace is None:
         if need == 0:
@@ -601,7 +602,13 @@ def _workspace(need: int, workspace, device, who: str):
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
         return workspace.data_ptr(), need, workspace
     _need(workspace.is_contiguous(), f"{who}: the workspace must be contiguous")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    at, size = workspace.data_ptr(), workspace.nbytes
+    end = at + min(need, size)
+    if end > at:
+        for t in beside:
+            if t is not None and t.data_ptr() < end and _end(t) > at:
+                raise PserveError(EINVAL, f"{who}: the workspace overlaps another buffer")
+    return at, size, workspace
 
 
 def _end(t) -> int:
@@ -685,7 +692,7 @@ def prompt_attention(q, k, v, cu_q, cu_k=None, causal: bool = True, scale: Optio
     out = _prompt_out(who, q, out, k, v)
     d, need = _prompt_desc(cu_q.shape[0] - 1, q.shape[1], k.shape[1], q.shape[2], BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), _number(scale),
                            _whole(who, "max_q", max_q), _whole(who, "max_k", max_k), q.shape[0], k.shape[0], q.stride(), sk, sv, out.stride())
-    ws, nws, keep = _workspace(need, workspace, q.device, who)
+    ws, nws, keep = _workspace(need, workspace, q.device, who, q, k, v, cu_q, cu_k, out)
     _check(lib().pserve_prompt_attention(d, q.data_ptr(), k.data_ptr(), v.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(),
                                          ws, nws, out.data_ptr(), _stream()))
     return out
@@ -758,7 +765,7 @@ class KV8:
         out = _prompt_out(who, q, out)
         d, need = _prompt_desc(n, q.shape[1], self.kv_heads, self.head_dim, BF16 if q.dtype == torch.bfloat16 else F32, bool(causal), _number(scale),
                                _whole(who, "max_q", max_q), _whole(who, "max_k", max_k), q.shape[0], 0, q.stride(), (0, 0), (0, 0), out.stride())
-        ws, nws, keep = _workspace(need, workspace, q.device, who)
+        ws, nws, keep = _workspace(need, workspace, q.device, who, q, cu_q, key_len, table, out)
         _check(lib().pserve_kv8_attention(self._h, d, q.data_ptr(), cu_q.data_ptr(), key_len.data_ptr(), table.data_ptr(),
                                           table.shape[1], page, ws, nws, out.data_ptr(), _stream()))
         return out
@@ -814,7 +821,7 @@ class Linear8:
             y = torch.empty((rows, self.N), dtype=x.dtype, device=x.device)
         else:
             _apart(who, y, x, *([res] if res is not None and res.data_ptr() != y.data_ptr() else []))
-        ws, nws, keep = _workspace(rows * self._row_bytes, workspace, x.device, who)
+        ws, nws, keep = _workspace(rows * self._row_bytes, workspace, x.device, who, x, res, y)
         _check(lib().pserve_linear8_forward(self._h, x.data_ptr(), ldx, rows, None if res is None else res.data_ptr(), ws, nws, y.data_ptr(), _stream()))
         return y
 
@@ -1043,7 +1050,7 @@ class LinearF8:
         if held:
             _check(lib().pserve_linear_f8_forward_rows(self._h, source.data_ptr(), rows, rp, y.data_ptr(), _stream()))
             return y
-        ws, nws, keep = _workspace(0 if rows <= self._bare else rows * self._row_bytes, workspace, x.device, who)
+        ws, nws, keep = _workspace(0 if rows <= self._bare else rows * self._row_bytes, workspace, x.device, who, x, res, y)
         _check(lib().pserve_linear_f8_forward(self._h, x.data_ptr(), ldx, rows, rp, ws, nws, y.data_ptr(), _stream()))
         return y
 
