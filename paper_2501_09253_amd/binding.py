@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from array import array
+from bisect import bisect_left
 from functools import lru_cache
 from itertools import chain
 from typing import Dict, List, Optional, Sequence
@@ -1008,10 +1009,9 @@ class LinearF8:
         _need(b is None or (tuple(b.shape) == (w.shape[1],) and b.is_contiguous() and b.dtype == w.dtype), f"{who}: b must be contiguous [N] of the given dtype")
         self.dtype, self.K, self.N = dtype, _whole(who, "K", w.shape[0]), _whole(who, "N", w.shape[1])
         _check(lib().pserve_linear_f8_create(self.K, self.N, dtype, w.data_ptr(), None if b is None else b.data_ptr(), _stream(), C.byref(self._h)))
-        # workspace_bytes is linear in the rows but for a few, which need none
-        self._dtype, self._row_bytes, self._bare = w.dtype, self.workspace_bytes(1 << 20) >> 20, 0
-        while self.workspace_bytes(self._bare + 16) == 0:
-            self._bare += 16
+        # workspace_bytes is linear in the rows but for a few, up to so many groups of 16, which need none
+        self._dtype, self._row_bytes = w.dtype, self.workspace_bytes(1 << 20) >> 20
+        self._bare = 16 * bisect_left(range(1, 1 << 16), 1, key=lambda groups: self.workspace_bytes(16 * groups))
 
     def workspace_bytes(self, rows: int) -> int:
         n = C.c_size_t()
