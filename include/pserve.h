@@ -411,8 +411,8 @@ int  pserve_linear8_forward(const pserve_linear8_t* op, const void* x, int64_t l
  * pserve_rotary_create: axis HOST int32 [pairs] (0 .. axes - 1), freq HOST double [pairs], radians for a unit of position; synchronises `stream`.
  * pserve_rotary_forward: pos DEVICE float [tokens][axes] (whole or not; what is not finite makes the pairs of its axis NaN); q DEVICE [tokens][heads]
  *   [head_dim], k DEVICE [tokens][kv_heads][head_dim] (kv_heads = 0: none), any strides in elements between tokens and between heads, a head's
- *   values consecutive; q_out may be q (with q's strides) and k_out k, nothing else may overlap.  Angles are formed in 64 bits (2^-52
- *   of an angle off), sines and cosines are good to 2^-22, products and sums fp32, rounded once.
+ *   values consecutive; q_out may be q (with q's strides) and k_out k, nothing else may overlap.  Angles are formed in 64 bits (3 * 2^-53
+ *   of an angle off at most), sines and cosines are good to 2^-22, products and sums fp32, rounded once.
  * pserve_plan_positions: pos DEVICE float [T][3] of a plan's tokens: (frame of the request, y, x) of a latent pixel; text token j of a request
  *   has text[i] + j * text[3 + i], i = 0 .. 2.  frame DEVICE float [n], caller order (NULL: 0); text HOST float [6] (NULL: zeros).  Padding rows get 0.
  * Errors: EINVAL (NULL, axes above 8, pairs above 256, a frequency that is not finite or beyond 1e9, head_dim below 2 pairs or above 512, heads above

@@ -5,7 +5,8 @@
 // for each pair p of values of a head.  Bound by memory: every value is read and written once.  The angles are a token's, whatever its
 // heads are: a block computes those of its tokens once, into LDS, then walks its tokens' heads in 16-byte pieces.
 // An angle is taken in revolutions, in 64 bits (positions reach 2^24, and 32 bits leave a position of 2^17 with an angle off by 2^-7); the
-// fraction of a revolution is rounded to fp32, at most 2^-26 off: 2^-23.3 radians.
+// fraction of a revolution is rounded to fp32, at most 2^-26 off: 2^-23.3 radians.  2 pi, the quotient of a frequency by it and the product are rounded to 64 bits:
+// together at most 3 * 2^-53 of an angle (1.12 * 2^-52 seen), 2^-22 radians at 2^29.
 // bf16, heads of 64: 12,544 tokens of 48, neighbours paired, 29 us (5.3 TB/s, part of the values from the last-level cache), 131,072 tokens of 20, halves
 // paired, 141 (4.8); a large copy runs at 5.0.  48 tokens of 40 heads of 128: 4.7, the way to positions, values and back.
 #include "f8.h"

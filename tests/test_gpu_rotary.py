@@ -198,3 +198,22 @@ def test_graph_and_streams():
         torch.cuda.synchronize()
         want = rot.forward(q, k, pos)
         assert torch.equal(oq, want[0]) and torch.equal(ok, want[1])
+
+
+def test_far_angles_within_what_the_header_says():
+    """Angles around 2^35 radians against whole-number arithmetic: 3 * 2^-53 of an angle (three roundings in 64 bits; 2^-52 is passed), 2^-22 of a sine and cosine."""
+    from fractions import Fraction
+    import random
+    rng = random.Random(1)
+    two_pi = Fraction(62831853071795864769252867665590057683943387987502116419498891846156328125724, 10 ** 76)
+    freq, place = [rng.uniform(2048, 4096) for _ in range(256)], [rng.randint(2 ** 23, 2 ** 24) for _ in range(150)]
+    q = torch.zeros((150, 1, 512))
+    q[:, :, :256] = 1                                                   # (1, 0): the cosine and the sine themselves
+    got, _ = ps.Rotary([0] * 256, freq).forward(q.cuda(), None, torch.tensor(place, dtype=torch.float32)[:, None].cuda())
+    got = got.double().cpu()[:, 0]
+    turn = [[Fraction(p) * Fraction(f) / two_pi % 1 for f in freq] for p in place]
+    want = torch.tensor([[float(t) for t in row] for row in turn], dtype=torch.float64) * (2 * math.pi)
+    angle = torch.tensor(place, dtype=torch.float64)[:, None] * torch.tensor(freq, dtype=torch.float64)
+    tol = 3 * 2.0 ** -53 * angle + 2.0 ** -22
+    for part, exact in ((got[:, :256], torch.cos(want)), (got[:, 256:], torch.sin(want))):
+        assert torch.all((part - exact).abs() <= tol), ((part - exact).abs() / angle).max() * 2 ** 52
