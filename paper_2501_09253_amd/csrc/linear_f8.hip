@@ -488,7 +488,8 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
         const int64_t r0 = m0 + wm * WM;
         const int c0 = n0 + wn * WN;
         constexpr int CV = 16 / sizeof(T), PC = 8 * CV;     // values of a 16-byte chunk, columns of a piece
-        constexpr int PJ = PC / 32, NP = TN / PJ, PS = TM * NP, RQ = RES ? (PS < 4 ? PS : 4) : 1;      // accumulator tiles of a piece; pieces of 32 rows, of all; residuals under way
+        constexpr int PJ = PC / 32, NP = TN / PJ, PS = TM * NP, RQ = RES ? PS : 1;      // accumulator tiles of a piece; pieces of 32 rows, of all; those whose residuals are held
+        static_assert(!RES || PS <= 4, "registers of the residuals");
         const int nt = t + t_step, er = lane >> 3, ec = lane & 7;
         // whole lines go past the L2, which holds the panels; where rows begin inside a line, its parts meet there
         const bool lines = a.N % (8 * CV) == 0 && !((uintptr_t)a.y & 127);
@@ -511,12 +512,12 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
                         __builtin_memcpy(&v, e, sizeof v);
                     }
                 }
-                rres[p % RQ][k] = v;
+                rres[p][k] = v;
             }
         };
         if constexpr (RES) {
 #pragma unroll
-            for (int p = 0; p < RQ; ++p) res_load(p);
+            for (int p = 0; p < PS; ++p) res_load(p);
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // every wavefront has read its last fragments
         if (nt < t_end) {                                   // the first steps of the next tile come in beside the end of this one
@@ -541,8 +542,7 @@ linear_f8_tile_kernel(LinearF8Args a, int m_tiles, int total) {
             u32x4 beside[4];
             if constexpr (RES) {                            // the residual as the accumulators lie, through the staging
 #pragma unroll
-                for (int k = 0; k < 4; ++k) ep[(8 * k + er) * 8 + (ec ^ (((8 * k + er) >> 1) & 7))] = rres[p % RQ][k];
-                if (p + RQ < PS) res_load(p + RQ);
+                for (int k = 0; k < 4; ++k) ep[(8 * k + er) * 8 + (ec ^ (((8 * k + er) >> 1) & 7))] = rres[p][k];
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) beside[q] = ep[fr * 8 + chunk(q)];
