@@ -11,7 +11,8 @@
 // fp32 tensors: the numbers times their power of two are exact in bf16, and the bf16 instruction's sums are fp32 throughout.
 // Few rows are bound by how fast a CU takes in operands, few tiles by the way of a tile's first operands and its outputs, many by the matrix
 // cores (8192^3 427 us, 2,570 TFLOP/s, the clock at 1.7 GHz under their load) and, where K is short, by the outputs and residuals that a tile
-// moves while they wait (12,544 x 1536 x 6144 with a residual 140 us, 1,690 TFLOP/s: they are busy 44 % of the time).
+// moves while they wait (12,544 x 1536 x 6144 with a residual 142 us beside its rows' rounding, 1,670 TFLOP/s, and 147 .. 181 product
+// behind product, by the clock: they are busy 44 % of the time).
 #include "f8.h"
 
 using namespace pserve;
