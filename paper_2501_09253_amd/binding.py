@@ -607,7 +607,7 @@ def _workspace(need: int, workspace, device, who: str, *beside):
     end = at + min(need, size)
     if end > at:
         for t in beside:
-            if t is not None and t.data_ptr() < end and _end(t) > at:
+            if t is not None and (first := t.data_ptr()) < end and (first + t.nbytes if t.is_contiguous() else _end(t)) > at:
                 raise PserveError(EINVAL, f"{who}: the workspace overlaps another buffer")
     return at, size, workspace
 
